@@ -210,6 +210,94 @@ int moe_expert_ffn_fp8_gather(moe_ctx* ctx, const uint8_t* xq_tok, const float* 
 int moe_combine(moe_ctx* ctx, const float* y_perm, const int32_t* inv_perm, const float* topk_w,
                 uint16_t* y_bf16, float* y_f32);
 
+/* ---- The training side of a replayed layer ------------------------------------------------------------------------
+ * The trainer evaluates the layer again from the routing log (section 2.4.4) to get the log-probabilities of the
+ * rollout's tokens, and then differentiates.  The calls below are what stands around the layer there: the norm in front
+ * of it, the policy loss behind it, and the gradients of the token order, of the combine and of the FP8 products.
+ *   - `dtype` (MOE_BF16 or MOE_F32) is the element type of the arrays given as void*; everything is summed in fp32.
+ *   - Two-dimensional arrays are row-major; an `ld` is a row's distance in elements.
+ *   - All calls are deterministic: no atomic adds, sums in an order that depends on the sizes alone. */
+#define MOE_BF16 0
+#define MOE_F32  1
+
+/* Allocates the workspace that the calls marked [reserved] need (64 MiB and a little, once per context; a second call does
+ * nothing).  They return MOE_EINVAL on a context without it.  MOE_ENOMEM if the memory cannot be had. */
+int moe_reserve_gradients(moe_ctx* ctx);
+
+/* Residual addition and root-mean-square norm, with the norm's output quantised for the FP8 products if wanted:
+ *   h = x + residual, rounded to dtype;  r = 1/sqrt(mean_c h^2 + eps);  y = h * r * gain.
+ * The norm is that of h as stored, so that the backward call, which reads it, differentiates what was computed.
+ *   x [rows,cols] dtype, ld_x; residual likewise with ld_res, or NULL (h = x); gain [cols] f32.
+ *   sum [rows,cols] dtype: receives h; NULL if not wanted.  It may be x or residual itself where that has ld == cols.
+ *   y [rows,cols] dtype, or NULL.
+ *   q [rows,cols] u8 and scales [cols/128][rows] f32, or both NULL: y as moe_quantize_fp8 would code it, but from the
+ *   fp32 y: one rounding.  cols must then be a multiple of 128.
+ *   rstd [rows] f32: receives r; or NULL.
+ * 1 <= cols <= 65536, eps >= 0.  A row that holds a NaN or an infinity affects its own outputs only. */
+int moe_add_rmsnorm(moe_ctx* ctx, const void* x, const void* residual, const float* gain, int64_t rows, int32_t cols,
+                    int64_t ld_x, int64_t ld_res, int32_t dtype, float eps, void* sum, void* y, uint8_t* q, float* scales,
+                    float* rstd);
+
+/* Its gradient [reserved].  With u = gain * dy:
+ *   dx = r*u - h * r^3/cols * sum_c(u*h)  (+ dh),   dgain[c] = sum_rows dy*h*r.
+ * dx is the gradient of x and of residual alike.  An e4m3 output is passed straight through: dy is the gradient of y.
+ *   dy, h [rows,cols] dtype (h: `sum` of the forward call, or its x where there was no residual); rstd [rows] as written
+ *   there; dh [rows,cols] dtype or NULL: the gradient that reaches h on another path; dx [rows,cols] dtype, may be dy or
+ *   dh; dgain [cols] f32 (zeros for rows == 0). */
+int moe_add_rmsnorm_backward(moe_ctx* ctx, const void* dy, const void* h, const float* rstd, const float* gain,
+                             const void* dh, int64_t rows, int32_t cols, int32_t dtype, void* dx, float* dgain);
+
+/* Token rows in expert order: x_perm[inv_perm[t*k+j]] = x[t] for j < k.  T, d, k are the context's; inv_perm [N] as a
+ * routing call wrote it.  Slots whose inv_perm is negative (an invalid id) or not below N are skipped: rows of x_perm that no slot
+ * names are not written.  x [T,d], x_perm [N,d] dtype. */
+int moe_dispatch(moe_ctx* ctx, const void* x, const int32_t* inv_perm, int32_t dtype, void* x_perm);
+/* Its gradient: dx[t] = sum_{j<k} dx_perm[inv_perm[t*k+j]] (+ dx_add[t]), fp32 in slot order, one rounding.  Skipped slots add
+ * nothing.  dx_add [T,d] dtype or NULL, may be dx itself. */
+int moe_dispatch_backward(moe_ctx* ctx, const void* dx_perm, const int32_t* inv_perm, const void* dx_add, int32_t dtype,
+                          void* dx);
+/* Gradient of moe_combine.  For each assignment i = t*k+j with row p = inv_perm[i]:
+ *   dy_perm[p] = topk_w[i] * dy[t];   dw[i] = sum_c dy[t,c] * y_perm[p,c]   (0 for a skipped slot)
+ * and, where dlogits is given, the gradient of the router's logits through topk_w = softmax over the chosen logits:
+ *   dlogits[t, topk_idx[i]] = topk_w[i] * (dw[i] - sum_l topk_w[l]*dw[l]), 0 for every expert that the token did not choose
+ *   (an id repeated inside a token receives the sum of its slots, ids outside [0,E) none).
+ *   dy [T,d] dtype; y_perm [N,d] f32; dy_perm [N,d] dtype; dw [T,k] f32; topk_idx [T,k] and dlogits [T,E] f32, both or
+ *   neither NULL. */
+int moe_combine_backward(moe_ctx* ctx, const void* dy, const float* y_perm, const int32_t* inv_perm, const float* topk_w,
+                         const int32_t* topk_idx, int32_t dtype, void* dy_perm, float* dw, float* dlogits);
+
+/* Clipped policy loss with a KL and an entropy term, and its gradient in the logits [reserved].  Row t, z = logits/temperature:
+ *   logp = z[target] - log sum_v exp z[v];  entropy H = -sum_v p_v log p_v;  rho = exp(logp - old_logp)
+ *   row_loss = weight * ( -min(rho*A, clip(rho, 1-low, 1+high)*A) + kl_coef*(e^x - x - 1) - entropy_coef*H ),  x = ref_logp - logp
+ *   loss[0] = sum of row_loss;  dlogits = d loss / d logits.
+ *   logits [rows,V] dtype, ld; target [rows] i32; old_logp, advantage, weight [rows] f32; ref_logp [rows] or NULL (no KL term).
+ *   clip_rows [rows] f32 or NULL: a bound of its own for each row in place of both clip_low and clip_high.
+ *   logp, entropy, row_loss [rows] f32, loss [1] f32: outputs.
+ *   dlogits [rows,V] grad_dtype, ld_grad, or NULL: forward only.  It may be logits itself if both types and lds are equal.
+ * Logits of -inf are masked: p = 0 and no gradient.  Without effect on the loss (row_loss 0, gradient row zero) is a row with
+ * weight 0, with a target outside [0,V) (its logp is written as 0), or whose logits are all -inf (logp -inf, entropy 0).
+ * V >= 1, temperature > 0, clip bounds and coefficients finite and >= 0. */
+int moe_policy_loss(moe_ctx* ctx, const void* logits, int64_t ld, int32_t dtype, int64_t rows, int32_t V,
+                    const int32_t* target, const float* old_logp, const float* ref_logp, const float* advantage,
+                    const float* weight, const float* clip_rows, float clip_low, float clip_high, float kl_coef,
+                    float entropy_coef, float temperature, float* logp, float* entropy, float* row_loss, float* loss,
+                    void* dlogits, int64_t ld_grad, int32_t grad_dtype);
+
+/* Gradients of the block-scaled FP8 linear y = x*W^T from what its forward pass read: the e4m3 weights, and the 8-bit activations as
+ * the checkpoint of x [reserved].  Dense (offsets NULL, E = 1) or grouped: expert e owns rows [offsets[e], offsets[e+1]) of dy, dx and
+ * xq, and its own Wq[e], ws[e], dW[e] (offsets [E+1] i32 on the device, non-decreasing, from 0 to at most rows; values outside
+ * [0,rows] are taken as the nearest in it).
+ *   dx[p,c] = sum_n dy[p,n] * ws[n/128,c/128] * Wq[n,c]
+ *     exact products of bf16 and e4m3 on the matrix cores, fp32 sums and block scales; rows behind offsets[E] are not written.
+ *   dW[n,c] = sum_p dy[p,n] * xs[c/128,p] * xq[p,c]   (0 for an expert without rows); accumulate != 0: added to dW
+ *     the scale runs along the sum, so the operand is xs*xq: rounded to bf16 for a bf16 dW (an error the size of the output's own
+ *     rounding), held to 24 bits in three bf16 planes for a f32 dW.
+ *   dy [rows,NOUT] bf16; Wq [E,NOUT,K] u8; ws [E,NOUT/128,K/128] f32; xq [rows,K] u8; xs [K/128][rows] f32;
+ *   dx [rows,K] bf16; dW [E,NOUT,K] dtype.  K and NOUT multiples of 128, NOUT*K < 2^32 and 1 <= E <= 256; rows < 2^31 - 256. */
+int moe_linear_fp8_dgrad(moe_ctx* ctx, const uint16_t* dy, int64_t rows, int32_t NOUT, const uint8_t* Wq, const float* ws, int32_t K,
+                         const int32_t* offsets, int32_t E, uint16_t* dx);
+int moe_linear_fp8_wgrad(moe_ctx* ctx, const uint16_t* dy, int64_t rows, int32_t NOUT, const uint8_t* xq, const float* xs, int32_t K,
+                         const int32_t* offsets, int32_t E, int32_t accumulate, int32_t dtype, void* dW);
+
 /* Length-based load balancing before rollout (paper section 3.1.1): distributes n samples over
  * n_groups worker groups so that the groups' total predicted generation lengths are about equal.
  * The paper states the goal only; the rule taken is longest-first list scheduling: samples are

@@ -21,11 +21,16 @@ EXPORTS = ("moe_create", "moe_destroy", "moe_strerror", "moe_route", "moe_route_
            "moe_route_replay_ids", "moe_route_quantize", "moe_route_replay_quantize",
            "moe_check_ids", "moe_quantize_fp8", "moe_quantize_weights_fp8", "moe_linear_fp8", "moe_expert_ffn_fp8",
            "moe_expert_ffn_fp8_gather", "moe_combine", "moe_balance_lengths", "moe_debug_copy_hidden",
+           "moe_reserve_gradients", "moe_add_rmsnorm", "moe_add_rmsnorm_backward", "moe_dispatch", "moe_dispatch_backward",
+           "moe_combine_backward", "moe_policy_loss", "moe_linear_fp8_dgrad", "moe_linear_fp8_wgrad",
            "moe_probe_copy", "moe_probe_fp8_mfma", "moe_profile_enable", "moe_profile_read", "moe_version")
 
 
 class MoEError(RuntimeError):
     pass
+
+
+_shapes = {}                       # (T, d, E, k) of the contexts made here, for the checks of the calls that go by them
 
 
 class _Dims(ctypes.Structure):
@@ -64,6 +69,16 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.moe_combine.argtypes = [vp] * 6
     lib.moe_balance_lengths.argtypes = [vp, i64, i32, i32, vp, vp, vp, vp]
     lib.moe_debug_copy_hidden.argtypes = [vp, vp, vp]
+    f32 = ctypes.c_float
+    lib.moe_reserve_gradients.argtypes = [vp]
+    lib.moe_add_rmsnorm.argtypes = [vp, vp, vp, vp, i64, i32, i64, i64, i32, f32] + [vp] * 5
+    lib.moe_add_rmsnorm_backward.argtypes = [vp] * 6 + [i64, i32, i32, vp, vp]
+    lib.moe_dispatch.argtypes = [vp, vp, vp, i32, vp]
+    lib.moe_dispatch_backward.argtypes = [vp, vp, vp, vp, i32, vp]
+    lib.moe_combine_backward.argtypes = [vp] * 6 + [i32, vp, vp, vp]
+    lib.moe_policy_loss.argtypes = [vp, vp, i64, i32, i64, i32] + [vp] * 6 + [f32] * 5 + [vp] * 5 + [i64, i32]
+    lib.moe_linear_fp8_dgrad.argtypes = [vp, vp, i64, i32, vp, vp, i32, vp, i32, vp]
+    lib.moe_linear_fp8_wgrad.argtypes = [vp, vp, i64, i32, vp, vp, i32, vp, i32, i32, i32, vp]
     lib.moe_probe_copy.argtypes = [vp, vp, vp, i64]
     lib.moe_probe_fp8_mfma.argtypes = [vp, i32, i32, i32, vp]
     lib.moe_profile_enable.argtypes = [vp, i32]
@@ -98,10 +113,12 @@ def moe_create(T: int, d: int, E: int, k: int, F: int, stream: Optional[torch.cu
     dims = _Dims(T, d, E, k, F)
     h = ctypes.c_void_p()
     _check(lib.moe_create(ctypes.byref(h), ctypes.byref(dims), ctypes.c_void_p(s.cuda_stream)), "moe_create")
+    _shapes[h.value] = (T, d, E, k)
     return h.value
 
 
 def moe_destroy(ctx: int) -> None:
+    _shapes.pop(ctx, None)
     _check(load_library().moe_destroy(ctx), "moe_destroy")
 
 
@@ -203,6 +220,139 @@ def moe_combine(ctx, y_perm, inv_perm, topk_w, y, y_f32=None) -> None:
     _check(load_library().moe_combine(ctx, _ptr(y_perm, torch.float32), _ptr(inv_perm, torch.int32),
                                       _ptr(topk_w, torch.float32), _ptr(y, torch.bfloat16),
                                       _ptr(y_f32, torch.float32)), "moe_combine")
+
+
+# ---- the training side: sizes are taken from the tensors, and every tensor's type and shape is checked ---------------------------------
+_TYPES = {torch.bfloat16: 0, torch.float32: 1}
+
+
+def _type(t: torch.Tensor) -> int:
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        raise MoEError(f"expected bfloat16 or float32, got {t.dtype}")
+    return code
+
+
+def _of(t: Optional[torch.Tensor], dtype, *shape) -> Optional[int]:
+    """Address of a contiguous tensor of this type and shape; None for None."""
+    if t is None:
+        return None
+    if t.shape != shape:
+        raise MoEError(f"expected shape {shape}, got {tuple(t.shape)}")
+    return _ptr(t, dtype)
+
+
+def _rows_of(t: Optional[torch.Tensor], dtype, rows: int, cols: int):
+    """(address, row stride) of a 2-D tensor whose rows are contiguous."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or t.dtype != dtype or t.shape != (rows, cols) or (cols > 1 and t.stride(1) != 1):
+        raise MoEError(f"expected a CUDA tensor ({rows}, {cols}) of {dtype} with contiguous rows, got {tuple(t.shape)} of {t.dtype}")
+    return t.data_ptr(), t.stride(0) if rows > 1 else max(cols, 1)
+
+
+def moe_reserve_gradients(ctx) -> None:
+    """Allocates what the gradient calls need beside their arguments (64 MiB, once per context)."""
+    _check(load_library().moe_reserve_gradients(ctx), "moe_reserve_gradients")
+
+
+def moe_add_rmsnorm(ctx, x, residual, gain, eps, sum=None, y=None, q=None, scales=None, rstd=None) -> None:
+    """x, residual [rows, cols] (bf16 or f32, rows may be strided); every output given is written."""
+    if x.dim() != 2:
+        raise MoEError("expected a 2-D tensor")
+    rows, cols = x.shape
+    code, t, f = _type(x), x.dtype, torch.float32
+    px, ld_x = _rows_of(x, t, rows, cols)
+    pr, ld_r = _rows_of(residual, t, rows, cols)
+    _check(load_library().moe_add_rmsnorm(ctx, px, pr, _of(gain, f, cols), rows, cols, ld_x, ld_r, code, eps, _of(sum, t, rows, cols),
+                                          _of(y, t, rows, cols), _of(q, torch.uint8, rows, cols), _of(scales, f, cols // 128, rows),
+                                          _of(rstd, f, rows)), "moe_add_rmsnorm")
+
+
+def moe_add_rmsnorm_backward(ctx, dy, h, rstd, gain, dh, dx, dgain) -> None:
+    if dy.dim() != 2:
+        raise MoEError("expected a 2-D tensor")
+    rows, cols = dy.shape
+    t, f = dy.dtype, torch.float32
+    _check(load_library().moe_add_rmsnorm_backward(ctx, _ptr(dy), _of(h, t, rows, cols), _of(rstd, f, rows), _of(gain, f, cols),
+                                                   _of(dh, t, rows, cols), rows, cols, _type(dy), _of(dx, t, rows, cols),
+                                                   _of(dgain, f, cols)), "moe_add_rmsnorm_backward")
+
+
+def _shape_of(ctx):
+    if ctx not in _shapes:
+        raise MoEError("not a context")
+    return _shapes[ctx]
+
+
+def moe_dispatch(ctx, x, inv_perm, x_perm) -> None:
+    T, d, _, k = _shape_of(ctx)
+    t = x.dtype
+    _check(load_library().moe_dispatch(ctx, _of(x, t, T, d), _of(inv_perm.view(-1), torch.int32, T * k), _type(x), _of(x_perm, t, T * k, d)),
+           "moe_dispatch")
+
+
+def moe_dispatch_backward(ctx, dx_perm, inv_perm, dx_add, dx) -> None:
+    T, d, _, k = _shape_of(ctx)
+    t = dx_perm.dtype
+    _check(load_library().moe_dispatch_backward(ctx, _of(dx_perm, t, T * k, d), _of(inv_perm.view(-1), torch.int32, T * k),
+                                                _of(dx_add, t, T, d), _type(dx_perm), _of(dx, t, T, d)), "moe_dispatch_backward")
+
+
+def moe_combine_backward(ctx, dy, y_perm, inv_perm, topk_w, topk_idx, dy_perm, dw, dlogits) -> None:
+    """topk_idx and dlogits: both given or both None."""
+    T, d, E, k = _shape_of(ctx)
+    t, f = dy.dtype, torch.float32
+    _check(load_library().moe_combine_backward(ctx, _of(dy, t, T, d), _of(y_perm, f, T * k, d), _of(inv_perm.view(-1), torch.int32, T * k),
+                                               _of(topk_w, f, T, k), _of(topk_idx, torch.int32, T, k), _type(dy), _of(dy_perm, t, T * k, d),
+                                               _of(dw, f, T, k), _of(dlogits, f, T, E)), "moe_combine_backward")
+
+
+def moe_policy_loss(ctx, logits, target, old_logp, ref_logp, advantage, weight, logp, entropy, row_loss, loss, dlogits=None, *,
+                    clip_rows=None, clip_low=0.2, clip_high=0.2, kl_coef=0.0, entropy_coef=0.0, temperature=1.0) -> None:
+    """logits [rows, V] (bf16 or f32, rows may be strided); dlogits None: forward only; it may be logits itself."""
+    if logits.dim() != 2:
+        raise MoEError("expected a 2-D tensor")
+    rows, V = logits.shape
+    f, code = torch.float32, _type(logits)
+    pz, ld = _rows_of(logits, logits.dtype, rows, V)
+    gcode = code if dlogits is None else _type(dlogits)
+    pg, ld_g = _rows_of(dlogits, dlogits.dtype if dlogits is not None else None, rows, V)
+    _check(load_library().moe_policy_loss(ctx, pz, ld, code, rows, V, _of(target, torch.int32, rows), _of(old_logp, f, rows),
+                                          _of(ref_logp, f, rows), _of(advantage, f, rows), _of(weight, f, rows), _of(clip_rows, f, rows),
+                                          clip_low, clip_high, kl_coef, entropy_coef, temperature, _of(logp, f, rows), _of(entropy, f, rows),
+                                          _of(row_loss, f, rows), _of(loss, f, 1), pg, ld_g, gcode), "moe_policy_loss")
+
+
+def _experts(offsets, matrices: torch.Tensor):
+    """(E, shape prefix) of a linear's matrices: dense without offsets, one per expert with them."""
+    if offsets is None:
+        if matrices.dim() != 2:
+            raise MoEError("a dense linear has one matrix")
+        return 1, ()
+    if matrices.dim() != 3:
+        raise MoEError("a grouped linear has a matrix per expert")
+    return matrices.shape[0], (matrices.shape[0],)
+
+
+def moe_linear_fp8_dgrad(ctx, dy, Wq, ws, offsets, dx) -> None:
+    """dy [rows, NOUT] bf16; Wq [NOUT, K] (offsets None) or [E, NOUT, K]; dx [rows, K] bf16."""
+    E, pre = _experts(offsets, Wq)
+    NOUT, K = Wq.shape[-2:]
+    rows, b = dy.shape[0], torch.bfloat16
+    _check(load_library().moe_linear_fp8_dgrad(ctx, _of(dy, b, rows, NOUT), rows, NOUT, _ptr(Wq, torch.uint8),
+                                               _of(ws, torch.float32, *pre, NOUT // 128, K // 128), K, _of(offsets, torch.int32, E + 1), E,
+                                               _of(dx, b, rows, K)), "moe_linear_fp8_dgrad")
+
+
+def moe_linear_fp8_wgrad(ctx, dy, xq, xs, offsets, dW, accumulate=False) -> None:
+    """dy [rows, NOUT] bf16; xq [rows, K] u8 and xs [K/128, rows] as the forward pass read them; dW [NOUT, K] or [E, NOUT, K], bf16 or f32."""
+    E, _ = _experts(offsets, dW)
+    NOUT, K = dW.shape[-2:]
+    rows = dy.shape[0]
+    _check(load_library().moe_linear_fp8_wgrad(ctx, _of(dy, torch.bfloat16, rows, NOUT), rows, NOUT, _of(xq, torch.uint8, rows, K),
+                                               _of(xs, torch.float32, K // 128, rows), K, _of(offsets, torch.int32, E + 1), E,
+                                               1 if accumulate else 0, _type(dW), _ptr(dW)), "moe_linear_fp8_wgrad")
 
 
 def moe_balance_lengths(pred_len, n_groups: int, equal_count: bool = True):

@@ -1,6 +1,7 @@
 // C-ABI entry points of libmoe355: argument validation, context and workspace.
 #include "moe_internal.hpp"
 
+#include <cmath>
 #include <new>
 
 using namespace moe355;
@@ -53,6 +54,19 @@ int route_replay(moe_ctx* c, const uint16_t* x, const int32_t* logged_idx, const
     float* w_copy = (topk_w == logged_w) ? nullptr : topk_w;
     return hip_rc(launch_permute(permute_args_of(c, true), logged_idx, idx_copy, logged_w, w_copy, offsets, perm, inv_perm,
                                  tokens_of(c, x, xq, xs)));
+}
+
+inline bool dtype_ok(int32_t t) { return t == MOE_BF16 || t == MOE_F32; }
+inline bool aligned(const void* p, int bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+inline int type_bytes(int32_t t) { return t == MOE_BF16 ? 2 : 4; }
+
+// the products of the FP8 linear's gradients: shapes, and addresses that are read and written 16 bytes at a time
+bool linear_grad_ok(const moe_ctx* c, int64_t rows, int32_t NOUT, int32_t K, const int32_t* offsets, int32_t E) {
+    if (!c || !c->grad_ws) return false;
+    if (rows < 0 || rows >= ((int64_t)1 << 31) - 256 || NOUT <= 0 || K <= 0 || NOUT % QBLOCK || K % QBLOCK) return false;
+    if ((int64_t)NOUT * K >= (int64_t)1 << 32 || E < 1 || E > MAX_E || (!offsets && E != 1)) return false;
+    // blocks of a launch
+    return (rows / 256 + E) * (((int64_t)K + 255) / 256) < (int64_t)1 << 31;
 }
 
 }  // namespace
@@ -125,6 +139,7 @@ int moe_destroy(moe_ctx* c) {
     if (c->route_partial) (void)hipFree(c->route_partial);
     if (c->hq) (void)hipFree(c->hq);
     if (c->hs) (void)hipFree(c->hs);
+    if (c->grad_ws) (void)hipFree(c->grad_ws);
     if (c->prof_events) {
         for (int i = 0; i < 3 * PROF_MAX_CALLS; ++i) (void)hipEventDestroy(c->prof_events[i]);
         delete[] c->prof_events;
@@ -239,6 +254,110 @@ int moe_combine(moe_ctx* c, const float* y_perm, const int32_t* inv_perm, const 
     if (c->dims.T == 0) return MOE_OK;
     if (!y_perm || !inv_perm || !topk_w || !y) return MOE_EINVAL;
     return hip_rc(launch_combine(c, y_perm, inv_perm, topk_w, y, y_f32));
+}
+
+int moe_reserve_gradients(moe_ctx* c) {
+    if (!c) return MOE_EINVAL;
+    if (c->grad_ws) return MOE_OK;
+    void* p = nullptr;
+    if (hipMalloc(&p, GRAD_WS_BYTES + 256) != hipSuccess) {
+        (void)hipGetLastError();
+        return MOE_ENOMEM;
+    }
+    int32_t* const ticket = reinterpret_cast<int32_t*>(static_cast<char*>(p) + GRAD_WS_BYTES);
+    if (launch_fill_i32(c->stream, ticket, 64, 0) != hipSuccess || set_grad_lds_limits() != hipSuccess) {
+        (void)hipGetLastError();
+        (void)hipStreamSynchronize(c->stream);
+        (void)hipFree(p);
+        return MOE_EHIP;
+    }
+    c->grad_ws = p;
+    c->grad_ticket = ticket;
+    return MOE_OK;
+}
+
+int moe_add_rmsnorm(moe_ctx* c, const void* x, const void* residual, const float* gain, int64_t rows, int32_t cols, int64_t ld_x,
+                    int64_t ld_res, int32_t dtype, float eps, void* sum, void* y, uint8_t* q, float* scales, float* rstd) {
+    if (!c || !dtype_ok(dtype) || rows < 0 || cols < 1 || cols > NORM_MAX_COLS || !(eps >= 0.f) || !std::isfinite(eps)) return MOE_EINVAL;
+    if (rows > (int64_t)1 << 40 || ld_x < cols || ld_x > (int64_t)1 << 20 || (residual && (ld_res < cols || ld_res > (int64_t)1 << 20)))
+        return MOE_EINVAL;
+    if (!q != !scales) return MOE_EINVAL;
+    if (rows == 0) return MOE_OK;
+    if (!x || !gain || (!sum && !y && !q && !rstd)) return MOE_EINVAL;
+    const int bytes = type_bytes(dtype);
+    if (!aligned(x, bytes) || !aligned(residual, bytes) || !aligned(sum, bytes) || !aligned(y, bytes) || !aligned(gain, 4)) return MOE_EINVAL;
+    if ((sum == x && ld_x != cols) || (sum && sum == residual && ld_res != cols)) return MOE_EINVAL;
+    if (q) {                                   // codes are made from rows of whole vectors
+        if (cols % QBLOCK || !norm_codes_fit(cols) || ld_x % 8 || (residual && ld_res % 8)) return MOE_EINVAL;
+        if (!aligned(x, 16) || !aligned(residual, 16) || !aligned(gain, 16) || !aligned(sum, 16) || !aligned(y, 16) || !aligned(q, 8))
+            return MOE_EINVAL;
+    }
+    return hip_rc(launch_norm(c->stream, x, residual, gain, rows, cols, ld_x, ld_res, dtype, eps, sum, y, q, scales, rstd));
+}
+
+int moe_add_rmsnorm_backward(moe_ctx* c, const void* dy, const void* h, const float* rstd, const float* gain, const void* dh, int64_t rows,
+                             int32_t cols, int32_t dtype, void* dx, float* dgain) {
+    if (!c || !c->grad_ws || !dtype_ok(dtype) || rows < 0 || rows > (int64_t)1 << 40 || cols < 1 || cols > NORM_MAX_COLS || !dgain)
+        return MOE_EINVAL;
+    if (rows > 0 && (!dy || !h || !rstd || !gain || !dx)) return MOE_EINVAL;
+    const int bytes = type_bytes(dtype);
+    if (!aligned(dy, bytes) || !aligned(h, bytes) || !aligned(dh, bytes) || !aligned(dx, bytes)) return MOE_EINVAL;
+    return hip_rc(launch_norm_backward(c, dy, h, rstd, gain, dh, rows, cols, dtype, dx, dgain));
+}
+
+int moe_dispatch(moe_ctx* c, const void* x, const int32_t* inv_perm, int32_t dtype, void* x_perm) {
+    if (!c || !dtype_ok(dtype)) return MOE_EINVAL;
+    if (c->dims.T == 0) return MOE_OK;
+    if (!x || !inv_perm || !x_perm || !aligned(x, 16) || !aligned(x_perm, 16)) return MOE_EINVAL;
+    return hip_rc(launch_dispatch(c, x, inv_perm, dtype, x_perm));
+}
+
+int moe_dispatch_backward(moe_ctx* c, const void* dx_perm, const int32_t* inv_perm, const void* dx_add, int32_t dtype, void* dx) {
+    if (!c || !dtype_ok(dtype)) return MOE_EINVAL;
+    if (c->dims.T == 0) return MOE_OK;
+    if (!dx_perm || !inv_perm || !dx || !aligned(dx_perm, 16) || !aligned(dx_add, 16) || !aligned(dx, 16)) return MOE_EINVAL;
+    return hip_rc(launch_dispatch_backward(c, dx_perm, inv_perm, dx_add, dtype, dx));
+}
+
+int moe_combine_backward(moe_ctx* c, const void* dy, const float* y_perm, const int32_t* inv_perm, const float* topk_w, const int32_t* topk_idx,
+                         int32_t dtype, void* dy_perm, float* dw, float* dlogits) {
+    if (!c || !dtype_ok(dtype)) return MOE_EINVAL;
+    if (c->dims.T == 0) return MOE_OK;
+    if (!dy || !y_perm || !inv_perm || !topk_w || !dy_perm || !dw || !topk_idx != !dlogits) return MOE_EINVAL;
+    if (!aligned(dy, 16) || !aligned(y_perm, 16) || !aligned(dy_perm, 16)) return MOE_EINVAL;
+    return hip_rc(launch_combine_backward(c, dy, y_perm, inv_perm, topk_w, topk_idx, dtype, dy_perm, dw, dlogits));
+}
+
+int moe_policy_loss(moe_ctx* c, const void* logits, int64_t ld, int32_t dtype, int64_t rows, int32_t V, const int32_t* target,
+                    const float* old_logp, const float* ref_logp, const float* advantage, const float* weight, const float* clip_rows,
+                    float clip_low, float clip_high, float kl_coef, float entropy_coef, float temperature, float* logp, float* entropy,
+                    float* row_loss, float* loss, void* dlogits, int64_t ld_grad, int32_t grad_dtype) {
+    if (!c || !c->grad_ws || !dtype_ok(dtype) || (dlogits && !dtype_ok(grad_dtype)) || !loss) return MOE_EINVAL;
+    if (rows < 0 || rows > (int64_t)1 << 30 || V < 1 || ld < V || (dlogits && ld_grad < V)) return MOE_EINVAL;
+    for (const float v : {clip_low, clip_high, kl_coef, entropy_coef})
+        if (!std::isfinite(v) || v < 0.f) return MOE_EINVAL;
+    if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.0f / temperature)) return MOE_EINVAL;
+    if (rows > 0 && (!logits || !target || !old_logp || !advantage || !weight || !logp || !entropy || !row_loss)) return MOE_EINVAL;
+    if (!aligned(logits, type_bytes(dtype)) || (dlogits && !aligned(dlogits, type_bytes(grad_dtype)))) return MOE_EINVAL;
+    if (dlogits && dlogits == logits && (grad_dtype != dtype || ld_grad != ld)) return MOE_EINVAL;
+    return hip_rc(launch_policy_loss(c, logits, ld, dtype, rows, V, target, old_logp, ref_logp, advantage, weight, clip_rows, clip_low,
+                                     clip_high, kl_coef, entropy_coef, temperature, logp, entropy, row_loss, loss, dlogits, ld_grad,
+                                     dlogits ? grad_dtype : dtype));
+}
+
+int moe_linear_fp8_dgrad(moe_ctx* c, const uint16_t* dy, int64_t rows, int32_t NOUT, const uint8_t* Wq, const float* ws, int32_t K,
+                         const int32_t* offsets, int32_t E, uint16_t* dx) {
+    if (!linear_grad_ok(c, rows, NOUT, K, offsets, E)) return MOE_EINVAL;
+    if (rows == 0) return MOE_OK;
+    if (!dy || !Wq || !ws || !dx || !aligned(dy, 16) || !aligned(Wq, 16) || !aligned(ws, 4) || !aligned(dx, 16)) return MOE_EINVAL;
+    return hip_rc(launch_linear_dgrad(c, dy, rows, NOUT, Wq, ws, K, offsets, E, dx));
+}
+
+int moe_linear_fp8_wgrad(moe_ctx* c, const uint16_t* dy, int64_t rows, int32_t NOUT, const uint8_t* xq, const float* xs, int32_t K,
+                         const int32_t* offsets, int32_t E, int32_t accumulate, int32_t dtype, void* dW) {
+    if (!linear_grad_ok(c, rows, NOUT, K, offsets, E) || !dtype_ok(dtype) || !dW || !aligned(dW, 16)) return MOE_EINVAL;
+    if (rows > 0 && (!dy || !xq || !xs || !aligned(dy, 16) || !aligned(xq, 16) || !aligned(xs, 4))) return MOE_EINVAL;
+    return hip_rc(launch_linear_wgrad(c, dy, rows, NOUT, xq, xs, K, offsets, E, accumulate != 0, dtype, dW));
 }
 
 int moe_profile_enable(moe_ctx* c, int32_t on) {

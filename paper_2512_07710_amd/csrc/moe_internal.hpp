@@ -15,7 +15,8 @@ constexpr int MAX_E = 256;
 constexpr int MAX_K = 16;
 constexpr int PROF_MAX_CALLS = 512;
 constexpr int ROUTE_TICKET = 32, FLAG_INTS = 33;   // (the ticket has a cache line of its own)
-
+constexpr size_t GRAD_WS_BYTES = (size_t)64 << 20;
+constexpr int NORM_MAX_COLS = 65536;
 
 }  // namespace moe355
 
@@ -36,6 +37,8 @@ struct moe_ctx {
     float* route_partial;    // [splits][T padded to 32][E padded] partial logits of the split router (small batches only)
     uint8_t* hq;             // [N][F]
     float* hs;               // [N][F/128]
+    void* grad_ws;           // workspace of the gradients (GRAD_WS_BYTES), null until it is reserved
+    int32_t* grad_ticket;    // behind it: zero between launches
     // optional kernel timing: three events per recorded expert-FFN call
     bool profiling;
     int prof_calls;
@@ -114,6 +117,25 @@ hipError_t set_flow_lds_limits();
 hipError_t launch_flow_gate_up(moe_ctx* c, const uint8_t* xq, const float* xs, const int32_t* perm, const int32_t* offsets,
                                const uint8_t* W1, const uint8_t* W3, const float* s1, const float* s3);
 hipError_t launch_flow_down(moe_ctx* c, const int32_t* offsets, const uint8_t* W2, const float* s2, float* y_perm);
+// The training side (norm.hip, tokens_grad.hip, policy_loss.hip, linear_grad.hip)
+bool norm_codes_fit(int32_t cols);
+hipError_t launch_norm(hipStream_t s, const void* x, const void* residual, const float* gain, int64_t rows, int32_t cols, int64_t ld_x,
+                       int64_t ld_res, int32_t dtype, float eps, void* sum, void* y, uint8_t* q, float* scales, float* rstd);
+hipError_t launch_norm_backward(moe_ctx* c, const void* dy, const void* h, const float* rstd, const float* gain, const void* dh, int64_t rows,
+                                int32_t cols, int32_t dtype, void* dx, float* dgain);
+hipError_t launch_dispatch(moe_ctx* c, const void* x, const int32_t* inv_perm, int32_t dtype, void* x_perm);
+hipError_t launch_dispatch_backward(moe_ctx* c, const void* dx_perm, const int32_t* inv_perm, const void* dx_add, int32_t dtype, void* dx);
+hipError_t launch_combine_backward(moe_ctx* c, const void* dy, const float* y_perm, const int32_t* inv_perm, const float* topk_w,
+                                   const int32_t* topk_idx, int32_t dtype, void* dy_perm, float* dw, float* dlogits);
+hipError_t launch_policy_loss(moe_ctx* c, const void* logits, int64_t ld, int32_t dtype, int64_t rows, int32_t V, const int32_t* target,
+                              const float* old_logp, const float* ref_logp, const float* advantage, const float* weight,
+                              const float* clip_rows, float clip_low, float clip_high, float kl_coef, float entropy_coef, float temperature,
+                              float* logp, float* entropy, float* row_loss, float* loss, void* dlogits, int64_t ld_grad, int32_t grad_dtype);
+hipError_t set_grad_lds_limits();
+hipError_t launch_linear_dgrad(moe_ctx* c, const uint16_t* dy, int64_t rows, int32_t NOUT, const uint8_t* Wq, const float* ws, int32_t K,
+                               const int32_t* offsets, int32_t E, uint16_t* dx);
+hipError_t launch_linear_wgrad(moe_ctx* c, const uint16_t* dy, int64_t rows, int32_t NOUT, const uint8_t* xq, const float* xs, int32_t K,
+                               const int32_t* offsets, int32_t E, int32_t accumulate, int32_t dtype, void* dW);
 size_t route_workspace_bytes(int E, int d);
 size_t route_partial_bytes(int T, int E);
 hipError_t launch_combine(moe_ctx* c, const float* y_perm, const int32_t* inv_perm,
