@@ -336,7 +336,7 @@ int moe_policy_loss(moe_ctx* c, const void* logits, int64_t ld, int32_t dtype, i
     if (rows < 0 || rows > (int64_t)1 << 30 || V < 1 || ld < V || (dlogits && ld_grad < V)) return MOE_EINVAL;
     for (const float v : {clip_low, clip_high, kl_coef, entropy_coef})
         if (!std::isfinite(v) || v < 0.f) return MOE_EINVAL;
-    if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.0f / temperature)) return MOE_EINVAL;
+    if (!(temperature >= 1e-6f && temperature <= 1e6f)) return MOE_EINVAL;
     if (rows > 0 && (!logits || !target || !old_logp || !advantage || !weight || !logp || !entropy || !row_loss)) return MOE_EINVAL;
     if (!aligned(logits, type_bytes(dtype)) || (dlogits && !aligned(dlogits, type_bytes(grad_dtype)))) return MOE_EINVAL;
     if (dlogits && dlogits == logits && (grad_dtype != dtype || ld_grad != ld)) return MOE_EINVAL;
