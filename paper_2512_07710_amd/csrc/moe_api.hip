@@ -260,19 +260,19 @@ int moe_reserve_gradients(moe_ctx* c) {
     if (!c) return MOE_EINVAL;
     if (c->grad_ws) return MOE_OK;
     void* p = nullptr;
-    if (hipMalloc(&p, GRAD_WS_BYTES + 256) != hipSuccess) {
+    if (hipMalloc(&p, GRAD_WS_BYTES + GRAD_TICKETS * sizeof(int32_t)) != hipSuccess) {
         (void)hipGetLastError();
         return MOE_ENOMEM;
     }
     int32_t* const ticket = reinterpret_cast<int32_t*>(static_cast<char*>(p) + GRAD_WS_BYTES);
-    if (launch_fill_i32(c->stream, ticket, 64, 0) != hipSuccess || set_grad_lds_limits() != hipSuccess) {
+    if (launch_fill_i32(c->stream, ticket, GRAD_TICKETS, 0) != hipSuccess || set_grad_lds_limits() != hipSuccess) {
         (void)hipGetLastError();
         (void)hipStreamSynchronize(c->stream);
         (void)hipFree(p);
         return MOE_EHIP;
     }
     c->grad_ws = p;
-    c->grad_ticket = ticket;
+    c->grad_tickets = ticket;
     return MOE_OK;
 }
 

@@ -16,6 +16,9 @@ constexpr int MAX_K = 16;
 constexpr int PROF_MAX_CALLS = 512;
 constexpr int ROUTE_TICKET = 32, FLAG_INTS = 33;   // (the ticket has a cache line of its own)
 constexpr size_t GRAD_WS_BYTES = (size_t)64 << 20;
+// Tickets behind it, each in a cache line of its own: the launch's, those of groups of rows, those of rows that are worked on in parts
+constexpr int GRAD_TICKET_INTS = 32, GRAD_GROUPS = 64, GRAD_MAX_SPLIT_ROWS = 512;
+constexpr int GRAD_TICKETS = (1 + GRAD_GROUPS + GRAD_MAX_SPLIT_ROWS) * GRAD_TICKET_INTS;
 constexpr int NORM_MAX_COLS = 65536;
 
 }  // namespace moe355
@@ -38,7 +41,7 @@ struct moe_ctx {
     uint8_t* hq;             // [N][F]
     float* hs;               // [N][F/128]
     void* grad_ws;           // workspace of the gradients (GRAD_WS_BYTES), null until it is reserved
-    int32_t* grad_ticket;    // behind it: zero between launches
+    int32_t* grad_tickets;    // behind it [GRAD_TICKETS], zero between launches
     // optional kernel timing: three events per recorded expert-FFN call
     bool profiling;
     int prof_calls;
