@@ -66,7 +66,7 @@ bool linear_grad_ok(const moe_ctx* c, int64_t rows, int32_t NOUT, int32_t K, con
     if (rows < 0 || rows >= ((int64_t)1 << 31) - 256 || NOUT <= 0 || K <= 0 || NOUT % QBLOCK || K % QBLOCK) return false;
     if ((int64_t)NOUT * K >= (int64_t)1 << 32 || E < 1 || E > MAX_E || (!offsets && E != 1)) return false;
     // blocks of a launch
-    return (rows / 256 + E) * (((int64_t)K + 255) / 256) < (int64_t)1 << 31;
+    return (rows / 128 + E) * (((int64_t)K + 255) / 256) < (int64_t)1 << 31 && (int64_t)E * (NOUT / 128) * (((int64_t)K + 255) / 256) < (int64_t)1 << 31;
 }
 
 }  // namespace
