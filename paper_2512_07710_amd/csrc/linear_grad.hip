@@ -61,11 +61,13 @@ __device__ inline v8bf codes_bf16(v2i c, float pow2) {
     return v8bf{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
 }
 
-// what a wave reads from LDS for 16 steps of the sum
+// what a wave reads from LDS for 16 steps of the sum, and its codes as operands
+template <int PLANES>
 struct operands {
     v8s d[4];                                  // dy: 4 x 32 rows of the tile
     v2i q[2];                                  // codes: 2 x 32 columns
     v4f s[2];                                  // (wgrad) the scales of a lane's eight steps
+    v8bf c[2][PLANES];
 };
 
 // W: the weights' gradient; PLANES: bf16 planes of its scaled operand; F32: type of the result
@@ -187,7 +189,7 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
         code_at[j] = lds0 + DY_STAGE + ((lane >> 5) * 8 + (lane >> 1 & 7)) * 256 + chunk * 16 + (lane & 1) * 8;
     }
     const uint32_t scale_at = lds0 + DY_STAGE + CODE_STAGE + (wave >> 1) * 256 + (lane >> 5) * 32;
-    auto fetch = [&](operands& o, uint32_t at, auto kk_) {     // at: the stage's offset
+    auto fetch = [&](operands<PLANES>& o, uint32_t at, auto kk_) {     // at: the stage's offset
         constexpr int kk = decltype(kk_)::value;
 #pragma unroll
         for (int j = 0; j < 2; ++j) o.q[j] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i_ptr)(uintptr_t)(code_at[j] + at + kk * 4096));
@@ -232,12 +234,11 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
         unit = to;
         return ratio;
     };
-    auto multiply = [&](operands& o, bool rescale, float ratio) {
-        v8bf c[2][PLANES];
+    auto convert = [&](operands<PLANES>& o) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             if (!W) {
-                c[j][0] = codes_bf16(o.q[j] & block_mask, pow2);
+                o.c[j][0] = codes_bf16(o.q[j] & block_mask, pow2);
                 continue;
             }
 #pragma unroll
@@ -248,31 +249,62 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
                     float y = x[v] * o.s[h >> 1][(h & 1) * 2 + v];
 #pragma unroll
                     for (int p = 0; p < PLANES; ++p) {
-                        c[j][p][h * 2 + v] = (__bf16)y;
+                        o.c[j][p][h * 2 + v] = (__bf16)y;
                         if (p + 1 < PLANES) {
-                            y -= (float)c[j][p][h * 2 + v];
+                            y -= (float)o.c[j][p][h * 2 + v];
                             if (y != y) y = 0.f;               // (the first plane has the infinity)
                         }
                     }
                 }
             }
         }
+    };
+    auto product = [&](const operands<PLANES>& o, int i, int p) {
 #pragma unroll
-        for (int p = 0; p < PLANES; ++p) {
-            if (p == 1) {                      // an infinite gradient counts in the first plane, the others have both signs and zeros
+        for (int j = 0; j < 2; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(o.c[j][p], __builtin_bit_cast(v8bf, o.d[i]), acc[i][j], 0, 0, 0);
+    };
+    // The products of `o`, while the operands of the next group (if there is one) come from LDS behind the first of them and are converted
+    // behind the others: in this order, which the compiler would not keep by itself
+    auto group = [&](operands<PLANES>& o, operands<PLANES>* next, auto rescale_, float ratio) {
+        constexpr bool rescale = decltype(rescale_)::value;
+        if (rescale) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i) {
+                acc[i][0] *= ratio;
+                acc[i][1] *= ratio;
+                product(o, i, 0);
+            }
+        } else {
 #pragma unroll
-                    for (int v = 0; v < 8; ++v) o.d[i][v] = (o.d[i][v] & 0x7F80) == 0x7F80 ? (short)0 : o.d[i][v];
+            for (int i = 0; i < 4; ++i) product(o, i, 0);
+        }
+        if (PLANES > 1) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {      // an infinite gradient counts in the first plane, the others have both signs and zeros
+#pragma unroll
+                for (int v = 0; v < 8; ++v) o.d[i][v] = (o.d[i][v] & 0x7F80) == 0x7F80 ? (short)0 : o.d[i][v];
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int p = 1; p < PLANES; ++p)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    if (rescale) acc[i][j] *= ratio;
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c[j][p], __builtin_bit_cast(v8bf, o.d[i]), acc[i][j], 0, 0, 0);
-                }
+                for (int i = 0; i < 4; ++i) product(o, i, p);
         }
+        if (next) convert(*next);
+        if (PLANES == 1) {
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                __builtin_amdgcn_sched_group_barrier(0x100, W ? 3 : 2, 0);     // LDS reads
+                if (rescale) __builtin_amdgcn_sched_group_barrier(0x2, 16, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);               // a product
+            }
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                __builtin_amdgcn_sched_group_barrier(0x2, rescale ? 18 : W ? 8 : 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
     };
 
     // ---- the sum.  Operands are fetched one group of products ahead; the barrier that hands over the stages stands before a stage's last group,
@@ -286,33 +318,36 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
             asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
         }
         if (W) clear_behind(0);
-        operands f, g;
+        operands<PLANES> f, g;
         fetch(f, 0, step<0>{});
-        auto stage = [&](int kb, auto rescale_) {
-            constexpr bool rescale = decltype(rescale_)::value;
+        auto stage = [&](int kb, auto first_) {
+            constexpr bool first = decltype(first_)::value;    // (dgrad) of a block of scales
             const uint32_t at = (uint32_t)(kb & 1) * G_STAGE;
-            const float ratio = rescale ? next_block(kb) : 1.f;
+            const float ratio = first ? next_block(kb) : 1.f;
+            if (!W && first) convert(f);
             fetch(g, at, step<1>{});
-            multiply(f, rescale, ratio);
+            group(f, &g, first_, ratio);
             fetch(f, at, step<2>{});
-            multiply(g, false, 1.f);
+            group(g, &f, std::false_type{}, 1.f);
             fetch(g, at, step<3>{});
-            multiply(f, false, 1.f);
+            group(f, &g, std::false_type{}, 1.f);
             if (kb + 1 < nk) {
                 asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // stage kb+1 is there, and this one has been read
                 if (kb + 2 < nk) copy(kb + 2);
                 if (W) clear_behind(kb + 1);
-                fetch(f, G_STAGE - at, step<0>{});
             }
-            multiply(g, false, 1.f);
+            fetch(f, G_STAGE - at, step<0>{});                 // (behind the last stage: of no use, and not used)
+            group(g, W || first ? &f : nullptr, std::false_type{}, 1.f);
         };
-        if (W)
+        if (W) {
+            convert(f);
             for (int kb = 0; kb < nk; ++kb) stage(kb, std::false_type{});
-        else
+        } else {
             for (int kb = 0; kb < nk; kb += 2) {               // two stages to a block of scales
                 stage(kb, std::true_type{});
                 stage(kb + 1, std::false_type{});
             }
+        }
     }
 
     // ---- a lane holds one row of the result, four neighbouring columns at a time
