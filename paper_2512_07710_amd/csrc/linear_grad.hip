@@ -42,7 +42,7 @@ struct grad_args {
     int E, NOUT, K;
     int accumulate;
     void* out;
-    float* parts;                              // [units][4][8][256] f32x4: a thread's sums, in its own order
+    float* parts;                              // [units][rows / 32][2][4][256] f32x4: a thread's sums, in its own order
 };
 
 // expert e's rows
@@ -171,17 +171,16 @@ __device__ inline bool unit_of(const grad_args& a, int b, find_scratch& s, unit&
     return true;
 }
 
-// A wave's 32 x 64 values of the result, a lane's four neighbouring columns of row lane%32 at a time, go through LDS to be stored as whole
+// A wave's 32 x 64 values of the result, four neighbouring columns of row lane%16 of a lane's at a time, go through LDS to be stored as whole
 // lines.  buffer: the wave's own place.
 constexpr int OUT_LD = 68;                     // floats of a row there
 template <bool F32>
 __device__ inline void store_rows(const grad_args& a, float* buffer, const f32x4 (&r)[2][4], size_t at, int rows) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-            *reinterpret_cast<f32x4*>(buffer + (lane & 31) * OUT_LD + j * 32 + g * 8 + (lane >> 5) * 4) = r[j][g];
+        for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4*>(buffer + (h * 16 + (lane & 15)) * OUT_LD + j * 16 + (lane >> 4) * 4) = r[h][j];
     __builtin_amdgcn_wave_barrier();
     constexpr int PER_ROW = F32 ? 16 : 8, STEP = 64 / PER_ROW, N = 64 / PER_ROW;               // lanes of a row, rows at a time, a lane's columns
 #pragma unroll
@@ -220,19 +219,10 @@ __device__ inline v8bf codes_bf16(v2i c, float pow2) {
     return v8bf{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
 }
 
-// what a wave reads from LDS for 16 steps of the sum, and its codes as operands
-template <int PLANES>
-struct operands {
-    v8s d[4];                                  // dy: 4 x 32 rows of the tile
-    v2i q[2];                                  // codes: 2 x 32 columns
-    v4f s[2];                                  // (wgrad) the scales of a lane's eight steps
-    v8bf c[2][PLANES];
-};
-
 // W: the weights' gradient; PLANES: bf16 planes of its scaled operand; F32: type of the result
 template <bool W, int PLANES, bool F32>
 __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
-    extern __shared__ __attribute__((aligned(16))) char lds[];
+    extern __shared__ __attribute__((aligned(1024))) char lds[];   // (the places of chunks are exchanged inside 256 bytes)
     __shared__ find_scratch s_find;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     unit u;
@@ -247,30 +237,38 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
     const uint16_t* const dy = W ? a.dy + (size_t)lo * a.NOUT + row0 : a.dy + (size_t)row0 * a.NOUT;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
 
-    // ---- copies of stage kb into its half of the ring; rows behind the segment repeat its last
-    const int r4 = lane >> 4, r8 = lane >> 3;
-    const uint32_t code_chunk = ((lane & 15) ^ ((r4 & 3) << 1)) & cmask, code_chunk4 = ((lane & 15) ^ ((r4 + 4) << 1)) & cmask;
+    // ---- copies of stage kb into its half of the ring; rows behind the segment repeat its last.  16-byte chunks of a row change places by
+    // the row's number, so that each transposing or plain read of a wave meets every LDS bank once
+    const int r4 = lane >> 4, r8 = lane >> 3, c16 = lane & 15;
+    const uint32_t dy_pitch = (uint32_t)a.NOUT * 2, code_pitch = (uint32_t)a.K;
+    // offsets of a lane from the first row that its wave's copy brings
+    const uint32_t code_row = (uint32_t)r4 * code_pitch, code_chunk = (uint32_t)((c16 ^ r4) & 15) * 16, code_mask = (uint32_t)cmask * 16;
+    uint32_t dy_off[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (W) dy_off[i] = (uint32_t)r4 * dy_pitch + (c16 ^ ((r4 | (i >> 1) << 2) << 1)) * 16;           // (rows 4 i on; only two of them differ)
+        else dy_off[i] = (uint32_t)min(wave * 32 + i * 8 + r8, hi - 1 - row0) * dy_pitch + ((lane & 7) ^ ((i & 1) * 4 + (r8 >> 1))) * 16;
     auto copy = [&](int kb) {
         const uint32_t at = lds0 + (uint32_t)((kb - k0) & 1) * G_STAGE;
         const int last = W ? hi - lo - 1 - kb * GK : GK - 1;
-        if (W) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = wave * 16 + i * 4 + r4, chunk = (lane & 15) ^ (r4 << 2);
-                dma16(at + (wave * 4 + i) * 1024, (uint32_t)min(row, last) * (uint32_t)(a.NOUT * 2) + chunk * 16, dy + (size_t)kb * GK * a.NOUT);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = wave * 32 + i * 8 + r8, chunk = (lane & 7) ^ r8 ^ (i & 1);
-                dma16(at + (wave * 4 + i) * 1024, (uint32_t)min(row, hi - 1 - row0) * (uint32_t)(a.NOUT * 2) + chunk * 16, dy + kb * GK);
-            }
-        }
+        const char* const dy_base = reinterpret_cast<const char*>(W ? dy + (size_t)kb * GK * a.NOUT : dy + kb * GK);
+        const uint8_t* const code_base = codes + (size_t)kb * GK * a.K;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int row = wave * 16 + i * 4 + r4;
-            dma16(at + DY_STAGE + (wave * 4 + i) * 1024, (uint32_t)min(row, last) * (uint32_t)a.K + (i & 1 ? code_chunk4 : code_chunk) * 16,
-                  codes + (size_t)kb * GK * a.K);
+            const uint32_t to = at + (wave * 4 + i) * 1024;
+            const int row = wave * 16 + i * 4;                 // of the sum
+            const uint32_t chunk = (code_chunk ^ i * 64) & code_mask;
+            if (!W) {
+                dma16(to, dy_off[i], dy_base);
+                dma16(to + DY_STAGE, code_row + chunk, code_base + (size_t)row * code_pitch);
+            } else if (last >= GK - 1) {
+                dma16(to, dy_off[i], dy_base + (size_t)row * dy_pitch);
+                dma16(to + DY_STAGE, code_row + chunk, code_base + (size_t)row * code_pitch);
+            } else {
+                const uint32_t r = (uint32_t)min(row + r4, last);
+                dma16(to, r * dy_pitch + (dy_off[i] - (uint32_t)r4 * dy_pitch), dy_base);
+                dma16(to + DY_STAGE, r * code_pitch + chunk, code_base);
+            }
         }
         if (W) {                               // wave w brings the scales of 128-column block w&1 of the tile (those of waves 0 and 1 are read)
             const int cb = min(c0 / QBLOCK + (wave & 1), a.K / QBLOCK - 1);
@@ -292,53 +290,49 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
         __syncthreads();
     };
 
-    // ---- this wave's part: 128 rows x 64 columns of the tile
+    // ---- this wave's part: 128 rows x 64 columns of the tile, in products of 16 x 16 over 32 steps of the sum, a stage is two groups of them.
+    // A lane has eight steps: from 8 (lane/16) on
     const int cols0 = c0 + wave * 64;
     const bool mine = cols0 < a.K;
-    uint32_t dy_at[4], code_at[2];
+    uint32_t dy_at[2], code_at;
+    if (W) {                                   // row of the sum 8 (lane/16) + (lane%16)/4, and 4 more; [0]: rows 0 to 15 of the tile
+        const int f = (lane >> 2 & 3) | (r4 & 1) << 2;
+        dy_at[0] = dy_at[1] = lds0 + (r4 * 8 + (lane >> 2 & 3)) * 256 + (((lane >> 1 & 1) ^ f << 1) << 4) + (lane & 1) * 8;
+    } else {                                   // [g]: group g
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (W) {
-            const int chunk = (i * 4 + (lane >> 4 & 1) * 2 + (lane >> 1 & 1)) ^ ((lane >> 2 & 3) << 2);
-            dy_at[i] = lds0 + ((lane >> 5) * 8 + (lane >> 2 & 3)) * 256 + chunk * 16 + (lane & 1) * 8;
-        } else {                               // i: sixteen steps of the sum
-            const int row = lane & 31;
-            dy_at[i] = lds0 + row * 128 + (((i * 2 + (lane >> 5)) ^ (row & 7) ^ (row >> 3 & 1)) << 4);
-        }
+        for (int g = 0; g < 2; ++g) dy_at[g] = lds0 + c16 * 128 + (((g * 4 + r4) ^ (c16 >> 1)) << 4);
     }
+    code_at = lds0 + DY_STAGE + (r4 * 8 + (c16 >> 1)) * 256 + (((wave * 4) ^ ((r4 & 1) * 8 + (c16 >> 1))) << 4) + (lane & 1) * 8;
+    const uint32_t scale_at = lds0 + DY_STAGE + CODE_STAGE + (wave >> 1) * 256 + r4 * 32;
+
+    v4f acc[8][4];                             // [rows / 16][columns / 16]
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int chunk = (wave * 4 + j * 2 + (lane >> 4 & 1)) ^ ((lane >> 1 & 7) << 1);
-        code_at[j] = lds0 + DY_STAGE + ((lane >> 5) * 8 + (lane >> 1 & 7)) * 256 + chunk * 16 + (lane & 1) * 8;
-    }
-    const uint32_t scale_at = lds0 + DY_STAGE + CODE_STAGE + (wave >> 1) * 256 + (lane >> 5) * 32;
-    auto fetch = [&](operands<PLANES>& o, uint32_t at, auto kk_) {     // at: the stage's offset
-        constexpr int kk = decltype(kk_)::value;
+    for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) o.q[j] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i_ptr)(uintptr_t)(code_at[j] + at + kk * 4096));
+        for (int j = 0; j < 4; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    v8s d[8];                                  // dy: of the present group, replaced by the next one's as soon as they have been used
+    v2i q[2][4];                               // codes of 4 x 16 columns, [of group 0 or 1]
+    v4f sc[2][2];                              // (wgrad) the scales of a lane's eight steps, [of group 0 or 1]
+    constexpr int NJ = PLANES == 1 ? 2 : 1, PARTS = 4 / NJ;    // a group's products in parts of 16 NJ columns
+    u32x4 c[2][NJ][PLANES];                    // codes as operands: of the present and of the next part
+    auto fetch_codes = [&](uint32_t at, int g) {               // at: the stage's offset
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[g][j] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i_ptr)(uintptr_t)((code_at ^ j * 16) + at + g * 8192));
         if (W) {
-            o.s[0] = *(lds_v4f_ptr)(uintptr_t)(scale_at + at + kk * 64);
-            o.s[1] = *(lds_v4f_ptr)(uintptr_t)(scale_at + at + kk * 64 + 16);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (W) {
-                const v4s p = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)(uintptr_t)(dy_at[i] + at + kk * 4096));
-                const v4s q = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)(uintptr_t)(dy_at[i] + at + kk * 4096 + 1024));
-                o.d[i] = __builtin_shufflevector(p, q, 0, 1, 2, 3, 4, 5, 6, 7);
-            } else {
-                o.d[i] = *(lds_v8s_ptr)(uintptr_t)(dy_at[kk] + at + i * 4096);
-            }
+            sc[g][0] = *(lds_v4f_ptr)(uintptr_t)(scale_at + at + g * 128);
+            sc[g][1] = *(lds_v4f_ptr)(uintptr_t)(scale_at + at + g * 128 + 16);
         }
     };
-
-    v16f acc[4][2];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+    auto fetch_dy = [&](uint32_t at, int g, int i) {
+        if (W) {
+            const uint32_t p = (dy_at[0] ^ i * 32) + at + g * 8192;
+            const v4s x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)(uintptr_t)p);
+            const v4s y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)(uintptr_t)(p + 1024));
+            d[i] = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+            d[i] = *(lds_v8s_ptr)(uintptr_t)(dy_at[g] + at + i * 2048);
+        }
+    };
     // (dgrad) acc is held in units of the present block's scale without its power of two, which the codes carry: a factor of less than
     // two either way from block to block, whatever the scales are.  (In the constant address space, so that they come as scalar loads:
     // a vector load's wait would include the copies)
@@ -357,81 +351,75 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
         unit_scale = to;
         return ratio;
     };
-    auto convert = [&](operands<PLANES>& o) {
+    // A quarter of the codes of 16 columns: two steps of the sum.  (The empty asm keeps the instructions where they are asked for; they would
+    // be moved down to where the operand is used)
+    auto convert = [&](u32x4 (&o)[PLANES], const v2i& codes_, const v4f (&scale)[2], int h) {
+        if (!W) {
+            const int w = codes_[h >> 1] & block_mask;
+            const v2bf x = h & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, pow2, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, pow2, false);
+            uint32_t r = __builtin_bit_cast(uint32_t, x);
+            asm volatile("" : "+v"(r));
+            o[0][h] = r;
+            return;
+        }
+        const v2f x = h & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8(codes_[h >> 1], true) : __builtin_amdgcn_cvt_pk_f32_fp8(codes_[h >> 1], false);
+        const float y[2] = {x[0] * scale[h >> 1][(h & 1) * 2], x[1] * scale[h >> 1][(h & 1) * 2 + 1]};
+        if (PLANES == 1) {
+            const v2bf z = {(__bf16)y[0], (__bf16)y[1]};
+            uint32_t r = __builtin_bit_cast(uint32_t, z);
+            asm volatile("" : "+v"(r));
+            o[0][h] = r;
+            return;
+        }
+        // 24 bits in three times eight, cut off, so that all planes have the sign of y and none is zero unless y is: an infinite gradient times
+        // each of them is the infinity that it is times y (an infinite or NaN y is whole in the first plane)
+        float rest[2] = {y[0], y[1]};
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            if (!W) {
-                o.c[j][0] = codes_bf16(o.q[j] & block_mask, pow2);
-                continue;
-            }
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                const v2f x = h & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8(o.q[j][h >> 1], true) : __builtin_amdgcn_cvt_pk_f32_fp8(o.q[j][h >> 1], false);
+        for (int p = 0; p < PLANES; ++p) {
+            uint32_t r = __builtin_amdgcn_perm(__float_as_uint(rest[1]), __float_as_uint(rest[0]), 0x07060302u);
+            asm volatile("" : "+v"(r));
+            o[p][h] = r;
+            if (p + 1 < PLANES)
 #pragma unroll
                 for (int v = 0; v < 2; ++v) {
-                    float y = x[v] * o.s[h >> 1][(h & 1) * 2 + v];
-#pragma unroll
-                    for (int p = 0; p < PLANES; ++p) {
-                        o.c[j][p][h * 2 + v] = (__bf16)y;
-                        if (p + 1 < PLANES) {
-                            y -= (float)o.c[j][p][h * 2 + v];
-                            if (y != y) y = 0.f;               // (the first plane has the infinity)
-                        }
-                    }
+                    rest[v] -= __uint_as_float(__float_as_uint(rest[v]) & 0xFFFF0000u);
+                    rest[v] = copysignf(fmaxf(fabsf(rest[v]), fminf(fabsf(y[v]), 0x1p-126f)), y[v]);
                 }
-            }
         }
     };
-    auto product = [&](const operands<PLANES>& o, int i, int p) {
+    // Part P of a group's products: all rows, columns 16 NJ P and on.  Between them, piece by piece, what comes behind needs: the codes of the next
+    // part are converted, those of the next group (at `at`, group G) come from LDS in the first part, and in the last dy of the next group takes
+    // the place of what has been used.  The compiler would gather these and wait for them.
+    auto part = [&](auto P_, uint32_t at, auto G_) {
+        constexpr int P = decltype(P_)::value, G = decltype(G_)::value, NP = (P + 1) % PARTS, NG = P + 1 < PARTS ? 1 - G : G;
+        if (P == 0) fetch_codes(at, G);
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(o.c[j][p], __builtin_bit_cast(v8bf, o.d[i]), acc[i][j], 0, 0, 0);
+        for (int i = 0; i < 8; ++i) {
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+                for (int jj = 0; jj < NJ; ++jj) {
+                    const int j = i & 1 ? NJ - 1 - jj : jj;    // (neighbouring products share an operand)
+                    v4f& r = acc[i][P * NJ + j];
+                    r = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, c[P & 1][j][p]), __builtin_bit_cast(v8bf, d[i]), r, 0, 0, 0);
+                }
+            __builtin_amdgcn_sched_barrier(0);
+            if (P == PARTS - 1) fetch_dy(at, G, i);
+            if (NJ == 2 || i % 2 == 0) convert(c[NP & 1][NJ == 2 ? i >> 2 : 0], q[NG][NP * NJ + (NJ == 2 ? i >> 2 : 0)], sc[NG], NJ == 2 ? i & 3 : i / 2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
-    // The products of `o`, while the operands of the next group (if there is one) come from LDS behind the first of them and are converted
-    // behind the others: in this order, which the compiler would not keep by itself
-    auto group = [&](operands<PLANES>& o, operands<PLANES>* next, auto rescale_, float ratio) {
-        constexpr bool rescale = decltype(rescale_)::value;
-        if (rescale) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                acc[i][0] *= ratio;
-                acc[i][1] *= ratio;
-                product(o, i, 0);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) product(o, i, 0);
+    auto group = [&](uint32_t at, auto G_) {
+        part(step<0>{}, at, G_);
+        part(step<1>{}, at, G_);
+        if (PARTS > 2) {
+            part(step<(PARTS > 2 ? 2 : 0)>{}, at, G_);
+            part(step<(PARTS > 2 ? 3 : 1)>{}, at, G_);
         }
-        if (PLANES > 1) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {      // an infinite gradient counts in the first plane, the others have both signs and zeros
-#pragma unroll
-                for (int v = 0; v < 8; ++v) o.d[i][v] = (o.d[i][v] & 0x7F80) == 0x7F80 ? (short)0 : o.d[i][v];
-            }
-#pragma unroll
-            for (int p = 1; p < PLANES; ++p)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) product(o, i, p);
-        }
-        if (next) convert(*next);
-        if (PLANES == 1) {
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                __builtin_amdgcn_sched_group_barrier(0x100, W ? 3 : 2, 0);     // LDS reads
-                if (rescale) __builtin_amdgcn_sched_group_barrier(0x2, 16, 0);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);               // a product
-            }
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                __builtin_amdgcn_sched_group_barrier(0x2, rescale ? 18 : W ? 8 : 2, 0);
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-            }
-        }
-        __builtin_amdgcn_sched_barrier(0);
     };
 
-    // ---- the sum.  Operands are fetched one group of products ahead; the barrier that hands over the stages stands before a stage's last group,
-    // so that the first operands of the next come during its products
+    // ---- the sum.  The barrier that hands over the stages stands between the two groups of a stage: the second's operands have been
+    // read by then, and those of the next stage come during its products
     if (nk > k0) {
         copy(k0);
         if (nk > k0 + 1) {
@@ -441,34 +429,35 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
             asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
         }
         if (W) clear_behind(k0);
-        operands<PLANES> f, g;
-        fetch(f, 0, step<0>{});
-        auto stage = [&](int kb, auto first_) {
-            constexpr bool first = decltype(first_)::value;    // (dgrad) of a block of scales
+        float ratio = W ? 1.f : next_block(k0);
+        fetch_codes(0, 0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) fetch_dy(0, 0, i);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int h = 0; h < 4; ++h) convert(c[0][j], q[0][j], sc[0], h);
+        for (int kb = k0; kb < nk; ++kb) {
             const uint32_t at = (uint32_t)((kb - k0) & 1) * G_STAGE;
-            const float ratio = first ? next_block(kb) : 1.f;
-            if (!W && first) convert(f);
-            fetch(g, at, step<1>{});
-            group(f, &g, first_, ratio);
-            fetch(f, at, step<2>{});
-            group(g, &f, std::false_type{}, 1.f);
-            fetch(g, at, step<3>{});
-            group(f, &g, std::false_type{}, 1.f);
+            if (!W && (kb & 1) == 0) {         // of a block of scales the first stage
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[i][j] *= ratio;
+            }
+            group(at, step<1>{});
             if (kb + 1 < nk) {
                 asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // stage kb+1 is there, and this one has been read
                 if (kb + 2 < nk) copy(kb + 2);
                 if (W) clear_behind(kb + 1);
             }
-            fetch(f, G_STAGE - at, step<0>{});                 // (behind the last stage: of no use, and not used)
-            group(g, W || first ? &f : nullptr, std::false_type{}, 1.f);
-        };
-        if (W) {
-            convert(f);
-            for (int kb = k0; kb < nk; ++kb) stage(kb, std::false_type{});
-        } else {
-            for (int kb = k0; kb < nk; kb += 2) {              // two stages to a block of scales
-                stage(kb, std::true_type{});
-                stage(kb + 1, std::false_type{});
+            // (behind the last stage what is fetched is of no use, and not used)
+            part(step<0>{}, G_STAGE - at, step<0>{});
+            if (!W && (kb & 1) && kb + 1 < nk) ratio = next_block(kb + 1);
+            part(step<1>{}, G_STAGE - at, step<0>{});
+            if (PARTS > 2) {
+                part(step<(PARTS > 2 ? 2 : 0)>{}, G_STAGE - at, step<0>{});
+                part(step<(PARTS > 2 ? 3 : 1)>{}, G_STAGE - at, step<0>{});
             }
         }
     }
@@ -480,13 +469,9 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        f32x4 r = {acc[i][j][g * 4], acc[i][j][g * 4 + 1], acc[i][j][g * 4 + 2], acc[i][j][g * 4 + 3]};
-                        if (!W) r *= unit_scale;
-                        out[((i * 2 + j) * 4 + g) * G_THREADS] = r;
-                    }
+                    for (int j = 0; j < 4; ++j) out[((i * 2 + h) * 4 + j) * G_THREADS] = W ? acc[i * 2 + h][j] : acc[i * 2 + h][j] * unit_scale;
         return;
     }
     __syncthreads();                           // (the last stage has been read)
@@ -497,12 +482,9 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
     for (int i = 0; i < 4; ++i) {
         f32x4 r[2][4];
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                r[j][g] = f32x4{acc[i][j][g * 4], acc[i][j][g * 4 + 1], acc[i][j][g * 4 + 2], acc[i][j][g * 4 + 3]};
-                if (!W) r[j][g] *= unit_scale;
-            }
+            for (int j = 0; j < 4; ++j) r[h][j] = W ? acc[i * 2 + h][j] : acc[i * 2 + h][j] * unit_scale;
         const int row = row0 + i * 32;
         if (row < end) store_rows<F32>(a, buffer, r, (W ? (size_t)e * mat : 0) + (size_t)row * a.K + cols0, end - row);
     }
@@ -522,9 +504,9 @@ __global__ __launch_bounds__(G_THREADS) void grad_join_kernel(const grad_args a)
     const f32x4* in = reinterpret_cast<const f32x4*>(a.parts) + ((size_t)u.slot * 4 + i) * 8 * G_THREADS + tid;
     for (int p = 0; p < u.parts; ++p, in += 4 * 8 * G_THREADS)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) r[j][g] += in[(j * 4 + g) * G_THREADS];
+            for (int j = 0; j < 4; ++j) r[h][j] += in[(h * 4 + j) * G_THREADS];
     store_rows<F32>(a, s_out + wave * 32 * OUT_LD, r, (W ? (size_t)u.e * a.NOUT * a.K : 0) + (size_t)row * a.K + cols0, end - row);
 }
 
