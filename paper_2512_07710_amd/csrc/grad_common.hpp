@@ -60,6 +60,39 @@ __device__ inline void store8(void* row, int64_t i, const vec8& r) {
         }
     }
 }
+// The same at any element (rows of odd length start at odd places) and past the caches, for rows that are requested ahead: as they lie in memory
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+typedef f32x4 __attribute__((aligned(4))) f32x4_any;
+template <bool BF16>
+struct raw8 {
+    u32x4 a[BF16 ? 1 : 2];
+    __device__ void load(const void* row, int64_t i) {
+        const u32x4_any* const p = reinterpret_cast<const u32x4_any*>(static_cast<const char*>(row) + i * (BF16 ? 2 : 4));
+#pragma unroll
+        for (int j = 0; j < (BF16 ? 1 : 2); ++j) a[j] = __builtin_nontemporal_load(p + j);
+    }
+    __device__ float at(int j) const {
+        return BF16 ? (j & 1 ? bf16hi(a[0][j >> 1]) : bf16lo(a[0][j >> 1])) : __uint_as_float(a[BF16 ? 0 : j >> 2][BF16 ? 0 : j & 3]);
+    }
+};
+template <bool BF16>
+__device__ inline void store8_any(void* row, int64_t i, const vec8& r) {
+    if (BF16) {
+        u32x4 u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) u[j] = bf16_bits(r.v[2 * j]) | (bf16_bits(r.v[2 * j + 1]) << 16);
+        __builtin_nontemporal_store(u, reinterpret_cast<u32x4_any*>(static_cast<uint16_t*>(row) + i));
+    } else {
+        f32x4_any* const p = reinterpret_cast<f32x4_any*>(static_cast<float*>(row) + i);
+        __builtin_nontemporal_store(f32x4{r.v[0], r.v[1], r.v[2], r.v[3]}, p);
+        __builtin_nontemporal_store(f32x4{r.v[4], r.v[5], r.v[6], r.v[7]}, p + 1);
+    }
+}
+__device__ inline vec8 load8_any(const float* row, int64_t i) {                // (kept in the caches)
+    const f32x4_any* const p = reinterpret_cast<const f32x4_any*>(row + i);
+    const f32x4 a = p[0], b = p[1];
+    return vec8{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
+}
 template <bool BF16>
 __device__ inline float load1(const void* row, int64_t i) {
     return BF16 ? __uint_as_float((uint32_t) static_cast<const uint16_t*>(row)[i] << 16) : static_cast<const float*>(row)[i];

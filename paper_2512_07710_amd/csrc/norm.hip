@@ -1,10 +1,12 @@
 // Residual addition, root-mean-square norm and e4m3 coding in one pass over a row, and the norm's gradient.
 #include "grad_common.hpp"
+#include "lanes.hpp"
 
 namespace moe355 {
 namespace {
 
 constexpr int NORM_MAX_THREADS = 1024;
+constexpr int NORM_ROWS = 16;                  // rows of a block at most
 constexpr int NORM_VECTORS = 4;                // vectors of eight elements that a thread holds at most
 
 struct norm_args {
@@ -18,45 +20,72 @@ struct norm_args {
     float *scales, *rstd;
 };
 
-// One block per row, the row in registers.  VEC: rows of whole aligned vectors, thread t of TPR holds vectors t, t+TPR, ...; sixteen
-// neighbouring threads hold a group of 128 columns.  Otherwise single elements, read again for the output.
-template <bool BF16, int NV>
-__global__ __launch_bounds__(NORM_MAX_THREADS) void norm_kernel(const norm_args a) {
-    __shared__ float lds[16];
-    const int vecs = a.cols / 8, waves = blockDim.x >> 6;
-    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const void* const x = row_of<BF16>(a.x, r * a.ld_x);
-        const void* const res = a.residual ? row_of<BF16>(a.residual, r * a.ld_res) : nullptr;
+// Rows in vectors of eight elements and what is left over, one to a thread; `per_block` neighbouring rows to a block, each in registers while the next is on its way: thread t of a block
+// of n holds vectors t, t+n, ...; sixteen neighbouring threads hold a group of 128 columns.  Scales leave in runs of NORM_ROWS words: as single
+// words each would be a part of a cache line of its own.
+template <bool BF16, int NV, bool REST>         // REST: cols is no multiple of eight (an instance of its own, it takes registers)
+__global__ __launch_bounds__(NORM_MAX_THREADS) void norm_kernel(const norm_args a, int per_block) {
+    __shared__ float lds[2][16];
+    extern __shared__ float s_scales[];        // [cols / 128][NORM_ROWS]
+    const int vecs = a.cols / 8, waves = blockDim.x >> 6, tid = threadIdx.x, lane = tid & 63;
+    const int rest = REST ? a.cols & 7 : 0, last = vecs * 8 + tid;        // thread t < rest has column `last` as well
+    const int64_t r0 = (int64_t)blockIdx.x * per_block;
+    const int rows = (int)(a.rows - r0 < per_block ? a.rows - r0 : per_block);
+    raw8<BF16> x[NV], res[NV];
+    float x1 = 0.f, res1 = 0.f;
+    auto request = [&](int64_t r) {
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+            const int i = tid + n * blockDim.x;
+            if (i >= vecs) continue;
+            x[n].load(row_of<BF16>(a.x, r * a.ld_x), (int64_t)i * 8);
+            if (a.residual) res[n].load(row_of<BF16>(a.residual, r * a.ld_res), (int64_t)i * 8);
+        }
+        if (REST && tid < rest) {
+            x1 = load1<BF16>(a.x, r * a.ld_x + last);
+            if (a.residual) res1 = load1<BF16>(a.residual, r * a.ld_res + last);
+        }
+    };
+    request(r0);
+    for (int k = 0; k < rows; ++k) {
+        const int64_t r = r0 + k;
         vec8 h[NV];
         float square = 0.f;
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
-            const int i = threadIdx.x + n * blockDim.x;
-            if (i >= vecs) {
-                h[n] = vec8{};
-                continue;
-            }
-            h[n] = load8<BF16>(x, (int64_t)i * 8);
-            if (res) {
-                const vec8 v = load8<BF16>(res, (int64_t)i * 8);
+            if (tid + n * (int)blockDim.x >= vecs) continue;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) h[n].v[j] = rounded<BF16>(h[n].v[j] + v.v[j]);
+            for (int j = 0; j < 8; ++j) {
+                h[n].v[j] = a.residual ? rounded<BF16>(x[n].at(j) + res[n].at(j)) : x[n].at(j);
+                square = fmaf(h[n].v[j], h[n].v[j], square);
             }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) square = fmaf(h[n].v[j], h[n].v[j], square);
         }
-        const float inv = 1.0f / sqrtf(block_sum(square, lds, waves) / (float)a.cols + a.eps);
-        if (a.rstd && threadIdx.x == 0) a.rstd[r] = inv;
+        const float h1 = REST && a.residual ? rounded<BF16>(x1 + res1) : x1;   // (zero for a thread without)
+        if (REST) square = fmaf(h1, h1, square);
+        if (k + 1 < rows) request(r + 1);
+        square = wave_total(square);
+        if (waves > 1) {
+            if (lane == 0) lds[k & 1][tid >> 6] = square;
+            __syncthreads();
+            square = wave_total(lane < waves ? lds[k & 1][lane] : 0.f);
+        }
+        const float inv = 1.0f / sqrtf(square / (float)a.cols + a.eps);
+        if (a.rstd && tid == 0) a.rstd[r] = inv;
+        if (REST && tid < rest) {
+            if (a.sum) store1<BF16>(a.sum, r * a.cols + last, h1);
+            if (a.y) store1<BF16>(a.y, r * a.cols + last, h1 * inv * a.gain[last]);
+        }
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
-            const int i = threadIdx.x + n * blockDim.x;
-            if (i >= vecs) continue;           // (whole groups of sixteen threads)
-            if (a.sum) store8<BF16>(row_of<BF16>(a.sum, r * a.cols), (int64_t)i * 8, h[n]);
-            const vec8 g = load8<false>(a.gain, (int64_t)i * 8);
+            const int i = tid + n * blockDim.x;
+            if (i >= vecs) continue;           // (with codes: whole groups of sixteen threads)
+            if (a.sum) store8_any<BF16>(row_of<BF16>(a.sum, r * a.cols), (int64_t)i * 8, h[n]);
+            if (!a.y && !a.q) continue;
+            const vec8 g = load8_any(a.gain, (int64_t)i * 8);
             vec8 y;
 #pragma unroll
             for (int j = 0; j < 8; ++j) y.v[j] = h[n].v[j] * inv * g.v[j];
-            if (a.y) store8<BF16>(row_of<BF16>(a.y, r * a.cols), (int64_t)i * 8, y);
+            if (a.y) store8_any<BF16>(row_of<BF16>(a.y, r * a.cols), (int64_t)i * 8, y);
             if (a.q) {
                 float amax = 0.f;
 #pragma unroll
@@ -67,14 +96,22 @@ __global__ __launch_bounds__(NORM_MAX_THREADS) void norm_kernel(const norm_args 
                 u32x2 c;
                 c[0] = coder.pack4(y.v[0], y.v[1], y.v[2], y.v[3]);
                 c[1] = coder.pack4(y.v[4], y.v[5], y.v[6], y.v[7]);
-                *reinterpret_cast<u32x2*>(a.q + r * a.cols + (int64_t)i * 8) = c;
-                if ((threadIdx.x & 15) == 0) a.scales[(int64_t)(i >> 4) * a.rows + r] = coder.s;
+                __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(a.q + r * a.cols + (int64_t)i * 8));
+                if ((tid & 15) == 0) {
+                    if (per_block == 1) a.scales[(int64_t)(i >> 4) * a.rows + r] = coder.s;
+                    else s_scales[(i >> 4) * NORM_ROWS + k] = coder.s;
+                }
             }
         }
     }
+    if (a.q && per_block > 1) {
+        __syncthreads();
+        for (int i = tid; i < a.cols / QBLOCK * NORM_ROWS; i += blockDim.x)
+            if (i % NORM_ROWS < rows) a.scales[(int64_t)(i / NORM_ROWS) * a.rows + r0 + i % NORM_ROWS] = s_scales[i];
+    }
 }
 
-// Any width, stride and alignment: element by element, the row read twice.  No codes.
+// Rows too wide for a block's registers: element by element, the row read twice.  No codes.
 template <bool BF16>
 __global__ __launch_bounds__(256) void norm_any_kernel(const norm_args a) {
     __shared__ float lds[4];
@@ -109,60 +146,92 @@ struct norm_back_args {
     float* partial;                            // [gridDim.x][cols]: each block's part of dgain
 };
 
-// Rows of block b: b, b + gridDim.x, ...; a thread keeps its columns' part of dgain in registers over all of them.
-template <bool BF16, int NV>
-__global__ __launch_bounds__(NORM_MAX_THREADS) void norm_back_kernel(const norm_back_args a) {
-    __shared__ float lds[16];
-    const int vecs = a.cols / 8, waves = blockDim.x >> 6;
+// Rows of block b: b, b + gridDim.x, ..., each requested while the one before is worked on; a thread keeps its columns' part of dgain in registers
+// over all of them.
+template <bool BF16, int NV, int THREADS, bool REST>
+__global__ __launch_bounds__(THREADS) void norm_back_kernel(const norm_back_args a) {
+    __shared__ float lds[2][16];
+    const int vecs = a.cols / 8, waves = blockDim.x >> 6, tid = threadIdx.x, lane = tid & 63;
     vec8 dg[NV];
 #pragma unroll
     for (int n = 0; n < NV; ++n) dg[n] = vec8{};
-    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    raw8<BF16> dy[NV], h[NV], dh[NV];
+    const int rest = REST ? a.cols & 7 : 0, last = vecs * 8 + tid;        // thread t < rest has column `last` as well
+    float dy1 = 0.f, h1 = 0.f, dh1 = 0.f, dg1 = 0.f;
+    const float g1 = REST && tid < rest ? a.gain[last] : 0.f;
+    auto request = [&](int64_t r) {
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+            const int i = tid + n * blockDim.x;
+            if (i >= vecs) continue;
+            dy[n].load(a.dy, r * a.cols + (int64_t)i * 8);
+            h[n].load(a.h, r * a.cols + (int64_t)i * 8);
+            if (a.dh) dh[n].load(a.dh, r * a.cols + (int64_t)i * 8);
+        }
+        if (REST && tid < rest) {
+            dy1 = load1<BF16>(a.dy, r * a.cols + last);
+            h1 = load1<BF16>(a.h, r * a.cols + last);
+            if (a.dh) dh1 = load1<BF16>(a.dh, r * a.cols + last);
+        }
+    };
+    request(blockIdx.x);
+    int turn = 0;
+    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
         const int64_t row = r * a.cols;
         const float inv = a.rstd[r];
-        vec8 u[NV], h[NV];
+        vec8 d[NV], f[NV];                     // inv * gain * dy (+ dh), and h
         float dot = 0.f;
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
-            const int i = threadIdx.x + n * blockDim.x;
-            if (i >= vecs) {
-                u[n] = h[n] = vec8{};
-                continue;
-            }
-            u[n] = load8<BF16>(a.dy, row + (int64_t)i * 8);
-            h[n] = load8<BF16>(a.h, row + (int64_t)i * 8);
-            const vec8 g = load8<false>(a.gain, (int64_t)i * 8);
+            const int i = tid + n * blockDim.x;
+            if (i >= vecs) continue;
+            const vec8 g = load8_any(a.gain, (int64_t)i * 8);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                dg[n].v[j] = fmaf(u[n].v[j] * inv, h[n].v[j], dg[n].v[j]);
-                u[n].v[j] *= g.v[j];
-                dot = fmaf(u[n].v[j], h[n].v[j], dot);
+                f[n].v[j] = h[n].at(j);
+                const float u = dy[n].at(j) * inv;
+                dg[n].v[j] = fmaf(u, f[n].v[j], dg[n].v[j]);
+                const float t = u * g.v[j];
+                dot = fmaf(t, f[n].v[j], dot);
+                d[n].v[j] = a.dh ? t + dh[n].at(j) : t;
             }
         }
-        const float f = block_sum(dot, lds, waves) / (float)a.cols * inv * inv * inv;
+        const float f1 = h1, u1 = dy1 * inv;
+        if (REST) {
+            dg1 = fmaf(u1, f1, dg1);
+            dot = fmaf(u1 * g1, f1, dot);
+        }
+        const float d1 = u1 * g1 + dh1;
+        if (r + gridDim.x < a.rows) request(r + gridDim.x);
+        dot = wave_total(dot);
+        if (waves > 1) {
+            if (lane == 0) lds[turn][tid >> 6] = dot;
+            __syncthreads();
+            dot = wave_total(lane < waves ? lds[turn][lane] : 0.f);
+        }
+        const float along = dot / (float)a.cols * inv * inv;
+        if (REST && tid < rest) store1<BF16>(a.dx, row + last, fmaf(-along, f1, d1));
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
-            const int i = threadIdx.x + n * blockDim.x;
+            const int i = tid + n * blockDim.x;
             if (i >= vecs) continue;
-            vec8 d;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) d.v[j] = fmaf(-f, h[n].v[j], inv * u[n].v[j]);
-            if (a.dh) {
-                const vec8 e = load8<BF16>(a.dh, row + (int64_t)i * 8);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) d.v[j] += e.v[j];
-            }
-            store8<BF16>(a.dx, row + (int64_t)i * 8, d);
+            for (int j = 0; j < 8; ++j) d[n].v[j] = fmaf(-along, f[n].v[j], d[n].v[j]);
+            store8_any<BF16>(a.dx, row + (int64_t)i * 8, d[n]);
         }
     }
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
-        const int i = threadIdx.x + n * blockDim.x;
-        if (i < vecs) store8<false>(a.partial, (int64_t)blockIdx.x * a.cols + (int64_t)i * 8, dg[n]);
+        const int i = tid + n * blockDim.x;
+        if (i >= vecs) continue;
+        f32x4_any* const p = reinterpret_cast<f32x4_any*>(a.partial + (int64_t)blockIdx.x * a.cols + (int64_t)i * 8);
+        p[0] = f32x4{dg[n].v[0], dg[n].v[1], dg[n].v[2], dg[n].v[3]};
+        p[1] = f32x4{dg[n].v[4], dg[n].v[5], dg[n].v[6], dg[n].v[7]};
     }
+    if (REST && tid < rest) a.partial[(int64_t)blockIdx.x * a.cols + last] = dg1;
 }
 
-// Any width and alignment.  A thread's columns of dgain are added up in the block's row of `partial`, which it alone touches.
+// Rows too wide for a block's registers.  A thread's columns of dgain are added up in the block's row of `partial`, which it alone touches.
 template <bool BF16>
 __global__ __launch_bounds__(256) void norm_back_any_kernel(const norm_back_args a) {
     __shared__ float lds[4];
@@ -186,25 +255,26 @@ __global__ __launch_bounds__(256) void norm_back_any_kernel(const norm_back_args
     }
 }
 
-// dgain[c] = sum of the blocks' parts: 32 columns a block, eight chains of rows joined at the end
-__global__ __launch_bounds__(256) void norm_gain_kernel(const float* __restrict__ partial, int parts, int cols, float* __restrict__ dgain) {
-    __shared__ float lds[8][32];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), chain = threadIdx.x >> 5;
+// dgain[c] = sum of the blocks' parts: 16 columns a block, 64 chains of parts joined at the end
+__global__ __launch_bounds__(1024) void norm_gain_kernel(const float* __restrict__ partial, int parts, int cols, float* __restrict__ dgain) {
+    __shared__ float lds[64][17];
+    const int lc = threadIdx.x & 15, c = blockIdx.x * 16 + lc, chain = threadIdx.x >> 4;
     float s = 0.f;
-    if (c < cols)
-        for (int p = chain; p < parts; p += 8) s += partial[(int64_t)p * cols + c];
-    lds[chain][threadIdx.x & 31] = s;
-    __syncthreads();
-    if (chain == 0 && c < cols) {
-        for (int w = 1; w < 8; ++w) s += lds[w][threadIdx.x];
-        dgain[c] = s;
+    if (c < cols) {
+#pragma unroll 4
+        for (int p = chain; p < parts; p += 64) s += partial[(int64_t)p * cols + c];
     }
+    lds[chain][lc] = s;
+    __syncthreads();
+    const int col = threadIdx.x >> 6, lane = threadIdx.x & 63;                 // a wave for each column
+    s = wave_total(lds[lane][col]);
+    if (lane == 0 && blockIdx.x * 16 + col < (unsigned)cols) dgain[blockIdx.x * 16 + col] = s;
 }
 
 // threads of a block that holds a row in vectors; 0: it does not fit
 int row_threads(int cols, int& vectors) {
-    const int vecs = cols / 8;
-    vectors = vecs <= 256 ? 1 : vecs <= 1024 ? 2 : NORM_VECTORS;
+    const int vecs = cols < 8 ? 1 : cols / 8;
+    vectors = vecs <= 256 ? 1 : vecs <= 2 * NORM_MAX_THREADS ? 2 : NORM_VECTORS;
     const int threads = ((vecs + vectors - 1) / vectors + 63) / 64 * 64;
     return threads <= NORM_MAX_THREADS ? threads : 0;
 }
@@ -214,44 +284,49 @@ constexpr int64_t NORM_MAX_GRID = 1 << 20;
 template <bool BF16>
 hipError_t norm_forward(hipStream_t s, const norm_args& a) {
     int vectors;
-    const int threads = row_threads(a.cols, vectors), eight = BF16 ? 8 : 4;
-    const unsigned grid = (unsigned)(a.rows < NORM_MAX_GRID ? a.rows : NORM_MAX_GRID);
-    const bool whole = threads && a.cols % 8 == 0 && a.ld_x % eight == 0 && a.ld_res % eight == 0 && aligned16(a.x) && aligned16(a.residual) &&
-                       aligned16(a.gain) && aligned16(a.sum) && aligned16(a.y) && ((uintptr_t)a.q & 7) == 0;
-    if (!whole) {
+    const int threads = row_threads(a.cols, vectors);
+    if (!threads) {
         if (a.q) return hipErrorInvalidValue;  // (the entry point has refused it)
-        norm_any_kernel<BF16><<<grid, 256, 0, s>>>(a);
-    } else if (vectors == 1) {
-        norm_kernel<BF16, 1><<<grid, threads, 0, s>>>(a);
-    } else if (vectors == 2) {
-        norm_kernel<BF16, 2><<<grid, threads, 0, s>>>(a);
-    } else {
-        norm_kernel<BF16, NORM_VECTORS><<<grid, threads, 0, s>>>(a);
+        norm_any_kernel<BF16><<<(unsigned)(a.rows < NORM_MAX_GRID ? a.rows : NORM_MAX_GRID), 256, 0, s>>>(a);
+        return hipGetLastError();
     }
+    // blocks of many rows for the sake of their scales, as long as 32 waves are left for a CU and no block is so long that the last ones run alone
+    // (32768 x 7168: 16 rows 352 us, 8 340, 4 332; 16384 x 2048: 8 rows 45.5, 4 47.7)
+    int64_t per_block = a.q ? a.rows * (threads / 64) / 8192 : 1;
+    if (per_block > 32768 / a.cols) per_block = 32768 / a.cols;
+    if (per_block > NORM_ROWS) per_block = NORM_ROWS;
+    if (per_block < 1) per_block = 1;
+    const int64_t blocks = (a.rows + per_block - 1) / per_block;
+    if (blocks > (int64_t)1 << 31) return hipErrorInvalidValue;
+    const size_t lds = a.q && per_block > 1 ? (size_t)a.cols / QBLOCK * NORM_ROWS * sizeof(float) : 0;
+    const bool rest = a.cols % 8 != 0;
+    const auto kernel = vectors == 1   ? (rest ? norm_kernel<BF16, 1, true> : norm_kernel<BF16, 1, false>)
+                        : vectors == 2 ? (rest ? norm_kernel<BF16, 2, true> : norm_kernel<BF16, 2, false>)
+                                       : (rest ? norm_kernel<BF16, NORM_VECTORS, true> : norm_kernel<BF16, NORM_VECTORS, false>);
+    kernel<<<(unsigned)blocks, threads, lds, s>>>(a, (int)per_block);
     return hipGetLastError();
 }
 
-constexpr int NORM_BACK_BLOCKS = 512;           // at most, and as many as the workspace has rows for
 
 template <bool BF16>
 hipError_t norm_backward(hipStream_t s, norm_back_args a, float* dgain) {
     int vectors;
     const int threads = row_threads(a.cols, vectors);
-    int blocks = (int)(GRAD_WS_BYTES / sizeof(float) / a.cols);
-    if (blocks > NORM_BACK_BLOCKS) blocks = NORM_BACK_BLOCKS;
-    if (blocks > a.rows) blocks = (int)a.rows;
-    const bool whole = threads && a.cols % 8 == 0 && aligned16(a.dy) && aligned16(a.h) && aligned16(a.dh) && aligned16(a.gain) && aligned16(a.dx);
-    if (blocks == 0) {
-    } else if (!whole) {
-        norm_back_any_kernel<BF16><<<blocks, 256, 0, s>>>(a);
-    } else if (vectors == 1) {
-        norm_back_kernel<BF16, 1><<<blocks, threads, 0, s>>>(a);
-    } else if (vectors == 2) {
-        norm_back_kernel<BF16, 2><<<blocks, threads, 0, s>>>(a);
-    } else {
-        norm_back_kernel<BF16, NORM_VECTORS><<<blocks, threads, 0, s>>>(a);
-    }
-    norm_gain_kernel<<<(a.cols + 31) / 32, 256, 0, s>>>(a.partial, blocks, a.cols, dgain);
+    // two blocks to a CU, more of narrow ones, all with about the same number of rows (4096 x 5120: 512 blocks of 8 rows 40 us, 716 of 5 or 6 48;
+    // 8192 x 1024: 512 blocks 31 us, 1024 23.5, 1792 22)
+    int blocks = threads > 192 || !threads ? 512 : threads > 128 ? 1024 : 1536;
+    if (blocks > (int)(GRAD_WS_BYTES / sizeof(float) / a.cols)) blocks = (int)(GRAD_WS_BYTES / sizeof(float) / a.cols);
+    const int64_t each = (a.rows + blocks - 1) / blocks;
+    blocks = each ? (int)((a.rows + each - 1) / each) : 0;
+    const bool rest = a.cols % 8 != 0;
+    const auto kernel = !threads         ? norm_back_any_kernel<BF16>
+                        : vectors == 1   ? (rest ? norm_back_kernel<BF16, 1, 512, true> : norm_back_kernel<BF16, 1, 512, false>)
+                        : threads <= 512 ? (rest ? norm_back_kernel<BF16, 2, 512, true> : norm_back_kernel<BF16, 2, 512, false>)
+                        : vectors == 2   ? (rest ? norm_back_kernel<BF16, 2, NORM_MAX_THREADS, true> : norm_back_kernel<BF16, 2, NORM_MAX_THREADS, false>)
+                                         : (rest ? norm_back_kernel<BF16, NORM_VECTORS, NORM_MAX_THREADS, true>
+                                                 : norm_back_kernel<BF16, NORM_VECTORS, NORM_MAX_THREADS, false>);
+    if (blocks > 0) kernel<<<blocks, threads ? threads : 256, 0, s>>>(a);
+    norm_gain_kernel<<<(a.cols + 15) / 16, 1024, 0, s>>>(a.partial, blocks, a.cols, dgain);
     return hipGetLastError();
 }
 

@@ -80,7 +80,6 @@ __device__ inline softmax_stats block_join(softmax_stats t, block_scratch& lds) 
 }
 
 // 16 bytes of a row, at any element: rows of odd length start at odd places
-typedef u32x4 __attribute__((aligned(2))) u32x4_any;
 typedef u32x2 __attribute__((aligned(2))) u32x2_any;
 template <bool BF16>
 struct row_type {
