@@ -237,18 +237,20 @@ def _of(t: Optional[torch.Tensor], dtype, *shape) -> Optional[int]:
     """Address of a contiguous tensor of this type and shape; None for None."""
     if t is None:
         return None
-    if t.shape != shape:
-        raise MoEError(f"expected shape {shape}, got {tuple(t.shape)}")
-    return _ptr(t, dtype)
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous() or not t.is_cuda:
+        raise MoEError(f"expected a contiguous CUDA tensor {shape} of {dtype}, got {tuple(t.shape)} of {t.dtype}, strides {t.stride()}, on {t.device}")
+    return t.data_ptr()
 
 
 def _rows_of(t: Optional[torch.Tensor], dtype, rows: int, cols: int):
     """(address, row stride) of a 2-D tensor whose rows are contiguous."""
     if t is None:
         return None, 0
-    if not t.is_cuda or t.dtype != dtype or t.shape != (rows, cols) or (cols > 1 and t.stride(1) != 1):
-        raise MoEError(f"expected a CUDA tensor ({rows}, {cols}) of {dtype} with contiguous rows, got {tuple(t.shape)} of {t.dtype}")
-    return t.data_ptr(), t.stride(0) if rows > 1 else max(cols, 1)
+    ld, unit = t.stride() if t.dim() == 2 else (0, 0)
+    if t.shape != (rows, cols) or t.dtype is not dtype or (unit != 1 and cols > 1) or not t.is_cuda:
+        raise MoEError(f"expected a CUDA tensor {(rows, cols)} of {dtype} with contiguous rows, got {tuple(t.shape)} of {t.dtype}, "
+                       f"strides {t.stride()}, on {t.device}")
+    return t.data_ptr(), ld if rows > 1 else max(cols, 1)
 
 
 def moe_reserve_gradients(ctx) -> None:

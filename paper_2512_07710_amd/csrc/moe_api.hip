@@ -279,7 +279,7 @@ int moe_reserve_gradients(moe_ctx* c) {
 int moe_add_rmsnorm(moe_ctx* c, const void* x, const void* residual, const float* gain, int64_t rows, int32_t cols, int64_t ld_x,
                     int64_t ld_res, int32_t dtype, float eps, void* sum, void* y, uint8_t* q, float* scales, float* rstd) {
     if (!c || !dtype_ok(dtype) || rows < 0 || cols < 1 || cols > NORM_MAX_COLS || !(eps >= 0.f) || !std::isfinite(eps)) return MOE_EINVAL;
-    if (rows > (int64_t)1 << 30 || ld_x < cols || ld_x > (int64_t)1 << 20 || (residual && (ld_res < cols || ld_res > (int64_t)1 << 20)))
+    if (rows > (int64_t)1 << 30 || ld_x < cols || ld_x >= (int64_t)1 << 31 || (residual && (ld_res < cols || ld_res >= (int64_t)1 << 31)))
         return MOE_EINVAL;
     if (!q != !scales) return MOE_EINVAL;
     if (rows == 0) return MOE_OK;
