@@ -41,6 +41,7 @@ struct grad_args {
     int64_t rows;
     int E, NOUT, K;
     int accumulate;
+    int cuts;                                  // whether tiles may be cut along the sum
     void* out;
     float* parts;                              // [units][rows / 32][2][4][256] f32x4: a thread's sums, in its own order
 };
@@ -83,7 +84,7 @@ struct unit {
     int row0, c0;                              // first row and column of the tile
     int part, parts, slot;                     // part of the sum; its place in the workspace
 };
-// The unit of block b; JOIN: of the launch that adds up, four blocks to a tile.  False: none.  Called by the whole block.
+// The unit of block b; JOIN: of the launch that adds up, a tile that was cut.  False: none.  Called by the whole block.
 template <bool W, bool JOIN = false>
 __device__ inline bool unit_of(const grad_args& a, int b, find_scratch& s, unit& u) {
     const int ctiles = (a.K + GN - 1) / GN, tid = threadIdx.x;
@@ -104,7 +105,7 @@ __device__ inline bool unit_of(const grad_args& a, int b, find_scratch& s, unit&
         }
     }
     const int total = row_tiles * ctiles;
-    const split_plan p = W && a.offsets ? split_plan{total, 0, 1} : plan_of(total, W ? (int)((a.rows + GK - 1) / GK) : a.NOUT / GK);
+    const split_plan p = !a.cuts ? split_plan{total, 0, 1} : plan_of(total, W ? (int)((a.rows + GK - 1) / GK) : a.NOUT / GK);
     int t;
     u.part = 0;
     u.parts = 1;
@@ -468,10 +469,12 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
         if (mine)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
+                if (W || row0 + i * 32 < hi)   // (the rows that there are)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) out[((i * 2 + h) * 4 + j) * G_THREADS] = W ? acc[i * 2 + h][j] : acc[i * 2 + h][j] * unit_scale;
+                    for (int n = 0; n < 8; ++n) {
+                        const v4f r = acc[i * 2 + (n >> 2)][n & 3];
+                        __builtin_nontemporal_store(W ? r : r * unit_scale, out + (i * 8 + n) * G_THREADS);
+                    }
         return;
     }
     __syncthreads();                           // (the last stage has been read)
@@ -490,24 +493,35 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
     }
 }
 
-// Adds up the parts of the tiles that were cut, in their order.  Four blocks to a tile, 32 rows each.
+// Adds up the parts of the tiles that were cut.  A block has 32 rows x 64 columns of a tile; each of its waves adds every fourth part, and the first
+// adds those sums, in their order: short chains, the parts come from other XCDs.
 template <bool W, bool F32>
 __global__ __launch_bounds__(G_THREADS) void grad_join_kernel(const grad_args a) {
+    constexpr int WAVES = G_THREADS / 64;
     __shared__ find_scratch s_find;
-    __shared__ __attribute__((aligned(16))) float s_out[4 * 32 * OUT_LD];
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = blockIdx.x & 3;
+    __shared__ __attribute__((aligned(16))) f32x4 s_sums[WAVES - 1][8][64];
+    __shared__ __attribute__((aligned(16))) float s_out[32 * OUT_LD];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = blockIdx.x >> 2 & 3, column = blockIdx.x & 3;
     unit u;
-    if (!unit_of<W, true>(a, blockIdx.x >> 2, s_find, u)) return;
-    const int cols0 = u.c0 + wave * 64, row = u.row0 + i * 32, end = W ? a.NOUT : u.hi;
+    if (!unit_of<W, true>(a, blockIdx.x >> 4, s_find, u)) return;
+    const int cols0 = u.c0 + column * 64, row = u.row0 + i * 32, end = W ? a.NOUT : u.hi;
     if (cols0 >= a.K || row >= end) return;
     f32x4 r[2][4] = {};
-    const f32x4* in = reinterpret_cast<const f32x4*>(a.parts) + ((size_t)u.slot * 4 + i) * 8 * G_THREADS + tid;
-    for (int p = 0; p < u.parts; ++p, in += 4 * 8 * G_THREADS)
+    const f32x4* const in = reinterpret_cast<const f32x4*>(a.parts) + ((size_t)u.slot * 4 + i) * 8 * G_THREADS + column * 64 + lane;
+#pragma unroll 3
+    for (int p = wave; p < u.parts; p += WAVES)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int n = 0; n < 8; ++n) r[n >> 2][n & 3] += __builtin_nontemporal_load(in + ((size_t)p * 4 * 8 + n) * G_THREADS);
+    if (wave > 0)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) r[h][j] += in[(h * 4 + j) * G_THREADS];
-    store_rows<F32>(a, s_out + wave * 32 * OUT_LD, r, (W ? (size_t)u.e * a.NOUT * a.K : 0) + (size_t)row * a.K + cols0, end - row);
+        for (int n = 0; n < 8; ++n) s_sums[wave - 1][n][lane] = r[n >> 2][n & 3];
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 0; w < WAVES - 1; ++w)
+#pragma unroll
+        for (int n = 0; n < 8; ++n) r[n >> 2][n & 3] += s_sums[w][n][lane];
+    store_rows<F32>(a, s_out, r, (W ? (size_t)u.e * a.NOUT * a.K : 0) + (size_t)row * a.K + cols0, end - row);
 }
 
 }  // namespace
@@ -524,14 +538,17 @@ static_assert((size_t)G_SLOTS * GM * GN * sizeof(float) <= GRAD_WS_BYTES, "the p
 
 // tiles: as many as there can be; stages: of a whole sum
 template <bool W, int PLANES, bool F32>
-hipError_t launch(moe_ctx* c, const grad_args& a, int64_t tiles, int stages) {
-    const bool known = !a.offsets;             // how many tiles there are
-    const split_plan p = W && !known ? split_plan{(int)tiles, 0, 1} : plan_of((int)tiles, stages);
+hipError_t launch(moe_ctx* c, grad_args a, int64_t tiles, int stages) {
+    // Grouped, the device alone knows how many tiles there are: they are cut only where they are sure to be less than a round (the second launch
+    // costs 5 us whether there is something to add up or not), and in the weights' gradient, where sums differ in length, not at all
+    const bool known = !a.offsets;
+    a.cuts = known || (!W && tiles <= G_SLOTS);
+    const split_plan p = known ? plan_of((int)tiles, stages) : split_plan{(int)tiles, 0, 1};
     int64_t units = p.whole + (int64_t)p.cut * p.parts;
-    if (!known) units = W ? (tiles + 511) / 512 * 512 : tiles + G_SLOTS;
+    if (!known) units = W ? (tiles + 511) / 512 * 512 : a.cuts ? G_SLOTS : tiles;
     grad_kernel<W, PLANES, F32><<<(unsigned)((units + 7) / 8 * 8 + 8), G_THREADS, G_LDS, c->stream>>>(a);
-    const int cut = known ? p.cut : W ? 0 : G_SLOTS / 2;
-    if (cut) grad_join_kernel<W, F32><<<(unsigned)(cut * 4), G_THREADS, 0, c->stream>>>(a);
+    const int cut = known ? p.cut : a.cuts ? (int)(tiles < G_SLOTS / 2 ? tiles : G_SLOTS / 2) : 0;
+    if (cut) grad_join_kernel<W, F32><<<(unsigned)(cut * 16), G_THREADS, 0, c->stream>>>(a);
     return hipGetLastError();
 }
 
@@ -539,13 +556,13 @@ hipError_t launch(moe_ctx* c, const grad_args& a, int64_t tiles, int stages) {
 
 hipError_t launch_linear_dgrad(moe_ctx* c, const uint16_t* dy, int64_t rows, int32_t NOUT, const uint8_t* Wq, const float* ws, int32_t K,
                                const int32_t* offsets, int32_t E, uint16_t* dx) {
-    const grad_args a{dy, Wq, ws, offsets, rows, E, NOUT, K, 0, dx, static_cast<float*>(c->grad_ws)};
+    const grad_args a{dy, Wq, ws, offsets, rows, E, NOUT, K, 0, 0, dx, static_cast<float*>(c->grad_ws)};
     return launch<false, 1, false>(c, a, (offsets ? rows / GM + E : (rows + GM - 1) / GM) * ((K + GN - 1) / GN), NOUT / GK);
 }
 
 hipError_t launch_linear_wgrad(moe_ctx* c, const uint16_t* dy, int64_t rows, int32_t NOUT, const uint8_t* xq, const float* xs, int32_t K,
                                const int32_t* offsets, int32_t E, int32_t accumulate, int32_t dtype, void* dW) {
-    const grad_args a{dy, xq, xs, offsets, rows, E, NOUT, K, accumulate, dW, static_cast<float*>(c->grad_ws)};
+    const grad_args a{dy, xq, xs, offsets, rows, E, NOUT, K, accumulate, 0, dW, static_cast<float*>(c->grad_ws)};
     const int64_t tiles = (int64_t)E * (NOUT / GM) * ((K + GN - 1) / GN);
     const int stages = (int)((rows + GK - 1) / GK);
     return dtype == MOE_BF16 ? launch<true, 1, false>(c, a, tiles, stages) : launch<true, 3, true>(c, a, tiles, stages);
