@@ -13,6 +13,11 @@ __device__ inline uint32_t bf16_bits(float v) {                // round to neare
     return (b + 0x7FFFu + ((b >> 16) & 1u)) >> 16;
 }
 
+__device__ inline uint32_t bf16_pair(float a, float b) {       // round to nearest even
+    typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, v2bf{(__bf16)a, (__bf16)b});
+}
+
 // Eight consecutive elements of a row as fp32.  BF16: 16 bytes, else 32; `p` is aligned to 16.
 struct vec8 {
     float v[8];

@@ -30,7 +30,8 @@ constexpr int GM = 128, GN = 256;              // tile of the result: rows (alon
 constexpr int GK = 64;                         // steps of the sum that are staged at a time
 constexpr int G_THREADS = 256;                 // four waves, each all 128 rows of the tile and 64 of its columns
 constexpr int DY_STAGE = GM * GK * 2, CODE_STAGE = GN * GK, SCALE_STAGE = 4 * GK * 4, G_STAGE = DY_STAGE + CODE_STAGE + SCALE_STAGE;
-constexpr int G_LDS = 2 * G_STAGE;             // two blocks to a CU
+constexpr int OUT_PITCH = 64 * 2 + 16, OUT_BYTES = 16 * OUT_PITCH;             // a wave's 16 x 64 results on their way out
+constexpr int G_LDS = 2 * G_STAGE + G_THREADS / 64 * OUT_BYTES;                // two blocks to a CU
 constexpr int G_MIN_PART = 4;                  // stages of a part of a sum at least
 
 struct grad_args {
@@ -46,15 +47,17 @@ struct grad_args {
     float* parts;                              // [units][rows / 32][2][4][256] f32x4: a thread's sums, in its own order
 };
 
-// expert e's rows
+// expert e's rows (in the constant address space, so that they come as scalar loads where e is the same for all: the wait for a vector load would
+// include the copies and stores that are under way)
 __device__ inline void segment(const grad_args& a, int e, int& lo, int& hi) {
     if (!a.offsets) {
         lo = 0;
         hi = (int)a.rows;
         return;
     }
-    lo = min(max(a.offsets[e], 0), (int)a.rows);
-    hi = min(max(a.offsets[e + 1], lo), (int)a.rows);
+    const __attribute__((address_space(4))) int32_t* const at = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)a.offsets + e;
+    lo = min(max(at[0], 0), (int)a.rows);
+    hi = min(max(at[1], lo), (int)a.rows);
 }
 
 // Tiles are dealt to the XCDs (blockIdx % 8) in runs, and run through a band of eight tile rows column by column, so that the 64 tiles that an XCD
@@ -92,7 +95,10 @@ __device__ inline bool unit_of(const grad_args& a, int b, find_scratch& s, unit&
     int first = 0, tiles = 0, l = 0, h = 0;    // (grouped dgrad) thread e: expert e's row tiles
     const bool search = !W && a.offsets;
     if (search) {
-        if (tid < a.E) segment(a, tid, l, h);
+        if (tid < a.E) {
+            l = min(max(a.offsets[tid], 0), (int)a.rows);
+            h = min(max(a.offsets[tid + 1], l), (int)a.rows);
+        }
         tiles = (h - l + GM - 1) / GM;
         const int upto = wave_scan(tiles);
         if ((tid & 63) == 63) s.waves[tid >> 6] = upto;
@@ -288,7 +294,7 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
             *reinterpret_cast<u32x4*>(at + DY_STAGE + i * 16) = zero;
         }
         if (lane >= left) *reinterpret_cast<float*>(at + DY_STAGE + CODE_STAGE + tid * 4) = 0.f;
-        __syncthreads();
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // (the copies that are under way are not waited for)
     };
 
     // ---- this wave's part: 128 rows x 64 columns of the tile, in products of 16 x 16 over 32 steps of the sum, a stage is two groups of them.
@@ -463,33 +469,53 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
         }
     }
 
-    // ---- a lane holds one row of the result, four neighbouring columns at a time
+    // ---- the result: a lane holds rows lane%16 of its tiles of 16 x 16, four neighbouring columns of each
+    if (!mine) return;
+    const int rows = W ? GM : min(hi - row0, GM);
     if (u.parts > 1) {
-        f32x4* const out = reinterpret_cast<f32x4*>(a.parts) + (size_t)u.slot * 4 * 8 * G_THREADS + tid;
-        if (mine)
+        char* const out = reinterpret_cast<char*>(a.parts) + ((size_t)u.slot * 4 * 8 * G_THREADS + wave * 64) * sizeof(f32x4);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (W || row0 + i * 32 < hi)   // (the rows that there are)
+        for (int i = 0; i < 4; ++i)
+            if (i * 32 < rows)                 // (those that there are)
 #pragma unroll
-                    for (int n = 0; n < 8; ++n) {
-                        const v4f r = acc[i * 2 + (n >> 2)][n & 3];
-                        __builtin_nontemporal_store(W ? r : r * unit_scale, out + (i * 8 + n) * G_THREADS);
-                    }
+                for (int n = 0; n < 8; ++n) {
+                    const v4f r = acc[i * 2 + (n >> 2)][n & 3];
+                    __builtin_nontemporal_store(W ? r : r * unit_scale, reinterpret_cast<f32x4*>(out + (i * 8 + n) * G_THREADS * sizeof(f32x4) + (uint32_t)lane * 16));
+                }
         return;
     }
-    __syncthreads();                           // (the last stage has been read)
-    if (!mine) return;
-    float* const buffer = reinterpret_cast<float*>(lds) + wave * 32 * OUT_LD;
-    const int end = W ? a.NOUT : hi;
+    // bf16 goes through LDS, a wave's own part of it, to be stored as whole lines of 128 bytes; fp32 has 64 bytes of a row in four lanes as it is
+    constexpr int BYTES = F32 ? 4 : 2;
+    char* const out_lds = lds + 2 * G_STAGE + wave * OUT_BYTES;
+    char* base = static_cast<char*>(a.out) + ((W ? (size_t)e * mat : 0) + (size_t)row0 * a.K + cols0) * BYTES;
+    const uint32_t own = (c16 * (uint32_t)a.K + r4 * 4) * BYTES, line = (r8 * (uint32_t)a.K + (lane & 7) * 8) * BYTES;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f32x4 r[2][4];
+    for (int i = 0; i < 8; ++i, base += (size_t)16 * a.K * BYTES) {
+        if (i * 16 >= rows) break;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int j = 0; j < 4; ++j) {
+            v4f r = acc[i][j];
+            if (!W) r *= unit_scale;
+            if (F32) {
+                f32x4* const p = reinterpret_cast<f32x4*>(base + j * 64 + own);
+                if (a.accumulate) r += *p;
+                *p = r;
+                continue;
+            }
+            if (W && a.accumulate) {
+                const u32x2 was = *reinterpret_cast<const u32x2*>(base + j * 32 + own);
+                r += v4f{bf16lo(was[0]), bf16hi(was[0]), bf16lo(was[1]), bf16hi(was[1])};
+            }
+            *reinterpret_cast<u32x2*>(out_lds + c16 * OUT_PITCH + j * 32 + r4 * 8) = u32x2{bf16_pair(r[0], r[1]), bf16_pair(r[2], r[3])};
+        }
+        if (F32) continue;
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
-            for (int j = 0; j < 4; ++j) r[h][j] = W ? acc[i * 2 + h][j] : acc[i * 2 + h][j] * unit_scale;
-        const int row = row0 + i * 32;
-        if (row < end) store_rows<F32>(a, buffer, r, (W ? (size_t)e * mat : 0) + (size_t)row * a.K + cols0, end - row);
+        for (int h = 0; h < 2; ++h) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(out_lds + (h * 8 + r8) * OUT_PITCH + (lane & 7) * 16);
+            if (i * 16 + h * 8 + r8 < rows) *reinterpret_cast<u32x4*>(base + (size_t)h * 8 * a.K * BYTES + line) = v;
+        }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 

@@ -91,10 +91,6 @@ struct row_type {
     }
 };
 
-__device__ inline uint32_t bf16_pair(float a, float b) {       // round to nearest even
-    typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, v2bf{(__bf16)a, (__bf16)b});
-}
 // vector i of N gradients
 template <bool BF16, int N>
 __device__ inline void store_grad(void* row, int64_t i, const float (&g)[N]) {
