@@ -484,7 +484,8 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
                 }
         return;
     }
-    // bf16 goes through LDS, a wave's own part of it, to be stored as whole lines of 128 bytes; fp32 has 64 bytes of a row in four lanes as it is
+    // bf16 goes through LDS, a wave's own part of it, to be stored as whole lines of 128 bytes, past the caches (1 to 4 % faster at all sizes tried);
+    // fp32 has 64 bytes of a row in four lanes as it is, which the caches put together (past them 40 x 6144 x 4096 26 -> 33 us)
     constexpr int BYTES = F32 ? 4 : 2;
     char* const out_lds = lds + 2 * G_STAGE + wave * OUT_BYTES;
     char* base = static_cast<char*>(a.out) + ((W ? (size_t)e * mat : 0) + (size_t)row0 * a.K + cols0) * BYTES;
@@ -513,7 +514,7 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const u32x4 v = *reinterpret_cast<const u32x4*>(out_lds + (h * 8 + r8) * OUT_PITCH + (lane & 7) * 16);
-            if (i * 16 + h * 8 + r8 < rows) *reinterpret_cast<u32x4*>(base + (size_t)h * 8 * a.K * BYTES + line) = v;
+            if (i * 16 + h * 8 + r8 < rows) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(base + (size_t)h * 8 * a.K * BYTES + line));
         }
         __builtin_amdgcn_wave_barrier();
     }
