@@ -293,7 +293,7 @@ int moe_policy_loss(moe_ctx* ctx, const void* logits, int64_t ld, int32_t dtype,
  *     the scale runs along the sum, so the operand is xs*xq: rounded to bf16 for a bf16 dW (an error the size of the output's own
  *     rounding), held to 24 bits in three bf16 planes for a f32 dW.
  *   dy [rows,NOUT] bf16; Wq [E,NOUT,K] u8; ws [E,NOUT/128,K/128] f32; xq [rows,K] u8; xs [K/128][rows] f32;
- *   dx [rows,K] bf16; dW [E,NOUT,K] dtype.  K and NOUT multiples of 128, NOUT*K < 2^32 and 1 <= E <= 256; rows < 2^31 - 256. */
+ *   dx [rows,K] bf16; dW [E,NOUT,K] dtype.  K and NOUT multiples of 128 up to 2^24, NOUT*K < 2^32 and 1 <= E <= 256; rows < 2^31 - 256. */
 int moe_linear_fp8_dgrad(moe_ctx* ctx, const uint16_t* dy, int64_t rows, int32_t NOUT, const uint8_t* Wq, const float* ws, int32_t K,
                          const int32_t* offsets, int32_t E, uint16_t* dx);
 int moe_linear_fp8_wgrad(moe_ctx* ctx, const uint16_t* dy, int64_t rows, int32_t NOUT, const uint8_t* xq, const float* xs, int32_t K,

@@ -6,6 +6,7 @@
 // What does not run along the sum is transposed on its way from LDS to the registers by the transposing LDS reads.
 #include "ffn_common.hpp"
 #include "grad_common.hpp"
+#include "grad_rules.hpp"
 
 #include <type_traits>
 
@@ -26,13 +27,10 @@ typedef __attribute__((address_space(3))) v4s* lds_v4s_ptr;
 typedef __attribute__((address_space(3))) const v8s* lds_v8s_ptr;
 typedef __attribute__((address_space(3))) const v4f* lds_v4f_ptr;
 
-constexpr int GM = 128, GN = 256;              // tile of the result: rows (along dy) and columns (along the codes)
-constexpr int GK = 64;                         // steps of the sum that are staged at a time
 constexpr int G_THREADS = 256;                 // four waves, each all 128 rows of the tile and 64 of its columns
 constexpr int DY_STAGE = GM * GK * 2, CODE_STAGE = GN * GK, SCALE_STAGE = 4 * GK * 4, G_STAGE = DY_STAGE + CODE_STAGE + SCALE_STAGE;
 constexpr int OUT_PITCH = 64 * 2 + 16, OUT_BYTES = 16 * OUT_PITCH;             // a wave's 16 x 64 results on their way out
 constexpr int G_LDS = 2 * G_STAGE + G_THREADS / 64 * OUT_BYTES;                // two blocks to a CU
-constexpr int G_MIN_PART = 4;                  // stages of a part of a sum at least
 
 struct grad_args {
     const uint16_t* dy;
@@ -58,25 +56,6 @@ __device__ inline void segment(const grad_args& a, int e, int& lo, int& hi) {
     const __attribute__((address_space(4))) int32_t* const at = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)a.offsets + e;
     lo = min(max(at[0], 0), (int)a.rows);
     hi = min(max(at[1], lo), (int)a.rows);
-}
-
-// Tiles are dealt to the XCDs (blockIdx % 8) in runs, and run through a band of eight tile rows column by column, so that the 64 tiles that an XCD
-// works on at a time share their operands in its L2.  Tiles that do not fill a round of the chip are cut along the sum: parts
-// go to the workspace and a second launch adds them up.
-constexpr int G_SLOTS = 512, G_BAND = 8;       // blocks that run at a time
-struct split_plan {
-    int whole, cut, parts;                     // tiles done at once; tiles in parts, and how many parts
-};
-__host__ __device__ inline split_plan plan_of(int tiles, int stages) {
-    split_plan p{tiles, 0, 1};
-    const int rest = tiles % G_SLOTS;
-    if (rest == 0) return p;
-    int parts = G_SLOTS / rest;
-    if (parts > stages / G_MIN_PART) parts = stages / G_MIN_PART;
-    if (parts < (tiles < G_SLOTS ? 2 : 3)) return p;
-    // (in stages) what is saved against what the parts' way through memory costs
-    if (tiles >= G_SLOTS && stages * (0.55f - 1.0f / parts) < 24.f) return p;
-    return split_plan{tiles - rest, rest, parts};
 }
 
 struct find_scratch {
@@ -122,21 +101,8 @@ __device__ inline bool unit_of(const grad_args& a, int b, find_scratch& s, unit&
         u.parts = p.parts;
         u.slot = b * p.parts;
     } else {
-        const int units = p.whole + p.cut * p.parts, x = b & 7, at = b >> 3;
-        int n;
-        if (W && a.offsets) {                  // experts' sums have different lengths: runs of 64 tiles, taken in turns
-            n = (at / 64 * 8 + x) * 64 + at % 64;
-            if (n >= units) return false;
-        } else if (p.whole > 0) {              // whole tiles in eight runs, then the parts
-            const int from = (int)((int64_t)p.whole * x / 8), count = (int)((int64_t)p.whole * (x + 1) / 8) - from;
-            const int pfrom = (int)((int64_t)(units - p.whole) * x / 8), pcount = (int)((int64_t)(units - p.whole) * (x + 1) / 8) - pfrom;
-            if (at >= count + pcount) return false;
-            n = at < count ? from + at : p.whole + pfrom + (at - count);
-        } else {
-            const int from = (int)((int64_t)units * x / 8), count = (int)((int64_t)units * (x + 1) / 8) - from;
-            if (at >= count) return false;
-            n = from + at;
-        }
+        const int n = unit_of_block(p, W && a.offsets, b);
+        if (n < 0) return false;
         t = n;
         if (n >= p.whole) {
             u.slot = n - p.whole;
@@ -571,9 +537,8 @@ hipError_t launch(moe_ctx* c, grad_args a, int64_t tiles, int stages) {
     const bool known = !a.offsets;
     a.cuts = known || (!W && tiles <= G_SLOTS);
     const split_plan p = known ? plan_of((int)tiles, stages) : split_plan{(int)tiles, 0, 1};
-    int64_t units = p.whole + (int64_t)p.cut * p.parts;
-    if (!known) units = W ? (tiles + 511) / 512 * 512 : a.cuts ? G_SLOTS : tiles;
-    grad_kernel<W, PLANES, F32><<<(unsigned)((units + 7) / 8 * 8 + 8), G_THREADS, G_LDS, c->stream>>>(a);
+    const int64_t units = known ? (int64_t)p.whole + (int64_t)p.cut * p.parts : a.cuts ? G_SLOTS : tiles;
+    grad_kernel<W, PLANES, F32><<<(unsigned)blocks_of(units, W && !known), G_THREADS, G_LDS, c->stream>>>(a);
     const int cut = known ? p.cut : a.cuts ? (int)(tiles < G_SLOTS / 2 ? tiles : G_SLOTS / 2) : 0;
     if (cut) grad_join_kernel<W, F32><<<(unsigned)(cut * 16), G_THREADS, 0, c->stream>>>(a);
     return hipGetLastError();

@@ -64,7 +64,8 @@ inline int type_bytes(int32_t t) { return t == MOE_BF16 ? 2 : 4; }
 bool linear_grad_ok(const moe_ctx* c, int64_t rows, int32_t NOUT, int32_t K, const int32_t* offsets, int32_t E) {
     if (!c || !c->grad_ws) return false;
     if (rows < 0 || rows >= ((int64_t)1 << 31) - 256 || NOUT <= 0 || K <= 0 || NOUT % QBLOCK || K % QBLOCK) return false;
-    if ((int64_t)NOUT * K >= (int64_t)1 << 32 || E < 1 || E > MAX_E || (!offsets && E != 1)) return false;
+    // (a lane's offset inside a tile of dy, of codes or of results: 127 rows of two bytes a column at most)
+    if (NOUT > 1 << 24 || K > 1 << 24 || (int64_t)NOUT * K >= (int64_t)1 << 32 || E < 1 || E > MAX_E || (!offsets && E != 1)) return false;
     // blocks of a launch
     return (rows / 128 + E) * (((int64_t)K + 255) / 256) < (int64_t)1 << 31 && (int64_t)E * (NOUT / 128) * (((int64_t)K + 255) / 256) < (int64_t)1 << 31;
 }

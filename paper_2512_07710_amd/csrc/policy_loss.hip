@@ -15,7 +15,7 @@ constexpr double LN2 = 0.69314718055994530942;
 
 struct loss_args {
     const void* logits;
-    int64_t ld, rows;
+    int64_t ld, rows, first;                   // (first: of a launch)
     int V;
     const int32_t* target;
     const float *old_logp, *ref_logp, *advantage, *weight, *clip_rows;
@@ -304,7 +304,7 @@ __global__ __launch_bounds__(LOSS_MAX_THREADS) void loss_kernel(const loss_args 
     __shared__ row_result s_row;
     __shared__ int32_t s_last;
     __shared__ double s_sum[LOSS_MAX_WAVES];
-    const int64_t r = blockIdx.x;
+    const int64_t r = a.first + blockIdx.x;
     const int tid = threadIdx.x, threads = blockDim.x;
     const void* const z = row_of<BF16>(a.logits, r * a.ld);
     const int vecs = a.V / N, rest = a.V % N;                  // thread t < rest has element t behind the vectors as well
@@ -470,14 +470,17 @@ int loss_parts(int64_t rows, int vecs, bool gradient) {
     return parts > MAX_PARTS ? MAX_PARTS : (int)parts;
 }
 
+constexpr int64_t LOSS_MAX_GRID = 1 << 21;     // blocks of a launch: a grid has fewer than 2^32 threads
+
 }  // namespace
 
 hipError_t launch_policy_loss(moe_ctx* c, const void* logits, int64_t ld, int32_t dtype, int64_t rows, int32_t V, const int32_t* target,
                               const float* old_logp, const float* ref_logp, const float* advantage, const float* weight,
                               const float* clip_rows, float clip_low, float clip_high, float kl_coef, float entropy_coef, float temperature,
                               float* logp, float* entropy, float* row_loss, float* loss, void* dlogits, int64_t ld_grad, int32_t grad_dtype) {
-    loss_args a{logits,     ld,      rows,     V,          target,       old_logp,           ref_logp, advantage, weight, clip_rows, clip_low,
-                      clip_high,  kl_coef, entropy_coef, 1.0f / temperature, logp, entropy, row_loss, loss,  dlogits,   ld_grad, c->grad_tickets};
+    loss_args a{logits,    ld,        rows,    0,            V,                  target, old_logp, ref_logp, advantage, weight,  clip_rows,
+                clip_low,  clip_high, kl_coef, entropy_coef, 1.0f / temperature, logp,   entropy,  row_loss, loss,      dlogits, ld_grad,
+                c->grad_tickets};
     if (rows == 0) return launch_fill_i32(c->stream, reinterpret_cast<int32_t*>(loss), 1, 0);
     const int vecs = V / (dtype == MOE_BF16 ? 8 : 4);
     const int parts = loss_parts(rows, vecs, dlogits != nullptr);
@@ -503,7 +506,8 @@ hipError_t launch_policy_loss(moe_ctx* c, const void* logits, int64_t ld, int32_
     if (threads < 64) threads = 64;
     if (held && threads * LOSS_HELD < vecs) threads += 64;
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(threads), 0, c->stream, a);
+        for (; a.first < rows; a.first += LOSS_MAX_GRID)
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(rows - a.first < LOSS_MAX_GRID ? rows - a.first : LOSS_MAX_GRID)), dim3(threads), 0, c->stream, a);
         if (rows > GRAD_MAX_SPLIT_ROWS) loss_total_kernel<<<1, LOSS_MAX_THREADS, 0, c->stream>>>(a);
         return hipGetLastError();
     };

@@ -11,7 +11,7 @@ from training_common import F32, HALF_ULP, TYPES, Context, f64, guarded, keep, r
 pytestmark = pytest.mark.gpu
 # T, d, E, k
 SHAPES = [(1, 128, 8, 2), (1, 7168, 256, 8), (3, 128, 1, 1), (64, 256, 8, 3), (33, 2176, 60, 5), (200, 1024, 40, 16), (129, 4096, 5, 4),
-          (17, 5120, 128, 7), (700, 384, 30, 6)]
+          (17, 5120, 128, 7), (700, 384, 30, 6), (1100, 640, 12, 3)]
 
 
 def _routing(T, E, k, seed, bad=True):
