@@ -222,8 +222,10 @@ def moe_combine(ctx, y_perm, inv_perm, topk_w, y, y_f32=None) -> None:
                                       _ptr(y_f32, torch.float32)), "moe_combine")
 
 
-# ---- the training side: sizes are taken from the tensors, and every tensor's type and shape is checked ---------------------------------
-_TYPES = {torch.bfloat16: 0, torch.float32: 1}
+# ---- the training side: sizes are taken from the tensors, and every tensor's type and shape is checked.  Short calls are bound by the
+# time on the host, and half of that is spent here: types as names of the module, shapes as ready tuples, no helper around the call
+_BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+_TYPES = {_BF16: 0, _F32: 1}
 
 
 def _type(t: torch.Tensor) -> int:
@@ -233,7 +235,7 @@ def _type(t: torch.Tensor) -> int:
     return code
 
 
-def _of(t: Optional[torch.Tensor], dtype, *shape) -> Optional[int]:
+def _of(t: Optional[torch.Tensor], dtype, shape: tuple) -> Optional[int]:
     """Address of a contiguous tensor of this type and shape; None for None."""
     if t is None:
         return None
@@ -242,15 +244,28 @@ def _of(t: Optional[torch.Tensor], dtype, *shape) -> Optional[int]:
     return t.data_ptr()
 
 
-def _rows_of(t: Optional[torch.Tensor], dtype, rows: int, cols: int):
-    """(address, row stride) of a 2-D tensor whose rows are contiguous."""
+def _flat(t: torch.Tensor, n: int) -> int:
+    """Address of a contiguous int32 tensor of n elements, of any shape."""
+    if t.numel() != n or t.dtype is not _I32 or not t.is_contiguous() or not t.is_cuda:
+        raise MoEError(f"expected a contiguous CUDA tensor of {n} elements of {_I32}, got {tuple(t.shape)} of {t.dtype}, strides {t.stride()}, on {t.device}")
+    return t.data_ptr()
+
+
+def _rows_of(t: Optional[torch.Tensor], dtype, shape: tuple):
+    """(address, row stride) of a 2-D tensor of this type and shape whose rows are contiguous."""
     if t is None:
         return None, 0
-    ld, unit = t.stride() if t.dim() == 2 else (0, 0)
-    if t.shape != (rows, cols) or t.dtype is not dtype or (unit != 1 and cols > 1) or not t.is_cuda:
-        raise MoEError(f"expected a CUDA tensor {(rows, cols)} of {dtype} with contiguous rows, got {tuple(t.shape)} of {t.dtype}, "
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or (t.stride(1) != 1 and shape[1] > 1):
+        raise MoEError(f"expected a CUDA tensor {shape} of {dtype} with contiguous rows, got {tuple(t.shape)} of {t.dtype}, "
                        f"strides {t.stride()}, on {t.device}")
-    return t.data_ptr(), ld if rows > 1 else max(cols, 1)
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else max(shape[1], 1)
+
+
+def _two(t: torch.Tensor) -> tuple:
+    shape = t.shape
+    if len(shape) != 2:
+        raise MoEError("expected a 2-D tensor")
+    return shape
 
 
 def moe_reserve_gradients(ctx) -> None:
@@ -260,101 +275,115 @@ def moe_reserve_gradients(ctx) -> None:
 
 def moe_add_rmsnorm(ctx, x, residual, gain, eps, sum=None, y=None, q=None, scales=None, rstd=None) -> None:
     """x, residual [rows, cols] (bf16 or f32, rows may be strided); every output given is written."""
-    if x.dim() != 2:
-        raise MoEError("expected a 2-D tensor")
-    rows, cols = x.shape
-    code, t, f = _type(x), x.dtype, torch.float32
-    px, ld_x = _rows_of(x, t, rows, cols)
-    pr, ld_r = _rows_of(residual, t, rows, cols)
-    _check(load_library().moe_add_rmsnorm(ctx, px, pr, _of(gain, f, cols), rows, cols, ld_x, ld_r, code, eps, _of(sum, t, rows, cols),
-                                          _of(y, t, rows, cols), _of(q, torch.uint8, rows, cols), _of(scales, f, cols // 128, rows),
-                                          _of(rstd, f, rows)), "moe_add_rmsnorm")
+    lib = _lib or load_library()
+    shape = rows, cols = _two(x)
+    code, t = _type(x), x.dtype
+    px, ld_x = _rows_of(x, t, shape)
+    pr, ld_r = _rows_of(residual, t, shape)
+    rc = lib.moe_add_rmsnorm(ctx, px, pr, _of(gain, _F32, (cols,)), rows, cols, ld_x, ld_r, code, eps, _of(sum, t, shape), _of(y, t, shape),
+                             _of(q, _U8, shape), _of(scales, _F32, (cols // 128, rows)), _of(rstd, _F32, (rows,)))
+    if rc:
+        _check(rc, "moe_add_rmsnorm")
 
 
 def moe_add_rmsnorm_backward(ctx, dy, h, rstd, gain, dh, dx, dgain) -> None:
-    if dy.dim() != 2:
-        raise MoEError("expected a 2-D tensor")
-    rows, cols = dy.shape
-    t, f = dy.dtype, torch.float32
-    _check(load_library().moe_add_rmsnorm_backward(ctx, _ptr(dy), _of(h, t, rows, cols), _of(rstd, f, rows), _of(gain, f, cols),
-                                                   _of(dh, t, rows, cols), rows, cols, _type(dy), _of(dx, t, rows, cols),
-                                                   _of(dgain, f, cols)), "moe_add_rmsnorm_backward")
+    lib = _lib or load_library()
+    shape = rows, cols = _two(dy)
+    code, t = _type(dy), dy.dtype
+    rc = lib.moe_add_rmsnorm_backward(ctx, _of(dy, t, shape), _of(h, t, shape), _of(rstd, _F32, (rows,)), _of(gain, _F32, (cols,)),
+                                      _of(dh, t, shape), rows, cols, code, _of(dx, t, shape), _of(dgain, _F32, (cols,)))
+    if rc:
+        _check(rc, "moe_add_rmsnorm_backward")
 
 
 def _shape_of(ctx):
-    if ctx not in _shapes:
+    shape = _shapes.get(ctx)
+    if shape is None:
         raise MoEError("not a context")
-    return _shapes[ctx]
+    return shape
 
 
 def moe_dispatch(ctx, x, inv_perm, x_perm) -> None:
+    lib = _lib or load_library()
     T, d, _, k = _shape_of(ctx)
-    t = x.dtype
-    _check(load_library().moe_dispatch(ctx, _of(x, t, T, d), _of(inv_perm.view(-1), torch.int32, T * k), _type(x), _of(x_perm, t, T * k, d)),
-           "moe_dispatch")
+    code, t = _type(x), x.dtype
+    rc = lib.moe_dispatch(ctx, _of(x, t, (T, d)), _flat(inv_perm, T * k), code, _of(x_perm, t, (T * k, d)))
+    if rc:
+        _check(rc, "moe_dispatch")
 
 
 def moe_dispatch_backward(ctx, dx_perm, inv_perm, dx_add, dx) -> None:
+    lib = _lib or load_library()
     T, d, _, k = _shape_of(ctx)
-    t = dx_perm.dtype
-    _check(load_library().moe_dispatch_backward(ctx, _of(dx_perm, t, T * k, d), _of(inv_perm.view(-1), torch.int32, T * k),
-                                                _of(dx_add, t, T, d), _type(dx_perm), _of(dx, t, T, d)), "moe_dispatch_backward")
+    code, t = _type(dx_perm), dx_perm.dtype
+    rc = lib.moe_dispatch_backward(ctx, _of(dx_perm, t, (T * k, d)), _flat(inv_perm, T * k), _of(dx_add, t, (T, d)), code, _of(dx, t, (T, d)))
+    if rc:
+        _check(rc, "moe_dispatch_backward")
 
 
 def moe_combine_backward(ctx, dy, y_perm, inv_perm, topk_w, topk_idx, dy_perm, dw, dlogits) -> None:
     """topk_idx and dlogits: both given or both None."""
+    lib = _lib or load_library()
     T, d, E, k = _shape_of(ctx)
-    t, f = dy.dtype, torch.float32
-    _check(load_library().moe_combine_backward(ctx, _of(dy, t, T, d), _of(y_perm, f, T * k, d), _of(inv_perm.view(-1), torch.int32, T * k),
-                                               _of(topk_w, f, T, k), _of(topk_idx, torch.int32, T, k), _type(dy), _of(dy_perm, t, T * k, d),
-                                               _of(dw, f, T, k), _of(dlogits, f, T, E)), "moe_combine_backward")
+    code, t, rows, slots = _type(dy), dy.dtype, (T * k, d), (T, k)
+    rc = lib.moe_combine_backward(ctx, _of(dy, t, (T, d)), _of(y_perm, _F32, rows), _flat(inv_perm, T * k), _of(topk_w, _F32, slots),
+                                  _of(topk_idx, _I32, slots), code, _of(dy_perm, t, rows), _of(dw, _F32, slots), _of(dlogits, _F32, (T, E)))
+    if rc:
+        _check(rc, "moe_combine_backward")
 
 
 def moe_policy_loss(ctx, logits, target, old_logp, ref_logp, advantage, weight, logp, entropy, row_loss, loss, dlogits=None, *,
                     clip_rows=None, clip_low=0.2, clip_high=0.2, kl_coef=0.0, entropy_coef=0.0, temperature=1.0) -> None:
     """logits [rows, V] (bf16 or f32, rows may be strided); dlogits None: forward only; it may be logits itself."""
-    if logits.dim() != 2:
-        raise MoEError("expected a 2-D tensor")
-    rows, V = logits.shape
-    f, code = torch.float32, _type(logits)
-    pz, ld = _rows_of(logits, logits.dtype, rows, V)
-    gcode = code if dlogits is None else _type(dlogits)
-    pg, ld_g = _rows_of(dlogits, dlogits.dtype if dlogits is not None else None, rows, V)
-    _check(load_library().moe_policy_loss(ctx, pz, ld, code, rows, V, _of(target, torch.int32, rows), _of(old_logp, f, rows),
-                                          _of(ref_logp, f, rows), _of(advantage, f, rows), _of(weight, f, rows), _of(clip_rows, f, rows),
-                                          clip_low, clip_high, kl_coef, entropy_coef, temperature, _of(logp, f, rows), _of(entropy, f, rows),
-                                          _of(row_loss, f, rows), _of(loss, f, 1), pg, ld_g, gcode), "moe_policy_loss")
+    lib = _lib or load_library()
+    shape = rows, V = _two(logits)
+    row = (rows,)
+    code = gcode = _type(logits)
+    pz, ld = _rows_of(logits, logits.dtype, shape)
+    pg, ld_g = None, 0
+    if dlogits is not None:
+        gcode = _type(dlogits)
+        pg, ld_g = _rows_of(dlogits, dlogits.dtype, shape)
+    rc = lib.moe_policy_loss(ctx, pz, ld, code, rows, V, _of(target, _I32, row), _of(old_logp, _F32, row), _of(ref_logp, _F32, row),
+                             _of(advantage, _F32, row), _of(weight, _F32, row), _of(clip_rows, _F32, row), clip_low, clip_high, kl_coef,
+                             entropy_coef, temperature, _of(logp, _F32, row), _of(entropy, _F32, row), _of(row_loss, _F32, row),
+                             _of(loss, _F32, (1,)), pg, ld_g, gcode)
+    if rc:
+        _check(rc, "moe_policy_loss")
 
 
 def _experts(offsets, matrices: torch.Tensor):
-    """(E, shape prefix) of a linear's matrices: dense without offsets, one per expert with them."""
+    """(E, NOUT, K, shape prefix) of a linear's matrices: dense without offsets, one per expert with them."""
+    shape = matrices.shape
     if offsets is None:
-        if matrices.dim() != 2:
+        if len(shape) != 2:
             raise MoEError("a dense linear has one matrix")
-        return 1, ()
-    if matrices.dim() != 3:
+        return 1, shape[0], shape[1], ()
+    if len(shape) != 3:
         raise MoEError("a grouped linear has a matrix per expert")
-    return matrices.shape[0], (matrices.shape[0],)
+    return shape[0], shape[1], shape[2], (shape[0],)
 
 
 def moe_linear_fp8_dgrad(ctx, dy, Wq, ws, offsets, dx) -> None:
     """dy [rows, NOUT] bf16; Wq [NOUT, K] (offsets None) or [E, NOUT, K]; dx [rows, K] bf16."""
-    E, pre = _experts(offsets, Wq)
-    NOUT, K = Wq.shape[-2:]
-    rows, b = dy.shape[0], torch.bfloat16
-    _check(load_library().moe_linear_fp8_dgrad(ctx, _of(dy, b, rows, NOUT), rows, NOUT, _ptr(Wq, torch.uint8),
-                                               _of(ws, torch.float32, *pre, NOUT // 128, K // 128), K, _of(offsets, torch.int32, E + 1), E,
-                                               _of(dx, b, rows, K)), "moe_linear_fp8_dgrad")
+    lib = _lib or load_library()
+    E, NOUT, K, pre = _experts(offsets, Wq)
+    rows = dy.shape[0]
+    rc = lib.moe_linear_fp8_dgrad(ctx, _of(dy, _BF16, (rows, NOUT)), rows, NOUT, _of(Wq, _U8, pre + (NOUT, K)),
+                                  _of(ws, _F32, pre + (NOUT // 128, K // 128)), K, _of(offsets, _I32, (E + 1,)), E, _of(dx, _BF16, (rows, K)))
+    if rc:
+        _check(rc, "moe_linear_fp8_dgrad")
 
 
 def moe_linear_fp8_wgrad(ctx, dy, xq, xs, offsets, dW, accumulate=False) -> None:
     """dy [rows, NOUT] bf16; xq [rows, K] u8 and xs [K/128, rows] as the forward pass read them; dW [NOUT, K] or [E, NOUT, K], bf16 or f32."""
-    E, _ = _experts(offsets, dW)
-    NOUT, K = dW.shape[-2:]
+    lib = _lib or load_library()
+    E, NOUT, K, pre = _experts(offsets, dW)
     rows = dy.shape[0]
-    _check(load_library().moe_linear_fp8_wgrad(ctx, _of(dy, torch.bfloat16, rows, NOUT), rows, NOUT, _of(xq, torch.uint8, rows, K),
-                                               _of(xs, torch.float32, K // 128, rows), K, _of(offsets, torch.int32, E + 1), E,
-                                               1 if accumulate else 0, _type(dW), _ptr(dW)), "moe_linear_fp8_wgrad")
+    rc = lib.moe_linear_fp8_wgrad(ctx, _of(dy, _BF16, (rows, NOUT)), rows, NOUT, _of(xq, _U8, (rows, K)), _of(xs, _F32, (K // 128, rows)), K,
+                                  _of(offsets, _I32, (E + 1,)), E, 1 if accumulate else 0, _type(dW), _of(dW, dW.dtype, pre + (NOUT, K)))
+    if rc:
+        _check(rc, "moe_linear_fp8_wgrad")
 
 
 def moe_balance_lengths(pred_len, n_groups: int, equal_count: bool = True):
