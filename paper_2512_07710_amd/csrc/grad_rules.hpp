@@ -12,20 +12,32 @@ constexpr int G_MIN_PART = 4;                  // stages of a part of a sum at l
 // works on at a time share their operands in its L2.  Tiles that do not fill a round of the chip are cut along the sum: parts
 // go to the workspace and a second launch adds them up.
 constexpr int G_SLOTS = 512, G_BAND = 8;       // blocks that run at a time
+constexpr int G_PART = 18;                     // parts that go through memory in the time of a stage
 struct split_plan {
     int whole, cut, parts;                     // tiles done at once; tiles in parts, and how many parts
 };
-__host__ __device__ inline split_plan plan_of(int tiles, int stages) {
-    split_plan p{tiles, 0, 1};
+// weight: time of a stage, in tenths of a bf16 one; fill: how much of the tiles' rows there is, in percent
+__host__ __device__ inline split_plan plan_of(int tiles, int stages, int weight, int fill) {
+    const split_plan none{tiles, 0, 1};
     const int rest = tiles % G_SLOTS;
-    if (rest == 0) return p;
-    int parts = G_SLOTS / rest;
-    if (parts > stages / G_MIN_PART) parts = stages / G_MIN_PART;
-    if (parts < (tiles < G_SLOTS ? 2 : 3)) return p;
-    // (in stages) what is saved against what the parts' way through memory costs
-    if (tiles >= G_SLOTS && stages * (0.55f - 1.0f / parts) < 24.f) return p;
-    return split_plan{tiles - rest, rest, parts};
+    if (rest == 0) return none;
+    const int most = G_SLOTS / rest < stages / G_MIN_PART ? G_SLOTS / rest : stages / G_MIN_PART;
+    if (tiles >= G_SLOTS) {                    // the rest of many: what is saved against what the parts' way through memory costs
+        if (most < 3 || stages * (0.55f - 1.0f / most) < 24.f) return none;
+        return split_plan{tiles - rest, rest, most};
+    }
+    // p parts take stages / p, and 4 for the second launch with 1 for every 18 full parts that go through memory: the best p is the last that
+    // p (p-1) rest / 18 <= stages holds for.  (Measured with 18 | 26 | 38 and with as many parts as fit, us: dgrad 200 x 6144 x 4096 31.4 | 34.8 | 33.8 |
+    // 34.3, 500 x 4096 x 4096 35.8 | 38.7 | 38.2 | 39.3, 8000 x 1024 x 1024 21.6 | 21.5 | 21.7 | 45; wgrad 700 x 2048 x 3584 17.5 | 17.5 | 17.5 | 38,
+    // 1000 x 2048 x 2048 22.6 | 22.6 | 22.6 | 35)
+    const int64_t sum = (int64_t)stages * weight * G_PART * 10;
+    int p = 1;
+    while (p < most && (int64_t)p * (p + 1) * rest * fill <= sum) ++p;
+    if (sum * (p - 1) < p * ((int64_t)400 * G_PART + (int64_t)rest * p * fill)) return none;
+    return split_plan{tiles - rest, rest, p};
 }
+
+inline __host__ __device__ int fill_of(int64_t rows, int row_tiles) { return row_tiles < 1 || rows >= (int64_t)row_tiles * GM ? 100 : (int)(rows * 100 / ((int64_t)row_tiles * GM)); }
 
 // The unit of block b, or -1.  Units 0 .. whole-1 are whole tiles, the others the cut ones' parts.  turns: runs of 64 units, taken in turns
 // (where sums differ in length); otherwise one run for each XCD.
@@ -41,6 +53,20 @@ __host__ __device__ inline int unit_of_block(const split_plan& p, bool turns, in
     if (at >= count + pcount) return -1;
     return at < count ? from + at : p.whole + pfrom + (at - count);
 }
+// Few rows (dgrad of one matrix): tiles of up to 64 rows and 64 or 128 columns, the sum cut into stages for the block's four waves and `parts` blocks.
+// us with 64 | 128 columns: 40 x 6144 x 4096 15.4 | 13.3, 48 x 25600 x 7168 66 | 47, 64 x 25600 x 7168 73 | 57, but 64 x 6144 x 5120 21.8 | 23.6,
+// 64 x 1024 x 1024 8.7 | 10.6, 10 x 3584 x 3584 9.7 | 10.4.  Against the tiles of 128 rows: 1 x 6144 x 4096 8.6 for 19.4, 65 x 6144 x 4096 16.2 for
+// 22.8, 128 x 2048 x 2048 10.4 for 16.2, 64 x 25600 x 7168 57 for 59, but 128 x 5120 x 5120 28.7 for 25.1.
+constexpr int GF_ROWS = 64, GF_WAVES = 4;
+inline int gf_cols(int rows, int NOUT, int K) { return (rows > 48 ? (int64_t)NOUT * K >= 1 << 26 : K >= 4096) ? 128 : 64; }
+inline bool few_rows(int64_t rows, int NOUT, int K) { return rows <= GF_ROWS || (rows <= 2 * GF_ROWS && rows * NOUT * K <= (int64_t)1 << 31); }
+// (rows: of a tile; row_tiles: of them)
+inline int gf_parts(int rows, int row_tiles, int NOUT, int K) {
+    const int cols = gf_cols(rows, NOUT, K), blocks = rows > 32 || cols == 128 ? 512 : 768;    // (those that run at a time)
+    const int room = blocks / (K / cols * row_tiles), most = NOUT / GK / GF_WAVES, parts = room < most ? room : most;
+    return parts < 1 ? 1 : parts;
+}
+
 // blocks of a launch that reach every one of up to `units` units
 inline int64_t blocks_of(int64_t units, bool turns) { return turns ? (units + 511) / 512 * 512 : (units + 7) / 8 * 8 + 8; }
 

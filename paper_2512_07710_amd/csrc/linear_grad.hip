@@ -40,6 +40,7 @@ struct grad_args {
     int64_t rows;
     int E, NOUT, K;
     int accumulate;
+    int weight;                                // of a stage, for plan_of
     int cuts;                                  // whether tiles may be cut along the sum
     void* out;
     float* parts;                              // [units][rows / 32][2][4][256] f32x4: a thread's sums, in its own order
@@ -61,14 +62,14 @@ __device__ inline void segment(const grad_args& a, int e, int& lo, int& hi) {
 struct find_scratch {
     int waves[G_THREADS / 64], found[4];
 };
-struct unit {
+struct unit_place {
     int e, lo, hi;                             // expert and its rows
     int row0, c0;                              // first row and column of the tile
     int part, parts, slot;                     // part of the sum; its place in the workspace
 };
 // The unit of block b; JOIN: of the launch that adds up, a tile that was cut.  False: none.  Called by the whole block.
 template <bool W, bool JOIN = false>
-__device__ inline bool unit_of(const grad_args& a, int b, find_scratch& s, unit& u) {
+__device__ inline bool unit_of(const grad_args& a, int b, find_scratch& s, unit_place& u) {
     const int ctiles = (a.K + GN - 1) / GN, tid = threadIdx.x;
     int row_tiles = W ? a.E * (a.NOUT / GM) : (int)((a.rows + GM - 1) / GM);
     int first = 0, tiles = 0, l = 0, h = 0;    // (grouped dgrad) thread e: expert e's row tiles
@@ -90,7 +91,7 @@ __device__ inline bool unit_of(const grad_args& a, int b, find_scratch& s, unit&
         }
     }
     const int total = row_tiles * ctiles;
-    const split_plan p = !a.cuts ? split_plan{total, 0, 1} : plan_of(total, W ? (int)((a.rows + GK - 1) / GK) : a.NOUT / GK);
+    const split_plan p = !a.cuts ? split_plan{total, 0, 1} : plan_of(total, W ? (int)((a.rows + GK - 1) / GK) : a.NOUT / GK, a.weight, W ? 100 : fill_of(a.rows, row_tiles));
     int t;
     u.part = 0;
     u.parts = 1;
@@ -192,13 +193,30 @@ __device__ inline v8bf codes_bf16(v2i c, float pow2) {
     return v8bf{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
 }
 
+// (dgrad) Sums are held in units of the present block's scale without its power of two, which the codes carry: a factor of less than two either way
+// from block to block, whatever the scales are.
+struct block_scale {
+    float scale = 1.f, pow2 = 1.f;
+    int mask = -1;                             // on the codes
+    __device__ float next(float s) {           // the factor on the sums
+        const uint32_t exponent = __float_as_uint(s) & 0x7F800000u;
+        const bool live = exponent != 0, finite = exponent != 0x7F800000u;
+        mask = live ? -1 : 0;                  // a zero scale (or one below the normal range): the block adds nothing
+        const float to = !live ? scale : finite ? __uint_as_float((__float_as_uint(s) & 0x807FFFFFu) | 0x3F800000u) : s;
+        pow2 = live && finite ? __uint_as_float(exponent) : 1.f;
+        const float ratio = scale / to;
+        scale = to;
+        return ratio;
+    }
+};
+
 // W: the weights' gradient; PLANES: bf16 planes of its scaled operand; F32: type of the result
 template <bool W, int PLANES, bool F32>
 __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];   // (the places of chunks are exchanged inside 256 bytes)
     __shared__ find_scratch s_find;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    unit u;
+    unit_place u;
     if (!unit_of<W>(a, blockIdx.x, s_find, u)) return;
     const int e = u.e, lo = u.lo, hi = u.hi, row0 = u.row0, c0 = u.c0;
     // this block's stages of the sum: all, or a part
@@ -306,30 +324,16 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
             d[i] = *(lds_v8s_ptr)(uintptr_t)(dy_at[g] + at + i * 2048);
         }
     };
-    // (dgrad) acc is held in units of the present block's scale without its power of two, which the codes carry: a factor of less than
-    // two either way from block to block, whatever the scales are.  (In the constant address space, so that they come as scalar loads:
-    // a vector load's wait would include the copies)
+    // (In the constant address space, so that they come as scalar loads: a vector load's wait would include the copies)
     const __attribute__((address_space(4))) float* const block_scales = (const __attribute__((address_space(4))) float*)(uintptr_t)(
         a.scales + (size_t)e * (a.NOUT / QBLOCK) * (a.K / QBLOCK) + min(cols0, a.K - 1) / QBLOCK);
-    float unit_scale = 1.f, pow2 = 1.f;
-    int block_mask = -1;
-    auto next_block = [&](int kb) {            // the factor on acc
-        const float s = block_scales[(size_t)(kb / 2) * (a.K / QBLOCK)];
-        const uint32_t exponent = __float_as_uint(s) & 0x7F800000u;
-        const bool live = exponent != 0, finite = exponent != 0x7F800000u;
-        block_mask = live ? -1 : 0;            // a zero scale (or one below the normal range): the block adds nothing
-        const float to = !live ? unit_scale : finite ? __uint_as_float((__float_as_uint(s) & 0x807FFFFFu) | 0x3F800000u) : s;
-        pow2 = live && finite ? __uint_as_float(exponent) : 1.f;
-        const float ratio = unit_scale / to;
-        unit_scale = to;
-        return ratio;
-    };
+    block_scale unit;                          // (dgrad) of acc
     // A quarter of the codes of 16 columns: two steps of the sum.  (The empty asm keeps the instructions where they are asked for; they would
     // be moved down to where the operand is used)
     auto convert = [&](u32x4 (&o)[PLANES], const v2i& codes_, const v4f (&scale)[2], int h) {
         if (!W) {
-            const int w = codes_[h >> 1] & block_mask;
-            const v2bf x = h & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, pow2, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, pow2, false);
+            const int w = codes_[h >> 1] & unit.mask;
+            const v2bf x = h & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, unit.pow2, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, unit.pow2, false);
             uint32_t r = __builtin_bit_cast(uint32_t, x);
             asm volatile("" : "+v"(r));
             o[0][h] = r;
@@ -402,6 +406,7 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
             asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
         }
         if (W) clear_behind(k0);
+        auto next_block = [&](int kb) { return unit.next(block_scales[(size_t)(kb / 2) * (a.K / QBLOCK)]); };
         float ratio = W ? 1.f : next_block(k0);
         fetch_codes(0, 0);
 #pragma unroll
@@ -446,7 +451,7 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
 #pragma unroll
                 for (int n = 0; n < 8; ++n) {
                     const v4f r = acc[i * 2 + (n >> 2)][n & 3];
-                    __builtin_nontemporal_store(W ? r : r * unit_scale, reinterpret_cast<f32x4*>(out + (i * 8 + n) * G_THREADS * sizeof(f32x4) + (uint32_t)lane * 16));
+                    __builtin_nontemporal_store(W ? r : r * unit.scale, reinterpret_cast<f32x4*>(out + (i * 8 + n) * G_THREADS * sizeof(f32x4) + (uint32_t)lane * 16));
                 }
         return;
     }
@@ -462,7 +467,7 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             v4f r = acc[i][j];
-            if (!W) r *= unit_scale;
+            if (!W) r *= unit.scale;
             if (F32) {
                 f32x4* const p = reinterpret_cast<f32x4*>(base + j * 64 + own);
                 if (a.accumulate) r += *p;
@@ -495,7 +500,7 @@ __global__ __launch_bounds__(G_THREADS) void grad_join_kernel(const grad_args a)
     __shared__ __attribute__((aligned(16))) f32x4 s_sums[WAVES - 1][8][64];
     __shared__ __attribute__((aligned(16))) float s_out[32 * OUT_LD];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = blockIdx.x >> 2 & 3, column = blockIdx.x & 3;
-    unit u;
+    unit_place u;
     if (!unit_of<W, true>(a, blockIdx.x >> 4, s_find, u)) return;
     const int cols0 = u.c0 + column * 64, row = u.row0 + i * 32, end = W ? a.NOUT : u.hi;
     if (cols0 >= a.K || row >= end) return;
@@ -517,6 +522,114 @@ __global__ __launch_bounds__(G_THREADS) void grad_join_kernel(const grad_args a)
     store_rows<F32>(a, s_out, r, (W ? (size_t)u.e * a.NOUT * a.K : 0) + (size_t)row * a.K + cols0, end - row);
 }
 
+// dgrad of few rows of one matrix, where all that counts is that the codes come at the rate of the memory.  A tile is up to 64 rows and 64 or 128
+// columns; each wave of a block has a part of the sum of its own, two or three stages of which it asks for at a time (no barriers), and the waves' sums
+// meet in LDS: a fourth of the parts that would go through memory otherwise.  1 x 6144 x 4096 8.6 us (25 MB of codes: 5.2 at a copy's rate, the rest is
+// the second launch, which adds the parts up), 40 rows 13.3, 16 x 25600 x 7168 37.9 us = 4.84 TB/s.
+template <int RT, int JT>                      // rows and columns in tiles of 16
+__global__ __launch_bounds__(GF_WAVES * 64, RT < 3 && JT == 4 ? 3 : 2) void few_dgrad_kernel(const grad_args a, int parts, int tile_rows, int row_tiles) {
+    constexpr int COLS = JT * 16, BATCH = JT == 4 ? 3 : 2, STAGE = GK * COLS;
+    constexpr int SUMS = RT * 16 * 64 * 4, EACH = SUMS > BATCH * STAGE ? SUMS : BATCH * STAGE;
+    __shared__ __attribute__((aligned(1024))) char lds[GF_WAVES * EACH];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r4 = lane >> 4, c16 = lane & 15;
+    const int tiles = a.K / COLS * row_tiles, units = tiles * parts, x = blockIdx.x & 7, at = blockIdx.x >> 3;
+    const int from = (int)((int64_t)units * x / 8), n = from + at;         // (an XCD has neighbouring columns)
+    if (n >= (int)((int64_t)units * (x + 1) / 8)) return;
+    const int part = n / tiles, c0 = n % tiles / row_tiles * COLS, row0 = n % row_tiles * tile_rows, rows = min((int)a.rows - row0, tile_rows);
+    const int stages = a.NOUT / GK, own = part * GF_WAVES + wave, all = parts * GF_WAVES;
+    const int k0 = (int)((int64_t)stages * own / all), nk = (int)((int64_t)stages * (own + 1) / all);
+    char* const mine = lds + wave * EACH;
+    const uint32_t mine0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine;
+    // the 16-byte chunks of a row change places by the row's number over 256 / COLS: a transposing read meets each bank as often as the others
+    constexpr int AT_ONCE = 1024 / COLS;       // rows that a copy brings
+    const int chunk = JT == 4 ? (lane & 3) ^ r4 : (lane & 7) ^ r4;         // (JT == 8: and ^ 4 in every other copy)
+    const uint32_t row_off = (uint32_t)(lane / JT) * (uint32_t)a.K;
+    const uint32_t code_at = mine0 + (r4 * 8 + (c16 >> 1)) * COLS + (lane & 1) * 8;
+    const int swap = JT == 4 ? (r4 * 2 + (c16 >> 3)) & 3 : (r4 * 4 + (c16 >> 2)) & 7;
+    const uint16_t* dy_row[RT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) dy_row[i] = a.dy + (size_t)(row0 + min(i * 16 + c16, rows - 1)) * a.NOUT + r4 * 8;
+    const __attribute__((address_space(4))) float* const block_scales =
+        (const __attribute__((address_space(4))) float*)(uintptr_t)(a.scales + c0 / QBLOCK);
+    v4f acc[RT][JT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int j = 0; j < JT; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    block_scale unit;
+    for (int kb = k0; kb < nk; kb += BATCH) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the batch before has been read
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b)
+            if (kb + b < nk)
+#pragma unroll
+                for (int i = 0; i < GK / AT_ONCE; ++i)
+                    dma16(mine0 + b * STAGE + i * 1024, row_off + (JT == 8 && i & 1 ? chunk ^ 4 : chunk) * 16,
+                          a.codes + (size_t)((kb + b) * GK + i * AT_ONCE) * a.K + c0);
+        v8s d[BATCH][2][RT];
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b)
+            if (kb + b < nk)
+#pragma unroll
+                for (int g = 0; g < 2; ++g)
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) d[b][g][i] = *reinterpret_cast<const v8s*>(dy_row[i] + (size_t)(kb + b) * GK + g * 32);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) {
+            if (kb + b >= nk) continue;
+            const float ratio = unit.next(block_scales[(size_t)((kb + b) / 2) * (a.K / QBLOCK)]);
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int j = 0; j < JT; ++j) acc[i][j] *= ratio;
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int j = 0; j < JT; ++j) {
+                    v2i q = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i_ptr)(uintptr_t)(code_at + b * STAGE + g * 32 * COLS + ((j ^ swap) << 4)));
+                    q[0] &= unit.mask;
+                    q[1] &= unit.mask;
+                    const v8bf c = codes_bf16(q, unit.pow2);
+#pragma unroll
+                    for (int i = 0; i < RT; ++i)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c, __builtin_bit_cast(v8bf, d[b][g][i]), acc[i][j], 0, 0, 0);
+                }
+        }
+    }
+    f32x4* const sums = reinterpret_cast<f32x4*>(lds);         // [wave][row tile][column tile][lane] of 64 columns
+#pragma unroll
+    for (int h = 0; h < JT; h += 4) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sums[((wave * RT + i) * 4 + j) * 64 + lane] = acc[i][h + j] * unit.scale;
+        __syncthreads();
+        for (int i = 0; i < RT; ++i) {         // wave w: column tile w
+            f32x4 r = sums[(i * 4 + wave) * 64 + lane];
+#pragma unroll
+            for (int w = 1; w < GF_WAVES; ++w) r += sums[((w * RT + i) * 4 + wave) * 64 + lane];
+            const int row = i * 16 + c16;
+            if (row >= rows) continue;
+            const size_t o = (size_t)(row0 + row) * a.K + c0 + (h + wave) * 16 + r4 * 4;
+            if (parts > 1) __builtin_nontemporal_store(r, reinterpret_cast<f32x4*>(a.parts + (size_t)part * a.rows * a.K + o));
+            else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + o) = u32x2{bf16_pair(r[0], r[1]), bf16_pair(r[2], r[3])};
+        }
+    }
+}
+
+// Adds up the parts, in their order; a thread has four columns
+__global__ __launch_bounds__(G_THREADS) void few_join_kernel(const grad_args a, int parts) {
+    const size_t n = (size_t)a.rows * a.K / 4, i = (size_t)blockIdx.x * G_THREADS + threadIdx.x;
+    if (i >= n) return;
+    const f32x4* const in = reinterpret_cast<const f32x4*>(a.parts) + i;
+    f32x4 r = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int p = 0; p < parts; ++p) r += __builtin_nontemporal_load(in + p * n);
+    reinterpret_cast<u32x2*>(a.out)[i] = u32x2{bf16_pair(r[0], r[1]), bf16_pair(r[2], r[3])};
+}
+
 }  // namespace
 
 hipError_t set_grad_lds_limits() {
@@ -527,6 +640,7 @@ hipError_t set_grad_lds_limits() {
 
 namespace {
 
+static_assert((size_t)512 * GF_ROWS * 128 * sizeof(float) <= GRAD_WS_BYTES, "the parts of few rows fit the workspace");
 static_assert((size_t)G_SLOTS * GM * GN * sizeof(float) <= GRAD_WS_BYTES, "the parts of a round fit the workspace");
 
 // tiles: as many as there can be; stages: of a whole sum
@@ -536,7 +650,7 @@ hipError_t launch(moe_ctx* c, grad_args a, int64_t tiles, int stages) {
     // costs 5 us whether there is something to add up or not), and in the weights' gradient, where sums differ in length, not at all
     const bool known = !a.offsets;
     a.cuts = known || (!W && tiles <= G_SLOTS);
-    const split_plan p = known ? plan_of((int)tiles, stages) : split_plan{(int)tiles, 0, 1};
+    const split_plan p = known ? plan_of((int)tiles, stages, a.weight, W ? 100 : fill_of(a.rows, (int)((a.rows + GM - 1) / GM))) : split_plan{(int)tiles, 0, 1};
     const int64_t units = known ? (int64_t)p.whole + (int64_t)p.cut * p.parts : a.cuts ? G_SLOTS : tiles;
     grad_kernel<W, PLANES, F32><<<(unsigned)blocks_of(units, W && !known), G_THREADS, G_LDS, c->stream>>>(a);
     const int cut = known ? p.cut : a.cuts ? (int)(tiles < G_SLOTS / 2 ? tiles : G_SLOTS / 2) : 0;
@@ -548,13 +662,22 @@ hipError_t launch(moe_ctx* c, grad_args a, int64_t tiles, int stages) {
 
 hipError_t launch_linear_dgrad(moe_ctx* c, const uint16_t* dy, int64_t rows, int32_t NOUT, const uint8_t* Wq, const float* ws, int32_t K,
                                const int32_t* offsets, int32_t E, uint16_t* dx) {
-    const grad_args a{dy, Wq, ws, offsets, rows, E, NOUT, K, 0, 0, dx, static_cast<float*>(c->grad_ws)};
+    const grad_args a{dy, Wq, ws, offsets, rows, E, NOUT, K, 0, 10, 0, dx, static_cast<float*>(c->grad_ws)};
+    if (!offsets && few_rows(rows, NOUT, K)) {
+        const int row_tiles = ((int)rows + GF_ROWS - 1) / GF_ROWS, rt = (((int)rows + row_tiles - 1) / row_tiles + 15) / 16;
+        const int cols = gf_cols(rt * 16, NOUT, K), parts = gf_parts(rt * 16, row_tiles, NOUT, K);
+        const auto kernel = cols == 64 ? (rt == 1 ? few_dgrad_kernel<1, 4> : rt == 2 ? few_dgrad_kernel<2, 4> : rt == 3 ? few_dgrad_kernel<3, 4> : few_dgrad_kernel<4, 4>)
+                                       : (rt == 1 ? few_dgrad_kernel<1, 8> : rt == 2 ? few_dgrad_kernel<2, 8> : rt == 3 ? few_dgrad_kernel<3, 8> : few_dgrad_kernel<4, 8>);
+        kernel<<<(unsigned)((K / cols * row_tiles * parts + 7) / 8 * 8), GF_WAVES * 64, 0, c->stream>>>(a, parts, rt * 16, row_tiles);
+        if (parts > 1) few_join_kernel<<<(unsigned)((rows * K / 4 + G_THREADS - 1) / G_THREADS), G_THREADS, 0, c->stream>>>(a, parts);
+        return hipGetLastError();
+    }
     return launch<false, 1, false>(c, a, (offsets ? rows / GM + E : (rows + GM - 1) / GM) * ((K + GN - 1) / GN), NOUT / GK);
 }
 
 hipError_t launch_linear_wgrad(moe_ctx* c, const uint16_t* dy, int64_t rows, int32_t NOUT, const uint8_t* xq, const float* xs, int32_t K,
                                const int32_t* offsets, int32_t E, int32_t accumulate, int32_t dtype, void* dW) {
-    const grad_args a{dy, xq, xs, offsets, rows, E, NOUT, K, accumulate, 0, dW, static_cast<float*>(c->grad_ws)};
+    const grad_args a{dy, xq, xs, offsets, rows, E, NOUT, K, accumulate, dtype == MOE_BF16 ? 10 : 25, 0, dW, static_cast<float*>(c->grad_ws)};
     const int64_t tiles = (int64_t)E * (NOUT / GM) * ((K + GN - 1) / GN);
     const int stages = (int)((rows + GK - 1) / GK);
     return dtype == MOE_BF16 ? launch<true, 1, false>(c, a, tiles, stages) : launch<true, 3, true>(c, a, tiles, stages);

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from training_common import F32, Context, randn
+from training_common import F32, HALF_ULP, Context, randn
 
 pytestmark = pytest.mark.gpu
 MANY = 2 ** 26 + 5                                             # times 64 threads: past 2^32
@@ -52,3 +52,28 @@ def test_matrices_too_wide_for_a_tile(gpu_lib):
         for NOUT, K in [(wide, 128), (128, wide)]:
             assert lib.moe_linear_fp8_dgrad(ctx, p, 1, NOUT, p, p, K, None, 1, p) == -1
             assert lib.moe_linear_fp8_wgrad(ctx, p, 1, NOUT, p, p, K, None, 1, 0, 0, p) == -1
+
+
+@pytest.mark.parametrize("rows,NOUT,K", [(1, 128, 4096), (7, 640, 4224), (30, 1024, 4096), (45, 384, 6144), (64, 16384, 4096), (33, 2048, 640),
+                                         (16, 192 * 128, 128), (48, 256, 3968), (90, 896, 1152), (128, 2048, 1024), (113, 128, 4096), (200, 4096, 512)])
+def test_dgrad_of_few_rows(gpu_lib, rows, NOUT, K):
+    """The forms for few rows: 64 and 128 columns, one to four tiles of rows, sums in one part and in many."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    dy = torch.randn((rows, NOUT), generator=g, device="cuda").bfloat16()
+    Wq = torch.randint(0, 256, (NOUT, K), generator=g, device="cuda", dtype=torch.int32).to(torch.uint8)
+    Wq[(Wq & 127) == 127] = 0                                  # (NaN)
+    ws = torch.exp2(torch.randint(-20, 20, (NOUT // 128, K // 128), generator=g, device="cuda").float()) * (
+        1 + torch.rand((NOUT // 128, K // 128), generator=g, device="cuda"))
+    ws[0, 0] = 0
+    whole = torch.full((rows + 2, K), 37.0, dtype=torch.bfloat16, device="cuda")
+    again = torch.empty((rows, K), dtype=torch.bfloat16, device="cuda")
+    with Context(gpu_lib) as ctx:
+        gpu_lib.moe_linear_fp8_dgrad(ctx, dy, Wq, ws, None, whole[1:-1])
+        gpu_lib.moe_linear_fp8_dgrad(ctx, dy, Wq, ws, None, again)
+    assert (whole[0] == 37).all() and (whole[-1] == 37).all() and torch.equal(whole[1:-1], again)
+    W = Wq.view(torch.float8_e4m3fn).double().view(NOUT // 128, 128, K // 128, 128) * ws.double()[:, None, :, None]
+    W = W.view(NOUT, K)
+    exact, size = dy.double() @ W, dy.double().abs() @ W.abs()
+    # fp32 sums of exact products in chains of at most NOUT / 32 matrix instructions, a rescaling each 64, and the result's own rounding
+    bound = (NOUT / 16 + 64) * F32 * size + HALF_ULP["bf16"] * 1.01 * exact.abs()
+    assert ((again.double() - exact).abs() <= bound).all()

@@ -18,7 +18,7 @@ using namespace moe355;
 int main() {
     int cut, turns, room, tiles, stages;                       // room: units that the launch is made for
     while (scanf("%d %d %d %d %d", &cut, &turns, &room, &tiles, &stages) == 5) {
-        const split_plan p = cut ? plan_of(tiles, stages) : split_plan{tiles, 0, 1};
+        const split_plan p = cut ? plan_of(tiles, stages, stages % 2 ? 25 : 10, stages % 3 ? 100 : stages % 7 * 15) : split_plan{tiles, 0, 1};
         const int units = p.whole + p.cut * p.parts;
         std::vector<char> seen(units);
         int bad = p.whole + p.cut != tiles || p.parts < 1, idle = 0;
