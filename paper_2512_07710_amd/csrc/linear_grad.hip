@@ -367,11 +367,11 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
     // Part P of a group's products: all rows, columns 16 NJ P and on.  Between them, piece by piece, what comes behind needs: the codes of the next
     // part are converted, those of the next group (at `at`, group G) come from LDS in the first part, and in the last dy of the next group takes
     // the place of what has been used.  The compiler would gather these and wait for them.
-    auto part = [&](auto P_, uint32_t at, auto G_) {
-        constexpr int P = decltype(P_)::value, G = decltype(G_)::value, NP = (P + 1) % PARTS, NG = P + 1 < PARTS ? 1 - G : G;
+    auto part = [&](auto I_, auto P_, uint32_t at, auto G_) {
+        constexpr int I = decltype(I_)::value, P = decltype(P_)::value, G = decltype(G_)::value, NP = (P + 1) % PARTS, NG = P + 1 < PARTS ? 1 - G : G;
         if (P == 0) fetch_codes(at, G);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < I; ++i) {
 #pragma unroll
             for (int p = 0; p < PLANES; ++p)
 #pragma unroll
@@ -382,22 +382,25 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
                 }
             __builtin_amdgcn_sched_barrier(0);
             if (P == PARTS - 1) fetch_dy(at, G, i);
-            if (NJ == 2 || i % 2 == 0) convert(c[NP & 1][NJ == 2 ? i >> 2 : 0], q[NG][NP * NJ + (NJ == 2 ? i >> 2 : 0)], sc[NG], NJ == 2 ? i & 3 : i / 2);
+#pragma unroll
+            for (int n = i * 8 / I; n < (i + 1) * 8 / I; ++n)
+                if (NJ == 2 || n % 2 == 0) convert(c[NP & 1][NJ == 2 ? n >> 2 : 0], q[NG][NP * NJ + (NJ == 2 ? n >> 2 : 0)], sc[NG], NJ == 2 ? n & 3 : n / 2);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto group = [&](uint32_t at, auto G_) {
-        part(step<0>{}, at, G_);
-        part(step<1>{}, at, G_);
+    auto group = [&](auto I_, uint32_t at, auto G_) {
+        part(I_, step<0>{}, at, G_);
+        part(I_, step<1>{}, at, G_);
         if (PARTS > 2) {
-            part(step<(PARTS > 2 ? 2 : 0)>{}, at, G_);
-            part(step<(PARTS > 2 ? 3 : 1)>{}, at, G_);
+            part(I_, step<(PARTS > 2 ? 2 : 0)>{}, at, G_);
+            part(I_, step<(PARTS > 2 ? 3 : 1)>{}, at, G_);
         }
     };
 
     // ---- the sum.  The barrier that hands over the stages stands between the two groups of a stage: the second's operands have been
     // read by then, and those of the next stage come during its products
-    if (nk > k0) {
+    auto sum = [&](auto I_) {
+        constexpr int I = decltype(I_)::value;
         copy(k0);
         if (nk > k0 + 1) {
             copy(k0 + 1);
@@ -410,7 +413,7 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
         float ratio = W ? 1.f : next_block(k0);
         fetch_codes(0, 0);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) fetch_dy(0, 0, i);
+        for (int i = 0; i < I; ++i) fetch_dy(0, 0, i);
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
@@ -419,25 +422,30 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
             const uint32_t at = (uint32_t)((kb - k0) & 1) * G_STAGE;
             if (!W && (kb & 1) == 0) {         // of a block of scales the first stage
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
+                for (int i = 0; i < I; ++i)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) acc[i][j] *= ratio;
             }
-            group(at, step<1>{});
+            group(I_, at, step<1>{});
             if (kb + 1 < nk) {
                 asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // stage kb+1 is there, and this one has been read
                 if (kb + 2 < nk) copy(kb + 2);
                 if (W) clear_behind(kb + 1);
             }
             // (behind the last stage what is fetched is of no use, and not used)
-            part(step<0>{}, G_STAGE - at, step<0>{});
+            part(I_, step<0>{}, G_STAGE - at, step<0>{});
             if (!W && (kb & 1) && kb + 1 < nk) ratio = next_block(kb + 1);
-            part(step<1>{}, G_STAGE - at, step<0>{});
+            part(I_, step<1>{}, G_STAGE - at, step<0>{});
             if (PARTS > 2) {
-                part(step<(PARTS > 2 ? 2 : 0)>{}, G_STAGE - at, step<0>{});
-                part(step<(PARTS > 2 ? 3 : 1)>{}, G_STAGE - at, step<0>{});
+                part(I_, step<(PARTS > 2 ? 2 : 0)>{}, G_STAGE - at, step<0>{});
+                part(I_, step<(PARTS > 2 ? 3 : 1)>{}, G_STAGE - at, step<0>{});
             }
         }
+    };
+    // (an expert's last tile: half the products where it has half the rows)
+    if (nk > k0) {
+        if (!W && hi - row0 <= GM / 2) sum(step<W ? 8 : 4>{});
+        else sum(step<8>{});
     }
 
     // ---- the result: a lane holds rows lane%16 of its tiles of 16 x 16, four neighbouring columns of each
