@@ -9,9 +9,11 @@ constexpr int GK = 64;                         // steps of the sum that are stag
 constexpr int G_MIN_PART = 4;                  // stages of a part of a sum at least
 
 // Tiles are dealt to the XCDs (blockIdx % 8) in runs, and run through a band of eight tile rows column by column, so that the 64 tiles that an XCD
-// works on at a time share their operands in its L2.  Tiles that do not fill a round of the chip are cut along the sum: parts
-// go to the workspace and a second launch adds them up.
-constexpr int G_SLOTS = 512, G_BAND = 8;       // blocks that run at a time
+// works on at a time share their operands in its L2 (dgrad 8192 x 8192 x 8192 with bands of 4 | 8 | 16: 858 | 851 | 870 us, experts 32768 x 5120 x 1536
+// zipf 587 | 598 | 624, 2600 x 8192 x 8192 304 | 308 | 314; wgrad 4096 x 32768 x 5120 1199 | 1182 | 1205).  Tiles that do not fill a round
+// of the chip are cut along the sum: parts go to the workspace and a second launch adds them up.
+constexpr int G_SLOTS = 512;                   // blocks that run at a time
+constexpr int G_BAND = 8, G_RUN = 16;
 constexpr int G_PART = 18;                     // parts that go through memory in the time of a stage
 struct split_plan {
     int whole, cut, parts;                     // tiles done at once; tiles in parts, and how many parts
@@ -22,7 +24,9 @@ __host__ __device__ inline split_plan plan_of(int tiles, int stages, int weight,
     const int rest = tiles % G_SLOTS;
     if (rest == 0) return none;
     const int most = G_SLOTS / rest < stages / G_MIN_PART ? G_SLOTS / rest : stages / G_MIN_PART;
-    if (tiles >= G_SLOTS) {                    // the rest of many: what is saved against what the parts' way through memory costs
+    // the rest of many: what is saved against what the parts' way through memory costs (dgrad 4096 x 32768 x 5120 not cut 1324 us, cut 1160; 4096 x
+    // 8192 x 5120 325, 295; 2600 x 8192 x 8192 341, 305; but 4096 x 2048 x 5120 85.8, 96.2 and 4096 x 4096 x 5120 166, 163)
+    if (tiles >= G_SLOTS) {
         if (most < 3 || stages * (0.55f - 1.0f / most) < 24.f) return none;
         return split_plan{tiles - rest, rest, most};
     }
@@ -37,14 +41,19 @@ __host__ __device__ inline split_plan plan_of(int tiles, int stages, int weight,
     return split_plan{tiles - rest, rest, p};
 }
 
-inline __host__ __device__ int fill_of(int64_t rows, int row_tiles) { return row_tiles < 1 || rows >= (int64_t)row_tiles * GM ? 100 : (int)(rows * 100 / ((int64_t)row_tiles * GM)); }
+__host__ __device__ inline int fill_of(int64_t rows, int row_tiles) {
+    const int64_t room = (int64_t)row_tiles * GM;
+    return rows >= room ? 100 : (int)(rows * 100 / room);
+}
 
-// The unit of block b, or -1.  Units 0 .. whole-1 are whole tiles, the others the cut ones' parts.  turns: runs of 64 units, taken in turns
-// (where sums differ in length); otherwise one run for each XCD.
+// The unit of block b, or -1.  Units 0 .. whole-1 are whole tiles, the others the cut ones' parts.  turns: runs of 16 units, taken in turns (experts'
+// weights' gradients: sums differ in length, and an expert's tiles go to several XCDs); otherwise one run for each XCD.  Runs of 64 | 32 | 16 | 8,
+// us: 16384 rows, 64 experts of 2048 x 1024, zipf 164 | 121 | 107 | 110, 32768, 128 of 5120 x 1536, zipf 868 | 796 | 804 | 820, uniform 809 | 833 |
+// 830 | 847, 32768, 32 of 4096 x 4096 1163 | 1134 | 1144 | 1147.
 __host__ __device__ inline int unit_of_block(const split_plan& p, bool turns, int b) {
     const int units = p.whole + p.cut * p.parts, x = b & 7, at = b >> 3;
     if (turns) {
-        const int n = (at / 64 * 8 + x) * 64 + at % 64;
+        const int n = (at / G_RUN * 8 + x) * G_RUN + at % G_RUN;
         return n < units ? n : -1;
     }
     // whole tiles in eight runs, then the parts
@@ -68,6 +77,6 @@ inline int gf_parts(int rows, int row_tiles, int NOUT, int K) {
 }
 
 // blocks of a launch that reach every one of up to `units` units
-inline int64_t blocks_of(int64_t units, bool turns) { return turns ? (units + 511) / 512 * 512 : (units + 7) / 8 * 8 + 8; }
+inline int64_t blocks_of(int64_t units, bool turns) { return turns ? (units + 8 * G_RUN - 1) / (8 * G_RUN) * (8 * G_RUN) : (units + 7) / 8 * 8 + 8; }
 
 }  // namespace moe355
