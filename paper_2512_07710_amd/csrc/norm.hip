@@ -23,7 +23,7 @@ struct norm_args {
 // h = x + residual (rounded to its type), r = 1 / sqrt(mean h^2 + eps), y = h r gain, q = e4m3(y / s) with s = max|y| / 448 of 128 columns.
 // Rows in vectors of eight elements and what is left over, one to a thread; `per_block` neighbouring rows to a block, each in registers while the
 // next is on its way, so that a row is read once and its results leave as it is done: bound by those bytes.  32768 x 7168 bf16 with residual, sum and
-// codes 326 us = 5.0 TB/s (a copy: 4.87); one row of 7168 8 us, which is the call.  Thread t of a block of n holds vectors t, t+n, ...; sixteen
+// codes 326 us = 5.1 TB/s (a copy: 4.87); one row of 4096 4.2 us, 8 with the call.  Thread t of a block of n holds vectors t, t+n, ...; sixteen
 // neighbouring threads hold a group of 128 columns.  Scales leave in runs of NORM_ROWS words: as single words each would be a part of a cache line
 // of its own.
 template <bool BF16, int NV, bool REST>         // REST: cols is no multiple of eight (an instance of its own, it takes registers)
@@ -149,8 +149,10 @@ struct norm_back_args {
     float* partial;                            // [gridDim.x][cols]: each block's part of dgain
 };
 
+// dx = u - h r^2 (u . h) / cols + dh with u = r gain dy; dgain = sum over rows of dy h r.
 // Rows of block b: b, b + gridDim.x, ..., each requested while the one before is worked on; a thread keeps its columns' part of dgain in registers
-// over all of them.
+// over all of them.  Bound by the bytes of dy, h, dh and dx, each once: 4096 x 5120 bf16 34.2 us = 4.9 TB/s, and 5.6 for the blocks' parts of dgain, which
+// leave them as one row a block (a fixed order of the sums, no atomics).
 template <bool BF16, int NV, int THREADS, bool REST>
 __global__ __launch_bounds__(THREADS) void norm_back_kernel(const norm_back_args a) {
     __shared__ float lds[2][16];

@@ -294,6 +294,9 @@ struct row_grad {
     __device__ void put_one(float v, int i) const { store1<GRAD_BF16>(out, i, f.live ? of(v) + (target == i ? f.target : 0.f) : 0.f); }
 };
 
+// dz[v] = (dlogp (1[v = target] - p_v) + w entropy_coef p_v (log p_v + H)) / temperature, which is 2^y (a y + b) for numbers a, b of the row.
+// Bound by the bytes: logits once, gradients once; 4096 x 131072 bf16 456 us = 4.7 TB/s (a copy: 4.87), with the row read twice 1390.  333 x 50001 f32
+// 30.9 us where a copy takes 20.5: a row is one CU's, and 77 of the rows have a second round.
 // One block per row.  HELD: the row stays in registers between the two passes that its maximum and its sum ask for and the pass
 // that writes its gradient, so it is read once; otherwise it is read again for the gradient.
 template <bool BF16, bool GRAD_BF16, bool HELD>
