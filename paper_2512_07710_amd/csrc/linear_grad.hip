@@ -474,32 +474,46 @@ __global__ __launch_bounds__(G_THREADS, 2) void grad_kernel(const grad_args a) {
                 }
         return;
     }
-    // bf16 goes through LDS, a wave's own part of it, to be stored as whole lines of 128 bytes, past the caches (1 to 4 % faster at all sizes tried);
-    // fp32 has 64 bytes of a row in four lanes as it is, which the caches put together (past them 40 x 6144 x 4096 26 -> 33 us)
+    // bf16 goes through LDS, a wave's own part of it, to be stored as whole lines of 128 bytes, past the caches (1 to 4 % faster at all sizes tried).
+    // fp32 has 64 bytes of a row of each column tile in four lanes; rows and column tiles change places by pairs of lanes for whole lines, which go past the
+    // caches too (8000 rows on 32 experts of 2048 x 4096, zipf 491 -> 469 us, 200 x 4096 x 2048 22.8 -> 21.5, 40 x 6144 x 4096 level; the 64 bytes alone
+    // past the caches 26 -> 33)
     constexpr int BYTES = F32 ? 4 : 2;
     char* const out_lds = lds + 2 * G_STAGE + wave * OUT_BYTES;
     char* base = static_cast<char*>(a.out) + ((W ? (size_t)e * mat : 0) + (size_t)row0 * a.K + cols0) * BYTES;
-    const uint32_t own = (c16 * (uint32_t)a.K + r4 * 4) * BYTES, line = (r8 * (uint32_t)a.K + (lane & 7) * 8) * BYTES;
+    const uint32_t own = F32 ? ((c16 & 7) * (uint32_t)a.K + (c16 >> 3) * 16 + r4 * 4) * BYTES : (c16 * (uint32_t)a.K + r4 * 4) * BYTES, line = (r8 * (uint32_t)a.K + (lane & 7) * 8) * BYTES;
 #pragma unroll
     for (int i = 0; i < 8; ++i, base += (size_t)16 * a.K * BYTES) {
         if (i * 16 >= rows) break;
+        if (F32) {
+#pragma unroll
+            for (int j = 0; j < 4; j += 2) {
+                const bool high = c16 >= 8;
+                v4f there = high ? acc[i][j] : acc[i][j + 1];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) there[n] = __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(there[n]), 0x128, 0xf, 0xf, false));
+                v4f up = high ? there : acc[i][j], down = high ? acc[i][j + 1] : there;
+                f32x4* const p = reinterpret_cast<f32x4*>(base + j * 64 + own);
+                f32x4* const q = reinterpret_cast<f32x4*>(base + (size_t)8 * a.K * BYTES + j * 64 + own);
+                if (a.accumulate) {
+                    up += *p;
+                    down += *q;
+                }
+                __builtin_nontemporal_store(up, p);
+                __builtin_nontemporal_store(down, q);
+            }
+            continue;
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             v4f r = acc[i][j];
             if (!W) r *= unit.scale;
-            if (F32) {
-                f32x4* const p = reinterpret_cast<f32x4*>(base + j * 64 + own);
-                if (a.accumulate) r += *p;
-                *p = r;
-                continue;
-            }
             if (W && a.accumulate) {
                 const u32x2 was = *reinterpret_cast<const u32x2*>(base + j * 32 + own);
                 r += v4f{bf16lo(was[0]), bf16hi(was[0]), bf16lo(was[1]), bf16hi(was[1])};
             }
             *reinterpret_cast<u32x2*>(out_lds + c16 * OUT_PITCH + j * 32 + r4 * 8) = u32x2{bf16_pair(r[0], r[1]), bf16_pair(r[2], r[3])};
         }
-        if (F32) continue;
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
