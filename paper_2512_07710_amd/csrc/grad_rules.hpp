@@ -64,15 +64,15 @@ __host__ __device__ inline int unit_of_block(const split_plan& p, bool turns, in
 }
 // Few rows (dgrad of one matrix): tiles of up to 64 rows and 64 or 128 columns, the sum cut into stages for the block's four waves and `parts` blocks.
 // us with 64 | 128 columns: 40 x 6144 x 4096 15.4 | 13.3, 48 x 25600 x 7168 66 | 47, 64 x 25600 x 7168 73 | 57, but 64 x 6144 x 5120 21.8 | 23.6,
-// 64 x 1024 x 1024 8.7 | 10.6, 10 x 3584 x 3584 9.7 | 10.4.  Against the tiles of 128 rows: 1 x 6144 x 4096 8.6 for 19.4, 65 x 6144 x 4096 16.2 for
+// 64 x 1024 x 1024 8.7 | 10.6, 10 x 3584 x 3584 8.0 | 10.4.  Against the tiles of 128 rows: 1 x 6144 x 4096 8.6 for 19.4, 65 x 6144 x 4096 16.2 for
 // 22.8, 128 x 2048 x 2048 10.4 for 16.2, 64 x 25600 x 7168 57 for 59, but 128 x 5120 x 5120 28.7 for 25.1.
 constexpr int GF_ROWS = 64, GF_WAVES = 4;
 inline int gf_cols(int rows, int NOUT, int K) { return (rows > 48 ? (int64_t)NOUT * K >= 1 << 26 : K >= 4096) ? 128 : 64; }
 inline bool few_rows(int64_t rows, int NOUT, int K) { return rows <= GF_ROWS || (rows <= 2 * GF_ROWS && rows * NOUT * K <= (int64_t)1 << 31); }
-// (rows: of a tile; row_tiles: of them)
+// (rows: of a tile; row_tiles: of them.  Two blocks to a CU, also where three fit: 768 | 512 blocks at most, 10 x 3584 x 3584 9.8 | 8.0 us, 5 x 20480 x
+// 1024 11.1 | 10.0, 30 x 2048 x 1024 8.0 | 7.9; 512 | 384, 40 x 6144 x 4096 13.3 | 14.7)
 inline int gf_parts(int rows, int row_tiles, int NOUT, int K) {
-    const int cols = gf_cols(rows, NOUT, K), blocks = rows > 32 || cols == 128 ? 512 : 768;    // (those that run at a time)
-    const int room = blocks / (K / cols * row_tiles), most = NOUT / GK / GF_WAVES, parts = room < most ? room : most;
+    const int room = G_SLOTS / (K / gf_cols(rows, NOUT, K) * row_tiles), most = NOUT / GK / GF_WAVES, parts = room < most ? room : most;
     return parts < 1 ? 1 : parts;
 }
 

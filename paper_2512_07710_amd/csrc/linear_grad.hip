@@ -560,7 +560,7 @@ __global__ __launch_bounds__(G_THREADS) void grad_join_kernel(const grad_args a)
 // meet in LDS: a fourth of the parts that would go through memory otherwise.  1 x 6144 x 4096 8.6 us (25 MB of codes: 5.2 at a copy's rate, the rest is
 // the second launch, which adds the parts up), 40 rows 13.3, 16 x 25600 x 7168 37.9 us = 4.84 TB/s.
 template <int RT, int JT>                      // rows and columns in tiles of 16
-__global__ __launch_bounds__(GF_WAVES * 64, RT < 3 && JT == 4 ? 3 : 2) void few_dgrad_kernel(const grad_args a, int parts, int tile_rows, int row_tiles) {
+__global__ __launch_bounds__(GF_WAVES * 64, 2) void few_dgrad_kernel(const grad_args a, int parts, int tile_rows, int row_tiles) {
     constexpr int COLS = JT * 16, BATCH = JT == 4 ? 3 : 2, STAGE = GK * COLS;
     constexpr int SUMS = RT * 16 * 64 * 4, EACH = SUMS > BATCH * STAGE ? SUMS : BATCH * STAGE;
     __shared__ __attribute__((aligned(1024))) char lds[GF_WAVES * EACH];
