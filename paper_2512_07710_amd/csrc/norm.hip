@@ -34,7 +34,7 @@ __global__ __launch_bounds__(NORM_MAX_THREADS) void norm_kernel(const norm_args 
     const int rest = REST ? a.cols & 7 : 0, last = vecs * 8 + tid;        // thread t < rest has column `last` as well
     const int64_t r0 = (int64_t)blockIdx.x * per_block;
     const int rows = (int)(a.rows - r0 < per_block ? a.rows - r0 : per_block);
-    raw8<BF16> x[NV], res[NV];
+    raw8<BF16, REST && NV < 4> x[NV], res[NV];
     float x1 = 0.f, res1 = 0.f;
     auto request = [&](int64_t r) {
 #pragma unroll
