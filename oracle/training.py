@@ -10,6 +10,7 @@ import numpy as np
 from . import fp_formats as ff
 
 BLOCK = 128
+MASKED = -1e30                                                  # logits up to it are masked
 
 
 def add_rmsnorm(x, residual, gain, eps, keep):
@@ -72,13 +73,12 @@ def policy_loss(logits, target, old_logp, ref_logp, advantage, weight, low, high
     low, high = np.broadcast_to(low, rows), np.broadcast_to(high, rows)
     logp, entropy, row_loss, grad = np.zeros(rows), np.zeros(rows), np.zeros(rows), np.zeros((rows, V))
     for t in range(rows):
-        z = logits[t] / temperature
-        known, m = 0 <= target[t] < V, z.max()
-        if m == -np.inf:
+        known, m = 0 <= target[t] < V, logits[t].max()
+        if m <= MASKED:
             logp[t] = -np.inf if known else 0.0
             continue
-        lse = m + np.log(np.exp(z - m).sum())
-        ls = z - lse
+        z = np.where(logits[t] > MASKED, (logits[t] - m) / temperature, -np.inf)               # (the maximum first: large logits differ by little)
+        ls = z - np.log(np.exp(z).sum())
         p = np.exp(ls)
         plogp = np.zeros(V)
         plogp[p > 0] = p[p > 0] * ls[p > 0]

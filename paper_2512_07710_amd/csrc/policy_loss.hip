@@ -9,7 +9,8 @@ namespace {
 constexpr int LOSS_MAX_THREADS = 1024, LOSS_MAX_WAVES = LOSS_MAX_THREADS / 64;
 constexpr int PART_THREADS = 256, MAX_PARTS = 64;   // rows in parts: a block's threads, parts of a row at most
 constexpr int LOSS_HELD = 16;                  // vectors of 16 bytes of a row that a thread holds in registers
-constexpr float LOWEST = -1e30f;               // logits not above it are masked; and in place of -inf in y it makes 2^y y = 0
+constexpr float LOWEST = -1e30f;               // logits not above it are masked
+constexpr float Y_LOWEST = -256.f;             // 2^y is zero from there on; in place of any y below (-inf among them) it makes 2^y y and 2^y (a y + b) zero
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr double LN2 = 0.69314718055994530942;
 
@@ -30,15 +31,16 @@ struct loss_args {
     struct row_result* results;                // [rows]
 };
 
-// Sums over logits in units of log 2, y = z log2 e - m: s = sum 2^y, u = sum y 2^y, which log-sum-exp and entropy are made of.  m is the whole
-// number next to the largest z log2 e: so y is one fused multiply-add of the logit, rounded once, and sums over different m are
-// brought together by exact powers of two.  m = -inf: nothing but masked logits so far (or NaN, which the sums hold)
+// Sums over logits v in units of log 2, y = (v - m) c with c = log2 e / temperature: s = sum 2^y, u = sum y 2^y, which log-sum-exp and entropy are
+// made of.  m is the largest logit as it is, and comes off before the factor: the roundings of c and of the product are then relative to a distance
+// from the maximum, where the softmax is decided, however large the logits themselves are (v c - m c would carry half a unit of the last place of
+// v c into the exponent).  m = -inf: nothing but masked logits so far (or NaN, which the sums hold)
 struct softmax_stats {
     float m, s, u;
 };
-__device__ inline void rebase(softmax_stats& t, float to) {
+__device__ inline void rebase(softmax_stats& t, float to, float c) {
     if (t.m == to) return;
-    const float d = fmaxf(t.m - to, LOWEST), f = __builtin_amdgcn_exp2f(d);
+    const float d = fmaxf((t.m - to) * c, Y_LOWEST), f = __builtin_amdgcn_exp2f(d);
     t.u = f * fmaf(t.s, d, t.u);
     t.s *= f;
     t.m = to;
@@ -73,9 +75,9 @@ __device__ inline softmax_stats block_sums(softmax_stats t, block_scratch& lds) 
     return t;
 }
 // the same for sums over different m
-__device__ inline softmax_stats block_join(softmax_stats t, block_scratch& lds) {
+__device__ inline softmax_stats block_join(softmax_stats t, float c, block_scratch& lds) {
     const float m = block_largest(t.m, lds);
-    if (m > -INFINITY) rebase(t, m);           // (otherwise there is nothing but masked logits, or NaN, which the sums hold)
+    if (m > -INFINITY) rebase(t, m, c);        // (otherwise there is nothing but masked logits, or NaN, which the sums hold)
     return block_sums(t, lds);
 }
 
@@ -111,17 +113,17 @@ struct row_result {
 
 struct row_inputs {
     int target;
-    double z_target;
+    float v_target;
     float old_logp, ref_logp, A, w, low, high;
 };
 template <bool BF16>
 __device__ inline row_inputs inputs_of(const loss_args& a, int64_t r) {
     row_inputs n;
     n.target = a.target[r];
-    n.z_target = 0.0;
+    n.v_target = 0.f;
     if (n.target >= 0 && n.target < a.V) {
-        const float v = load1<BF16>(row_of<BF16>(a.logits, r * a.ld), n.target);
-        n.z_target = v <= LOWEST ? -INFINITY : (double)v * (double)a.inv_temp;
+        n.v_target = load1<BF16>(row_of<BF16>(a.logits, r * a.ld), n.target);
+        if (n.v_target <= LOWEST) n.v_target = -INFINITY;
     }
     n.old_logp = a.old_logp[r];
     n.ref_logp = a.ref_logp ? a.ref_logp[r] : 0.f;
@@ -161,7 +163,7 @@ __device__ inline row_result finish_row(const loss_args& a, int64_t r, const sof
     const double log_s = st.s > 0.f && st.s < INFINITY ? log2_of(st.s) * LN2 : (double)logf(st.s);
     const float mean = st.u / st.s;            // (of y: a rounding of H at most)
     const double H = empty ? 0.0 : log_s - (double)mean * LN2;
-    const double logp = !known ? 0.0 : empty ? -INFINITY : n.z_target - (double)st.m * LN2 - log_s;
+    const double logp = !known ? 0.0 : empty ? -INFINITY : ((double)n.v_target - (double)st.m) * (double)a.inv_temp - log_s;
     const bool live = known && !empty && n.w != 0.f;
     double loss = 0.0, slope = 0.0;
     if (live) {
@@ -226,17 +228,15 @@ struct running_sums {
     softmax_stats st{-INFINITY, 0.f, 0.f};
     const float c;                             // log2 e / temperature
     __device__ explicit running_sums(float c_) : c(c_) {}
-    __device__ float whole(float v) const { return v > LOWEST ? rintf(v * c) : -INFINITY; }
     __device__ void take(float top) {          // before logits up to `top` are added
-        const float m = whole(top);
-        if (m > st.m) rebase(st, m);
+        if (top > LOWEST && top > st.m) rebase(st, top, c);
     }
-    __device__ void one(float v, float base) { // base = -m
-        const float y = fmaf(v, c, base), e = __builtin_amdgcn_exp2f(y);
+    __device__ void one(float v, float m) {
+        const float y = (v - m) * c, e = __builtin_amdgcn_exp2f(y);
         st.s += e;
-        st.u = fmaf(e, fmaxf(y, LOWEST), st.u);
+        st.u = fmaf(e, fmaxf(y, Y_LOWEST), st.u);
     }
-    __device__ float base() const { return st.m > -INFINITY ? -st.m : 0.f; }
+    __device__ float base() const { return st.m > -INFINITY ? st.m : 0.f; }    // (0: all are masked, 2^y = 0)
     template <int M>
     __device__ static float largest(const u32x4 (&v)[M]) {
         float top = -INFINITY;
@@ -276,8 +276,8 @@ struct row_grad {
     __device__ row_grad(const loss_args& a, int64_t r, const row_result& f_, int target_)
         : f(f_), out(row_of<GRAD_BF16>(a.dlogits, r * a.ld_grad)), c(a.inv_temp * LOG2E), target(target_), at(target_ / N) {}
     __device__ float of(float v) const {
-        const float y = fmaf(v, c, -f.m);
-        return __builtin_amdgcn_exp2f(y) * fmaf(f.a, fmaxf(y, LOWEST), f.b);
+        const float y = (v - f.m) * c;
+        return __builtin_amdgcn_exp2f(y) * fmaf(f.a, fmaxf(y, Y_LOWEST), f.b);
     }
     __device__ void put(const u32x4& v, int i) const {
         float g[N] = {};
@@ -343,7 +343,7 @@ __global__ __launch_bounds__(LOSS_MAX_THREADS) void loss_kernel(const loss_args 
             sums.add(v);
         }
         if (tid < rest) sums.add_one(extra);
-        st = block_join(sums.st, s_scratch);
+        st = block_join(sums.st, sums.c, s_scratch);
     }
     if (tid == 0) {
         s_row = finish_row(a, r, st, in);
@@ -414,7 +414,7 @@ __global__ __launch_bounds__(PART_THREADS) void loss_part_kernel(const loss_args
         sums.add(v);
     }
     if (part == 0 && tid < a.V % N) sums.add_one(load1<BF16>(z, vecs * N + tid));
-    softmax_stats st = block_join(sums.st, s_scratch);
+    softmax_stats st = block_join(sums.st, sums.c, s_scratch);
     float* const mine = a.part_sums + (r * a.parts + part) * 3;
     if (tid == 0) {
         __hip_atomic_store(mine, st.m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -430,7 +430,7 @@ __global__ __launch_bounds__(PART_THREADS) void loss_part_kernel(const loss_args
                                __hip_atomic_load(all + tid * 3 + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
                                __hip_atomic_load(all + tid * 3 + 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)};
         const float m = wave_largest(st.m);
-        if (m > -INFINITY) rebase(st, m);
+        if (m > -INFINITY) rebase(st, m, c);
         st = softmax_stats{m, wave_total(st.s), wave_total(st.u)};
     }
     if (tid == 0) {
