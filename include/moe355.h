@@ -276,7 +276,7 @@ int moe_combine_backward(moe_ctx* ctx, const void* dy, const float* y_perm, cons
  * Logits of -inf, and all not above -1e30 (a type's lowest value as a mask), are masked: p = 0 and no gradient.  The others may be of any size at
  * any temperature: errors go by a logit's distance from the row's largest, and logits that a constant shifts exactly give the same bits.
  * Without effect on the loss (row_loss 0, gradient row zero) is a row with weight 0,
- * with a target outside [0,V) (its logp is written as 0), or whose logits are all masked (logp -inf, entropy 0).
+ * with a target outside [0,V) (its logp is written as 0), with a masked target (logp -inf), or whose logits are all masked (logp -inf, entropy 0).
  * V >= 1, temperature in [1e-6, 1e6], clip bounds and coefficients finite and >= 0. */
 int moe_policy_loss(moe_ctx* ctx, const void* logits, int64_t ld, int32_t dtype, int64_t rows, int32_t V,
                     const int32_t* target, const float* old_logp, const float* ref_logp, const float* advantage,

@@ -86,7 +86,7 @@ def policy_loss(logits, target, old_logp, ref_logp, advantage, weight, low, high
         if not known:
             continue
         lp = logp[t] = ls[target[t]]
-        if weight[t] == 0:
+        if weight[t] == 0 or lp == -np.inf:                    # (a masked target has no effect)
             continue
         A, loss, slope = advantage[t], 0.0, 0.0
         if A != 0:

@@ -164,7 +164,9 @@ __device__ inline row_result finish_row(const loss_args& a, int64_t r, const sof
     const float mean = st.u / st.s;            // (of y: a rounding of H at most)
     const double H = empty ? 0.0 : log_s - (double)mean * LN2;
     const double logp = !known ? 0.0 : empty ? -INFINITY : ((double)n.v_target - (double)st.m) * (double)a.inv_temp - log_s;
-    const bool live = known && !empty && n.w != 0.f;
+    // (a masked target: the ratio is zero and the KL term infinite, with gradients that are 0 * inf.  Nothing can be learnt from a token that the policy
+    // excludes)
+    const bool live = known && !empty && n.w != 0.f && n.v_target != -INFINITY;
     double loss = 0.0, slope = 0.0;
     if (live) {
         const double A = n.A;

@@ -17,3 +17,13 @@ def test_shifted_and_large_rows():
         assert np.allclose(logp, -np.log(40)) and np.allclose(H, np.log(40))
     logp, H, loss, g = tr.policy_loss(np.full((5, 40), -3e38), *arg)                           # a mask, not a size
     assert (logp == -np.inf).all() and (H == 0).all() and (loss == 0).all() and (g == 0).all()
+
+
+def test_masked_target_has_no_effect():
+    rng = np.random.default_rng(2)
+    z = rng.normal(size=(4, 30))
+    z[0, 3], z[1, 3] = -np.inf, -3e38
+    old, ref, A = (rng.normal(size=4) - 3 for _ in range(3))
+    logp, H, loss, g = tr.policy_loss(z, np.full(4, 3), old, ref, A, np.ones(4), 0.2, 0.2, 0.1, 0.01, 0.5)
+    assert (logp[:2] == -np.inf).all() and (loss[:2] == 0).all() and (g[:2] == 0).all() and (H > 0).all()
+    assert np.isfinite(logp[2:]).all() and (loss[2:] != 0).all() and np.isfinite(g).all()
