@@ -147,13 +147,18 @@ __device__ inline double log2_of(float x) {
     const float rest = fmaf(ldexpf(x, -(int)whole), __builtin_amdgcn_exp2f(-part), -1.f);
     return (double)l + (double)rest * (1.0 / LN2);
 }
-// e^x - 1 - x
-__device__ inline double exp_above_line(double x) {
-    if (!(x > -0.5 && x < 0.5)) return exp2_of(x * (1.0 / LN2)) - 1.0 - x;
+// e^x - 1 and, in `above`, e^x - 1 - x
+__device__ inline double exp_minus_one(double x, double& above) {
+    if (!(x > -0.5 && x < 0.5)) {
+        const double e = exp2_of(x * (1.0 / LN2)) - 1.0;
+        above = e - x;                         // (x = -inf: the slope e stays -1 where the term is infinite)
+        return e;
+    }
     const float t = (float)x;
     float p = 1.f / 362880.f;
     for (const float c : {1.f / 40320.f, 1.f / 5040.f, 1.f / 720.f, 1.f / 120.f, 1.f / 24.f, 1.f / 6.f, 0.5f}) p = fmaf(p, t, c);
-    return (double)p * x * x;
+    above = (double)p * x * x;
+    return above + x;
 }
 
 // One thread.  Sums and products in fp64: a loss near zero is the difference of terms that are not
@@ -178,9 +183,10 @@ __device__ inline row_result finish_row(const loss_args& a, int64_t r, const sof
             if (free != free) loss = slope = free;             // NaN is not lost in the comparisons
         }
         if (a.ref_logp && a.kl_coef != 0.f) {
-            const double x = (double)n.ref_logp - logp, e = exp_above_line(x);
-            loss += (double)a.kl_coef * e;
-            slope -= (double)a.kl_coef * (e + x);
+            double above;
+            const double e = exp_minus_one((double)n.ref_logp - logp, above);
+            loss += (double)a.kl_coef * above;
+            slope -= (double)a.kl_coef * e;
         }
         loss = (double)n.w * (loss - (double)a.entropy_coef * H);
         slope *= (double)n.w;
