@@ -10,7 +10,11 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 __device__ inline float bf16lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ inline float bf16hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-__device__ inline float clamp448(float v) { return fminf(fmaxf(v, -448.f), 448.f); }
+template <bool KEEP_NAN = false>
+__device__ inline float clamp448(float v) {
+    if (KEEP_NAN) return __builtin_elementwise_minimum(__builtin_elementwise_maximum(v, -448.f), 448.f);
+    return fminf(fmaxf(v, -448.f), 448.f);
+}
 
 // largest magnitude of 8 bf16 values (a NaN does not count)
 __device__ inline float bf16x8_amax(const u32x4& u) {
@@ -44,14 +48,16 @@ struct E4m3Coder {
     __device__ float quotient(float v) const { return corrected_quotient(v, s, inv); }
     // four codes, a in the low byte.  |v| <= amax, so the quotient is at most 448 up to one rounding, which the conversion
     // rounds back; the lower bound stays because it is what makes a NaN -448.
+    // KEEP_NAN: for a scale that is NaN or infinite where a value is, the codes are those of the quotients: NaN or zero.
+    template <bool KEEP_NAN = false>
     __device__ uint32_t pack4(float a, float b, float c, float d) const {
         int p = 0;
         if (mid_range) {
             p = __builtin_amdgcn_cvt_pk_fp8_f32(fmaxf(quotient(a), -448.f), fmaxf(quotient(b), -448.f), p, false);
             p = __builtin_amdgcn_cvt_pk_fp8_f32(fmaxf(quotient(c), -448.f), fmaxf(quotient(d), -448.f), p, true);
         } else {
-            p = __builtin_amdgcn_cvt_pk_fp8_f32(clamp448(a / s), clamp448(b / s), p, false);
-            p = __builtin_amdgcn_cvt_pk_fp8_f32(clamp448(c / s), clamp448(d / s), p, true);
+            p = __builtin_amdgcn_cvt_pk_fp8_f32(clamp448<KEEP_NAN>(a / s), clamp448<KEEP_NAN>(b / s), p, false);
+            p = __builtin_amdgcn_cvt_pk_fp8_f32(clamp448<KEEP_NAN>(c / s), clamp448<KEEP_NAN>(d / s), p, true);
         }
         return (uint32_t)p;
     }

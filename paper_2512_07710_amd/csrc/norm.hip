@@ -90,15 +90,15 @@ __global__ __launch_bounds__(NORM_MAX_THREADS) void norm_kernel(const norm_args 
             for (int j = 0; j < 8; ++j) y.v[j] = h[n].v[j] * inv * g.v[j];
             if (a.y) store8_any<BF16>(row_of<BF16>(a.y, r * a.cols), (int64_t)i * 8, y);
             if (a.q) {
-                float amax = 0.f;
+                float amax = 0.f;              // (NaN stays NaN)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf(y.v[j]));
+                for (int j = 0; j < 8; ++j) amax = __builtin_elementwise_maximum(amax, fabsf(y.v[j]));
 #pragma unroll
-                for (int o = 1; o < 16; o <<= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
+                for (int o = 1; o < 16; o <<= 1) amax = __builtin_elementwise_maximum(amax, __shfl_xor(amax, o));
                 const E4m3Coder coder(amax == 0.f ? 1.0f : amax / 448.0f);
                 u32x2 c;
-                c[0] = coder.pack4(y.v[0], y.v[1], y.v[2], y.v[3]);
-                c[1] = coder.pack4(y.v[4], y.v[5], y.v[6], y.v[7]);
+                c[0] = coder.pack4<true>(y.v[0], y.v[1], y.v[2], y.v[3]);
+                c[1] = coder.pack4<true>(y.v[4], y.v[5], y.v[6], y.v[7]);
                 __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(a.q + r * a.cols + (int64_t)i * 8));
                 if ((tid & 15) == 0) {
                     if (per_block == 1) a.scales[(int64_t)(i >> 4) * a.rows + r] = coder.s;
