@@ -33,6 +33,12 @@ __host__ __device__ inline float corrected_quotient(float v, float s, float inv)
     return fmaf(-fmaf(q0, s, -v), inv, q0);
 }
 
+// For any fp32 v and s the same holds of the codes: the quotient is the division's wherever the refined reciprocal is the nearest fp32 number to 1/s, which
+// with an estimate up to 2 ulp off is so for all but some thirty significands of s; for those it misses by an ulp at two values of v, which moves a code
+// in one case: s of nothing but ones, below, where 2^j / s is a little more than a power of two and may be a tie
+// (tests/test_quotient_fp32_host.py goes through them all).
+__host__ __device__ inline bool significand_all_ones(float s) { return (__builtin_bit_cast(uint32_t, s) & 0x7FFFFFu) == 0x7FFFFFu; }
+
 // Codes of 8 bf16 values over the group's scale s = amax/448 (1 for an all-zero group).
 // A true division is some ten instructions and made the quantisation kernels bound by the vector ALU (weights: 4.4 TB/s,
 // against 5.8 with this form).  In the stated range of s no remainder of a quotient that can reach a non-zero code underflows;
@@ -41,9 +47,10 @@ constexpr float SCALE_MID_MIN = 1e-25f, SCALE_MID_MAX = 1e25f;
 struct E4m3Coder {
     float s, inv;
     bool mid_range;
-    __device__ explicit E4m3Coder(float scale) : s(scale) {
+    // any_fp32: neither the values nor their maximum need be bf16 numbers
+    __device__ explicit E4m3Coder(float scale, bool any_fp32 = false) : s(scale) {
         inv = refined_reciprocal(s, __builtin_amdgcn_rcpf(s));
-        mid_range = s > SCALE_MID_MIN && s < SCALE_MID_MAX;
+        mid_range = s > SCALE_MID_MIN && s < SCALE_MID_MAX && !(any_fp32 && significand_all_ones(s));
     }
     __device__ float quotient(float v) const { return corrected_quotient(v, s, inv); }
     // four codes, a in the low byte.  |v| <= amax, so the quotient is at most 448 up to one rounding, which the conversion
