@@ -1,18 +1,18 @@
 // Residual addition, root-mean-square norm and e4m3 coding in one pass over a row, and the norm's gradient.
 #include "grad_common.hpp"
+#include "grad_rules.hpp"
 #include "lanes.hpp"
 
 namespace moe355 {
 namespace {
 
 constexpr int NORM_MAX_THREADS = 1024;
-constexpr int NORM_ROWS = 16;                  // rows of a block with codes at most
 constexpr int NORM_VECTORS = 4;                // vectors of eight elements that a thread holds at most
 
 struct norm_args {
     const void *x, *residual;
     const float* gain;
-    int64_t rows, ld_x, ld_res;
+    int64_t rows, first, ld_x, ld_res;         // (first: of a launch)
     int cols;
     float eps;
     void *sum, *y;
@@ -32,7 +32,7 @@ __global__ __launch_bounds__(NORM_MAX_THREADS) void norm_kernel(const norm_args 
     extern __shared__ float s_scales[];        // [cols / 128][NORM_ROWS]
     const int vecs = a.cols / 8, waves = blockDim.x >> 6, tid = threadIdx.x, lane = tid & 63;
     const int rest = REST ? a.cols & 7 : 0, last = vecs * 8 + tid;        // thread t < rest has column `last` as well
-    const int64_t r0 = (int64_t)blockIdx.x * per_block;
+    const int64_t r0 = a.first + (int64_t)blockIdx.x * per_block;
     const int rows = (int)(a.rows - r0 < per_block ? a.rows - r0 : per_block);
     raw8<BF16, REST && NV < 4> x[NV], res[NV];
     float x1 = 0.f, res1 = 0.f;
@@ -287,7 +287,7 @@ int row_threads(int cols, int& vectors) {
 constexpr int64_t NORM_MAX_GRID = 1 << 20;
 
 template <bool BF16>
-hipError_t norm_forward(hipStream_t s, const norm_args& a) {
+hipError_t norm_forward(hipStream_t s, norm_args a) {
     int vectors;
     const int threads = row_threads(a.cols, vectors);
     if (!threads) {
@@ -295,24 +295,18 @@ hipError_t norm_forward(hipStream_t s, const norm_args& a) {
         norm_any_kernel<BF16><<<(unsigned)(a.rows < NORM_MAX_GRID ? a.rows : NORM_MAX_GRID), 256, 0, s>>>(a);
         return hipGetLastError();
     }
-    // blocks of many rows for the sake of their scales, as long as 32 waves are left for a CU and no block is so long that the last ones run alone
-    // (32768 x 7168: 16 rows 352 us, 8 340, 4 332; 16384 x 2048: 8 rows 45.5, 4 47.7)
-    int64_t per_block = a.q ? a.rows * (threads / 64) / 8192 : 1;
-    if (per_block > 32768 / a.cols) per_block = 32768 / a.cols;
-    if (per_block > NORM_ROWS) per_block = NORM_ROWS;
-    const int64_t least = (a.rows * threads >> 31) + 1;        // (a grid has fewer than 2^32 threads)
-    if (per_block < least) per_block = least;
-    if (a.q && per_block > NORM_ROWS) return hipErrorInvalidValue;         // (x alone would be larger than the card's memory)
-    const int64_t blocks = (a.rows + per_block - 1) / per_block;
+    const int per_block = norm_rows_per_block(a.rows, a.cols, threads, a.q != nullptr);
     const size_t lds = a.q && per_block > 1 ? (size_t)a.cols / QBLOCK * NORM_ROWS * sizeof(float) : 0;
     const bool rest = a.cols % 8 != 0;
     const auto kernel = vectors == 1   ? (rest ? norm_kernel<BF16, 1, true> : norm_kernel<BF16, 1, false>)
                         : vectors == 2 ? (rest ? norm_kernel<BF16, 2, true> : norm_kernel<BF16, 2, false>)
                                        : (rest ? norm_kernel<BF16, NORM_VECTORS, true> : norm_kernel<BF16, NORM_VECTORS, false>);
-    kernel<<<(unsigned)blocks, threads, lds, s>>>(a, (int)per_block);
+    for (int64_t blocks; a.first < a.rows; a.first += blocks * per_block) {
+        blocks = norm_blocks(a.rows - a.first, threads, per_block);
+        kernel<<<(unsigned)blocks, threads, lds, s>>>(a, per_block);
+    }
     return hipGetLastError();
 }
-
 
 template <bool BF16>
 hipError_t norm_backward(hipStream_t s, norm_back_args a, float* dgain) {
@@ -346,7 +340,7 @@ bool norm_codes_fit(int32_t cols) {
 
 hipError_t launch_norm(hipStream_t s, const void* x, const void* residual, const float* gain, int64_t rows, int32_t cols, int64_t ld_x,
                        int64_t ld_res, int32_t dtype, float eps, void* sum, void* y, uint8_t* q, float* scales, float* rstd) {
-    const norm_args a{x, residual, gain, rows, ld_x, residual ? ld_res : 0, cols, eps, sum, y, q, scales, rstd};
+    const norm_args a{x, residual, gain, rows, 0, ld_x, residual ? ld_res : 0, cols, eps, sum, y, q, scales, rstd};
     return dtype == MOE_BF16 ? norm_forward<true>(s, a) : norm_forward<false>(s, a);
 }
 
