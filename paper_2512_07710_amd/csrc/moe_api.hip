@@ -290,7 +290,7 @@ int moe_add_rmsnorm(moe_ctx* c, const void* x, const void* residual, const float
     if ((sum == x && ld_x != cols) || (sum && sum == residual && ld_res != cols)) return MOE_EINVAL;
     if (q) {
         if (cols % QBLOCK || !norm_codes_fit(cols) || !aligned(q, 8) || !aligned(scales, 4)) return MOE_EINVAL;
-        if (ld_x % 8 || !aligned(x, 16) || (residual && (ld_res % 8 || !aligned(residual, 16)))) return MOE_EINVAL;
+        if (ld_x * bytes % 16 || !aligned(x, 16) || (residual && (ld_res * bytes % 16 || !aligned(residual, 16)))) return MOE_EINVAL;
     }
     return hip_rc(launch_norm(c->stream, x, residual, gain, rows, cols, ld_x, ld_res, dtype, eps, sum, y, q, scales, rstd));
 }
