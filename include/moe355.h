@@ -291,7 +291,8 @@ int moe_policy_loss(moe_ctx* ctx, const void* logits, int64_t ld, int32_t dtype,
  * xq, and its own Wq[e], ws[e], dW[e] (offsets [E+1] i32 on the device, non-decreasing, from 0 to at most rows; values outside
  * [0,rows] are taken as the nearest in it).
  *   dx[p,c] = sum_n dy[p,n] * ws[n/128,c/128] * Wq[n,c]
- *     exact products of bf16 and e4m3 on the matrix cores, fp32 sums and block scales; rows behind offsets[E] are not written.
+ *     exact products of bf16 and e4m3 on the matrix cores, fp32 sums and block scales (any finite ws; beside one below 2^-117 the sums stay below
+ *     2^95); rows behind offsets[E] are not written.
  *   dW[n,c] = sum_p dy[p,n] * xs[c/128,p] * xq[p,c]   (0 for an expert without rows); accumulate != 0: added to dW
  *     the scale runs along the sum, so the operand is xs*xq: rounded to bf16 for a bf16 dW (an error the size of the output's own
  *     rounding), held to 24 bits in three bf16 planes for a f32 dW.

@@ -201,16 +201,18 @@ __device__ inline v8bf codes_bf16(v2i c, float pow2) {
 }
 
 // (dgrad) Sums are held in units of the present block's scale without its power of two, which the codes carry: a factor of less than two either way
-// from block to block, whatever the scales are.
+// from block to block.  That power of two stays where every code, 2^-9 to 448, is a normal bf16 number; what a scale has beyond is left in the unit, which
+// then is up to 2^10 or down to 2^-32 (a scale below the normal range).
 struct block_scale {
+    static constexpr uint32_t LEAST = (127 - 117) << 23, MOST = (127 + 118) << 23;             // 2^-117 and 2^118
     float scale = 1.f, pow2 = 1.f;
     int mask = -1;                             // on the codes
     __device__ float next(float s) {           // the factor on the sums
-        const uint32_t exponent = __float_as_uint(s) & 0x7F800000u;
-        const bool live = exponent != 0, finite = exponent != 0x7F800000u;
-        mask = live ? -1 : 0;                  // a zero scale (or one below the normal range): the block adds nothing
-        const float to = !live ? scale : finite ? __uint_as_float((__float_as_uint(s) & 0x807FFFFFu) | 0x3F800000u) : s;
+        const uint32_t bits = __float_as_uint(s) & 0x7FFFFFFFu, exponent = min(max(bits & 0x7F800000u, LEAST), MOST);
+        const bool live = bits != 0, finite = bits < 0x7F800000u;
+        mask = live ? -1 : 0;                  // a zero scale: the block adds nothing
         pow2 = live && finite ? __uint_as_float(exponent) : 1.f;
+        const float to = !live ? scale : finite ? s * __uint_as_float((254u << 23) - exponent) : s;
         const float ratio = scale / to;
         scale = to;
         return ratio;
