@@ -18,6 +18,7 @@ constexpr int G_PART = 18;                     // parts that go through memory i
 struct split_plan {
     int whole, cut, parts;                     // tiles done at once; tiles in parts, and how many parts
 };
+// The host launches by this plan and each block works out its own: whole numbers throughout, so that both come to the same one.
 // weight: time of a stage, in tenths of a bf16 one; fill: how much of the tiles' rows there is, in percent
 __host__ __device__ inline split_plan plan_of(int tiles, int stages, int weight, int fill) {
     const split_plan none{tiles, 0, 1};
@@ -27,7 +28,7 @@ __host__ __device__ inline split_plan plan_of(int tiles, int stages, int weight,
     // the rest of many: what is saved against what the parts' way through memory costs (dgrad 4096 x 32768 x 5120 not cut 1324 us, cut 1160; 4096 x
     // 8192 x 5120 325, 295; 2600 x 8192 x 8192 341, 305; but 4096 x 2048 x 5120 85.8, 96.2 and 4096 x 4096 x 5120 166, 163)
     if (tiles >= G_SLOTS) {
-        if (most < 3 || stages * (0.55f - 1.0f / most) < 24.f) return none;
+        if (most < 3 || (int64_t)stages * (11 * most - 20) < (int64_t)480 * most) return none;     // stages (0.55 - 1 / most) < 24
         return split_plan{tiles - rest, rest, most};
     }
     // p parts take stages / p, and 4 for the second launch with 1 for every 18 full parts that go through memory: the best p is the last that
