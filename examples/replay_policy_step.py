@@ -4,11 +4,16 @@
 
 The trainer's second evaluation of the rollout's tokens (Router Replay, section 2.4.4): the layer runs from the routing log, its output
 joins the residual stream, is normalised and coded for the FP8 head, and the clipped policy loss is taken on the head's logits.  Then
-everything is walked back to the tokens, the experts' matrices, the router's logits, the norm's gain and the head.
+everything is walked back to the tokens, the experts' matrices, the router, the norm's gain and the head.
+
+Router Replay comes in two forms.  With a router, the log's expert ids are replayed and the gates are this policy's own, a softmax over its logits of those
+experts: they depend on the tokens and on the router, and the gradient goes on into both.  Without one, the logged gates are replayed too and are constants;
+`drouter` is then the gradient that logits behind such gates would receive, and goes no further.
 
 The 8-bit activations that the forward pass made are the checkpoints of the backward pass: no activation is kept in bf16 but the
-norm's input.  SwiGLU's own derivative, which is elementwise, is written in torch here; it and the gate and up projections that it needs are
-recomputed from the codes.
+norm's input.  SwiGLU's own derivative, which is elementwise, and the router's two products are written in torch here; SwiGLU's and the gate and up
+projections that it needs are recomputed from the codes, expert by expert, for which the experts' bounds come to the host: that, and the layer's
+`hidden()`, which waits for its copies, are what a captured graph could not take.
 """
 from __future__ import annotations
 
@@ -56,23 +61,32 @@ class ReplayPolicyStep:
         self.dhidden, self.dW2 = new(N, F, t=b16), new(E, d, F)
         self.x_perm, self.xq, self.xs = new(N, d, t=b16), new(N, d, t=u8), new(d // BLOCK, N)
         self.dx_gate, self.dx_up, self.dx = new(N, d, t=b16), new(N, d, t=b16), new(T, d, t=b16)
+        self.dW_router = new(E, d)
         self.dW1, self.dW3 = new(E, F, d), new(E, F, d)
 
     def close(self):
         self.layer.close()
 
-    def forward(self, x, log_ids, log_w, w, gain, head_q, head_s, batch):
-        """The loss [1] of this batch: target, old_logp, ref_logp, advantage, weight."""
+    def forward(self, x, log_ids, log_w, w, gain, head_q, head_s, batch, router=None):
+        """The loss [1] of this batch: target, old_logp, ref_logp, advantage, weight.  router [E, d]: log_w is not read, the gates are computed."""
         L, c = self.layer, self.ctx
-        y = L.forward_replay(x, log_ids, log_w, w)
+        if router is None:
+            y = L.forward_replay(x, log_ids, log_w, w)
+        else:
+            L.route_replay_ids(x, router, log_ids)
+            L.quantize_tokens(x)
+            L.expert_ffn_gather(w)
+            L.combine()
+            y = L.y
         moe.moe_add_rmsnorm(c, y, x, gain, EPS, sum=self.h, q=self.n_q, scales=self.n_s, rstd=self.rstd)
         moe.moe_linear_fp8(c, self.n_q, self.n_s, self.T, self.d, head_q, head_s, self.wide, self.logits)
         moe.moe_policy_loss(c, self.logits[:, :self.V], batch["target"], batch["old_logp"], batch["ref_logp"], batch["advantage"], batch["weight"],
                             self.logp, self.entropy, self.row_loss, self.loss, self.dlogits[:, :self.V], **LOSS)
         return self.loss
 
-    def backward(self, x, w, gain, head_q, head_s):
-        """Gradients of the last forward pass, in this object's buffers: dx, dW1, dW3, dW2, drouter, dgain, dhead."""
+    def backward(self, x, w, gain, head_q, head_s, router=None):
+        """Gradients of the last forward pass, in this object's buffers: dx, dW1, dW3, dW2, drouter, dgain, dhead, and with the forward pass's router
+        dW_router."""
         L, c = self.layer, self.ctx
         moe.moe_linear_fp8_dgrad(c, self.dlogits, head_q, head_s, None, self.dn)
         moe.moe_linear_fp8_wgrad(c, self.dlogits, self.n_q, self.n_s, None, self.dhead)
@@ -89,7 +103,11 @@ class ReplayPolicyStep:
         moe.moe_linear_fp8_dgrad(c, du, w["W3q"], w["s3"], L.offsets, self.dx_up)
         moe.moe_linear_fp8_wgrad(c, dg, self.xq, self.xs, L.offsets, self.dW1)
         moe.moe_linear_fp8_wgrad(c, du, self.xq, self.xs, L.offsets, self.dW3)
-        moe.moe_dispatch_backward(c, self.dx_gate.add_(self.dx_up), L.inv_perm, self.dh, self.dx)        # dh: the residual's own way
+        beside = self.dh                                       # the residual's own way
+        if router is not None:                                 # and the gates'
+            beside = (self.dh.float() + self.drouter @ router).to(torch.bfloat16)
+            torch.matmul(self.drouter.t(), x.float(), out=self.dW_router)
+        moe.moe_dispatch_backward(c, self.dx_gate.add_(self.dx_up), L.inv_perm, beside, self.dx)
         return self.dx
 
     def _swiglu_backward(self, w, bounds):
@@ -139,15 +157,19 @@ def main():
     T, d, E, k, F, V = 512, 1024, 16, 4, 512, 4000
     x, ids, log_w, w, gain, head_q, head_s, batch = make_batch(T, d, E, k, F, V)
     step = ReplayPolicyStep(T, d, E, k, F, V)
-    # the rollout's own log-probabilities: the old policy is the present one, the reference near it
-    step.forward(x, ids, log_w, w, gain, head_q, head_s, batch)
+    # the rollout's log: ids of its own router, which the present one has moved away from
+    router = torch.randn(E, d, generator=torch.Generator(device=x.device).manual_seed(1), device=x.device) * 2 * d ** -0.5
+    step.layer.route(x, router, None)
+    ids, router = step.layer.topk_idx.clone(), router + 0.02 * torch.randn_like(router)
+    # its log-probabilities: the old policy is the present one, the reference near it
+    step.forward(x, ids, None, w, gain, head_q, head_s, batch, router)
     batch["old_logp"] = step.logp.clone()
     batch["ref_logp"] = step.logp + 0.1 * torch.randn_like(step.logp)
-    loss = step.forward(x, ids, log_w, w, gain, head_q, head_s, batch).clone()
-    step.backward(x, w, gain, head_q, head_s)
+    loss = step.forward(x, ids, None, w, gain, head_q, head_s, batch, router).clone()
+    step.backward(x, w, gain, head_q, head_s, router)
     torch.cuda.synchronize()
     print(f"loss {float(loss):.6f}, mean log-probability {float(step.logp.mean()):.4f}, mean entropy {float(step.entropy.mean()):.4f}")
-    for name in ("dx", "dW1", "dW3", "dW2", "drouter", "dgain", "dhead"):
+    for name in ("dx", "dW1", "dW3", "dW2", "drouter", "dW_router", "dgain", "dhead"):
         print(f"  |{name}| = {float(getattr(step, name).float().norm()):.4e}")
     step.close()
 
