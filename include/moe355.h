@@ -292,10 +292,10 @@ int moe_policy_loss(moe_ctx* ctx, const void* logits, int64_t ld, int32_t dtype,
  * [0,rows] are taken as the nearest in it).
  *   dx[p,c] = sum_n dy[p,n] * ws[n/128,c/128] * Wq[n,c]
  *     exact products of bf16 and e4m3 on the matrix cores, fp32 sums and block scales (any finite ws; beside one below 2^-117 the sums stay below
- *     2^95); rows behind offsets[E] are not written.
+ *     2^95; a zero scale's block adds nothing, whatever its codes); rows behind offsets[E] are not written.
  *   dW[n,c] = sum_p dy[p,n] * xs[c/128,p] * xq[p,c]   (0 for an expert without rows); accumulate != 0: added to dW
  *     the scale runs along the sum, so the operand is xs*xq: rounded to bf16 for a bf16 dW (an error the size of the output's own
- *     rounding), held to 24 bits in three bf16 planes for a f32 dW.
+ *     rounding; who wants the operand whole asks for a f32 dW), held to 24 bits in three bf16 planes for a f32 dW (values down to 2^-101).
  *   dy [rows,NOUT] bf16; Wq [E,NOUT,K] u8; ws [E,NOUT/128,K/128] f32; xq [rows,K] u8; xs [K/128][rows] f32;
  *   dx [rows,K] bf16; dW [E,NOUT,K] dtype.  K and NOUT multiples of 128 up to 2^24, NOUT*K < 2^32 and 1 <= E <= 256; rows < 2^31 - 256. */
 int moe_linear_fp8_dgrad(moe_ctx* ctx, const uint16_t* dy, int64_t rows, int32_t NOUT, const uint8_t* Wq, const float* ws, int32_t K,

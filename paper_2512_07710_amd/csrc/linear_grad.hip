@@ -9,7 +9,8 @@
 // PFLOP/s (32x32x16: 1.88), the library's bf16 products of these sizes at 1.32 to 1.53.  A tile is 128 x 256, two blocks to a CU: a wave's 128 x 64
 // take 10 KiB of LDS for 0.5 million operations, and one block's products cover the other's waits.  dgrad 8192 x 8192 x
 // 8192 827 us = 1.33 PFLOP/s, 4096 x 32768 x 5120 1145 = 1.20; wgrad 897 = 1.23 and 1165 = 1.18, with three planes for fp32 results 4096 x 4096 x 4096
-// 324 = 0.42 (three times the products: 1.27).  Fewer rows: the codes (dgrad) or the results (wgrad) at the memory's rate: 128 rows on 128 experts of
+// 324 = 0.42 (three times the products: 1.27); cards differ by 3 %.  With accumulate, dW is read just before it is written, 8 or 16 bytes of a row at a
+// time: 128 experts of 5120 x 1536 under 32768 rows 811 -> 1432 us, 32768 x 5120 under 4096 rows 1222 -> 1287.  Fewer rows: the codes (dgrad) or the results (wgrad) at the memory's rate: 128 rows on 128 experts of
 // 5120 x 1536 176 us = 5.7 TB/s read, wgrad 331 = 6.1 TB/s written.
 #include "ffn_common.hpp"
 #include "grad_common.hpp"

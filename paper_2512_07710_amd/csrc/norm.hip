@@ -114,7 +114,8 @@ __global__ __launch_bounds__(NORM_MAX_THREADS) void norm_kernel(const norm_args 
     }
 }
 
-// Rows too wide for a block's registers: element by element, the row read twice.  No codes.
+// Rows too wide for a block's registers: element by element, the row read twice.  No codes.  2000 x 65536 bf16 with residual and sum 747 us = 1.4 TB/s
+// (2000 x 32768, in vectors: 114 us = 4.6 TB/s).
 template <bool BF16>
 __global__ __launch_bounds__(256) void norm_any_kernel(const norm_args a) {
     __shared__ float lds[4];
@@ -236,7 +237,8 @@ __global__ __launch_bounds__(THREADS) void norm_back_kernel(const norm_back_args
     if (REST && tid < rest) a.partial[(int64_t)blockIdx.x * a.cols + last] = dg1;
 }
 
-// Rows too wide for a block's registers.  A thread's columns of dgain are added up in the block's row of `partial`, which it alone touches.
+// Rows too wide for a block's registers.  A thread's columns of dgain are added up in the block's row of `partial`, which it alone touches: a read and a write
+// of memory for each element, 2000 x 65536 bf16 2930 us = 0.36 TB/s (2000 x 32768 in registers, one block of 1024 threads to a CU: 319).
 template <bool BF16>
 __global__ __launch_bounds__(256) void norm_back_any_kernel(const norm_back_args a) {
     __shared__ float lds[4];

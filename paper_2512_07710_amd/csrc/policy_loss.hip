@@ -303,8 +303,9 @@ struct row_grad {
 };
 
 // dz[v] = (dlogp (1[v = target] - p_v) + w entropy_coef p_v (log p_v + H)) / temperature, which is 2^y (a y + b) for numbers a, b of the row.
-// Bound by the bytes: logits once, gradients once; 4096 x 131072 bf16 456 us = 4.7 TB/s (a copy: 4.87), with the row read twice 1390.  333 x 50001 f32
-// 30.9 us where a copy takes 20.5: a row is one CU's, and 77 of the rows have a second round.
+// Bound by the bytes, logits once and gradients once, and by the vector ALU: with one row to a CU its copies, sums and gradient follow one another, and an
+// instruction for each logit is 14 us of 4096 x 131072 bf16, 476 us = 4.5 TB/s (a copy: 4.87; v c - m c in one instruction each, which large logits do not
+// allow, 456).  333 x 50001 f32 32 us where a copy takes 20.5: a row is held by the registers of one CU, and 77 of the rows have a second round.
 // One block per row.  HELD: the row stays in registers between the two passes that its maximum and its sum ask for and the pass
 // that writes its gradient, so it is read once; otherwise it is read again for the gradient.
 template <bool BF16, bool GRAD_BF16, bool HELD>
@@ -473,8 +474,10 @@ __global__ __launch_bounds__(PART_THREADS) void loss_part_grad_kernel(const loss
 }
 
 // Parts of a row: long rows that alone leave much of the chip idle.  With a gradient that makes two launches of one and the row is read
-// twice: 64 x 131072 bf16 25 -> 18 us, 128 27 -> 22, but 192 31 -> 34 and 100 x 64000 15.4 -> 16.3.  Without: 8 x 131072 f32 18 -> 12,
-// 500 x 131072 bf16 44 -> 32, 256 x 64000 level.
+// twice: 64 x 131072 bf16 25 -> 18 us, 128 28.5 -> 22.5, but 192 31 -> 34 and 100 x 64000 15.4 -> 16.3; f32 rows of the same 16-byte vectors lose a little:
+// 64 x 32768 10.5 -> 12.4, 128 x 60000 17.4 -> 19.6, 128 x 131072 31.2 -> 33.3, 200 x 60000 20 -> 27.  Without: 8 x 60000 f32 10 -> 8, 500 x 60000 f32
+// 32 -> 27.5, 512 x 131072 bf16 46.5 -> 33, f32 level, 500 x 32768 f32 15.4 -> 16.7.  GRAD_MAX_SPLIT_ROWS is how many rows have a ticket, no measured bound
+// (600 x 131072 bf16 in one block each: 60 us).
 int loss_parts(int64_t rows, int vecs, bool gradient) {
     if (vecs < 8192 || rows > (gradient ? 128 : GRAD_MAX_SPLIT_ROWS)) return 1;
     const int64_t parts = 1024 / rows < vecs / 512 ? 1024 / rows : vecs / 512;
