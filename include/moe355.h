@@ -231,8 +231,9 @@ int moe_reserve_gradients(moe_ctx* ctx);
  *   sum [rows,cols] dtype: receives h; NULL if not wanted.  It may be x or residual itself where that has ld == cols.
  *   y [rows,cols] dtype, or NULL.
  *   q [rows,cols] u8 and scales [cols/128][rows] f32, or both NULL: y as moe_quantize_fp8 would code it, but from the
- *   fp32 y: one rounding; and a NaN is kept: its group of 128 columns leaves as scale NaN and NaN codes (moe_quantize_fp8 passes over it), a group
- *   with an infinity as scale inf, with a NaN code where y is infinite and zeros elsewhere.
+ *   fp32 y: one rounding.  The scale is 1 wherever amax/448 is zero.  A NaN is kept (moe_quantize_fp8 passes over it): its
+ *   group of 128 columns leaves as scale NaN and NaN codes, a group with an infinity as scale inf, with a NaN code where y
+ *   is infinite and zeros elsewhere.
  *   cols must then be a multiple of 128, at most 32768, and the rows of x and residual lie at multiples of 16 bytes.
  *   rstd [rows] f32: receives r; or NULL.
  * 1 <= cols <= 65536, eps >= 0.  A row that holds a NaN or an infinity affects its own outputs only. */

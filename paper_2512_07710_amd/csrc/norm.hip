@@ -95,7 +95,8 @@ __global__ __launch_bounds__(NORM_MAX_THREADS) void norm_kernel(const norm_args 
                 for (int j = 0; j < 8; ++j) amax = __builtin_elementwise_maximum(amax, fabsf(y.v[j]));
 #pragma unroll
                 for (int o = 1; o < 16; o <<= 1) amax = __builtin_elementwise_maximum(amax, __shfl_xor(amax, o));
-                const E4m3Coder coder(amax == 0.f ? 1.0f : amax / 448.0f, true);
+                const float scale = amax / 448.0f;
+                const E4m3Coder coder(scale == 0.f ? 1.0f : scale, true);                      // (zero up to a maximum of 448 * 2^-150)
                 u32x2 c;
                 c[0] = coder.pack4<true>(y.v[0], y.v[1], y.v[2], y.v[3]);
                 c[1] = coder.pack4<true>(y.v[4], y.v[5], y.v[6], y.v[7]);

@@ -52,3 +52,16 @@ def test_scales_of_nothing_but_ones(gpu_lib):
         g[0], g[1::2] = amax, -g[1::2]
         groups.append(g.astype(np.float32))
     _check(gpu_lib, np.concatenate(groups))
+
+
+def test_maxima_whose_scale_underflows(gpu_lib):
+    """amax / 448 is zero in fp32 up to 448 * 2^-150: scale 1 and codes of zero, with zeros in the group and without"""
+    gain = np.zeros(512, np.float32)
+    gain[:3] = 1e-43, -1e-44, 1.5e-45
+    gain[128:256] = 1e-44
+    gain[256:384] = np.float32(2.0) ** -140                    # (the scale is the smallest subnormal)
+    gain[384] = 1.0
+    q, s = _codes(gpu_lib, gain, 3)
+    assert (s[:2] == 1).all() and (s[2] == np.float32(2.0) ** -149).all() and (s[3] == np.float32(1) / np.float32(448)).all()
+    assert (q[:, :256] & 0x7F == 0).all() and (q[:, 385:] & 0x7F == 0).all() and (q[:, 384] == 0x7E).all()
+    assert (q[:, 256:384] == 0x7E).all()                       # 2^-140 / 2^-149 = 512, the largest code
