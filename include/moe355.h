@@ -304,6 +304,58 @@ int moe_linear_fp8_dgrad(moe_ctx* ctx, const uint16_t* dy, int64_t rows, int32_t
 int moe_linear_fp8_wgrad(moe_ctx* ctx, const uint16_t* dy, int64_t rows, int32_t NOUT, const uint8_t* xq, const float* xs, int32_t K,
                          const int32_t* offsets, int32_t E, int32_t accumulate, int32_t dtype, void* dW);
 
+/* ---- The two ends of a policy step ------------------------------------------------------------------------------------
+ * Token ids to rows in front of the layer and the table's gradient behind it; what a rollout logs about its tokens, as a function with a gradient of
+ * its own; the norm of all gradients and the clipping to it.  dtype, ld, [reserved] and determinism as on the training side. */
+
+/* Rows of an embedding: y[t] = scale * table[ids[t]], multiplied in fp32, rounded once to y's type.  Ids outside [0,V), padding among them, give a row of
+ * zeros.  ids [T] i32; table [V,d] dtype, ld; y [T,d] out_dtype, ld_y.  T <= 2^30, 1 <= d <= 65536, lds below 2^31, scale finite. */
+int moe_embed(moe_ctx* ctx, const int32_t* ids, int64_t T, const void* table, int32_t V, int32_t d, int64_t ld, int32_t dtype, float scale, void* y,
+              int64_t ld_y, int32_t out_dtype);
+
+/* Its gradient [reserved]: G[v] = scale * sum of dy[t] over the t with ids[t] = v, fp32 sums in an order that depends on the ids and the sizes alone.
+ *   accumulate == 0: dtable[v] = G[v], zeros for a token that does not occur;  != 0: dtable[v] += G[v], the others' rows are neither read nor written.
+ *   Ids outside [0,V) add nothing, and their rows of dy are not read.
+ *   dy [T,d] dtype, ld; dtable [V,d] grad_dtype, ld_grad.  T <= 2^21, sizes otherwise as moe_embed. */
+int moe_embed_backward(moe_ctx* ctx, const void* dy, const int32_t* ids, int64_t T, int32_t V, int32_t d, int64_t ld, int32_t dtype, float scale,
+                       int32_t accumulate, void* dtable, int64_t ld_grad, int32_t grad_dtype);
+
+/* Log-probabilities of given tokens, entropy, and the most likely tokens [reserved].  Row t, z = logits/temperature, m its largest logit:
+ *   logp[t,j] = z[ids[t,j]] - log sum_v exp z[v];  entropy[t] = -sum_v p_v log p_v;
+ *   top_idx[t,i], top_logp[t,i]: the n largest logits, in descending order, equal ones by ascending index, and their log-probabilities;
+ *   stats[t] = { m, sum_v exp((logits[v] - m)/temperature) }: what the gradient reads beside the logits.
+ *   logits [rows,V] dtype, ld; ids, logp [rows,m], null for m == 0; top_idx [rows,n] i32, top_logp [rows,n] f32, null for n == 0; entropy [rows] f32 or
+ *   NULL; stats [rows,2] f32 or NULL.  m, n <= 64 (n may exceed V).
+ * Masked logits and errors as in moe_policy_loss.  logp is 0 for an id outside [0,V) and -inf for a masked one.  Masked logits and NaN are no alternatives:
+ * places that are left have top_idx -1 and top_logp -inf.  A row with nothing but masked logits has entropy 0 and stats { -inf, 0 }.  A NaN or +inf makes
+ * its row's entropy and log-probabilities NaN (0 and -1 for what is outside or left as above stay). */
+int moe_token_logp(moe_ctx* ctx, const void* logits, int64_t ld, int32_t dtype, int64_t rows, int32_t V, const int32_t* ids, int32_t m, float temperature,
+                   float* logp, float* entropy, int32_t n, int32_t* top_idx, float* top_logp, float* stats);
+
+/* The logits' gradient from that of logp and of entropy; p from stats:
+ *   dlogits[t,v] = ( sum_j dlogp[t,j] (1[v = ids[t,j]] - p_v) - dentropy[t] p_v (log p_v + H) ) / temperature
+ *   dlogp [rows,m] f32, null for m == 0; dentropy [rows] f32 or NULL, entropy (H) [rows] f32 then as moe_token_logp wrote it, otherwise not read;
+ *   stats [rows,2] as written there, from the same logits and temperature; dlogits [rows,V] grad_dtype, ld_grad: may be logits itself if both types and
+ *   lds are equal.  The same token may be given several times: the terms add up.
+ * Without effect are tokens outside [0,V) and masked ones, whatever their dlogp.  A row with no dlogp of effect other than zero and a dentropy of zero is
+ * written as zeros, and so is a row with nothing but masked logits; masked logits have no gradient. */
+int moe_token_logp_backward(moe_ctx* ctx, const void* logits, int64_t ld, int32_t dtype, int64_t rows, int32_t V, const int32_t* ids, int32_t m,
+                            float temperature, const float* dlogp, const float* dentropy, const float* stats, const float* entropy, void* dlogits,
+                            int64_t ld_grad, int32_t grad_dtype);
+
+/* Norm of a list of n gradients taken together [reserved]: sum_sq[0] = the sum of all squares in fp64, which holds the square of any fp32 number (add it up
+ * over the ranks that own different parameters before clipping); norm[0] = its square root in f32, or norm NULL.
+ *   grads, counts, dtypes: HOST arrays of n device pointers, element counts and types, read during the call; an array of elements each, any alignment
+ *   that its type has, null for a count of 0.  0 <= n <= 65536, counts together at most 2^40. */
+int moe_grad_norm(moe_ctx* ctx, const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n, double* sum_sq, float* norm);
+
+/* Clipping to a largest norm: outs[i] = grads[i] * min(1, max_norm / sqrt(sum_sq[0])), the factor rounded to fp32, the product to the gradient's type.
+ *   outs: HOST array of n device pointers, or NULL: in place; outs[i] == grads[i] is in place as well; no array may overlap another otherwise.
+ *   A factor of 1 changes nothing, and gradients in place are then neither read nor written.  sum_sq 0: factor 1; infinite: 0; NaN: NaN, as their elements
+ *   then come out.  max_norm >= 0, finite. */
+int moe_clip_grads(moe_ctx* ctx, const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n, const double* sum_sq, float max_norm,
+                   void* const* outs);
+
 /* Length-based load balancing before rollout (paper section 3.1.1): distributes n samples over
  * n_groups worker groups so that the groups' total predicted generation lengths are about equal.
  * The paper states the goal only; the rule taken is longest-first list scheduling: samples are

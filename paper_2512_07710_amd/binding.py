@@ -23,6 +23,7 @@ EXPORTS = ("moe_create", "moe_destroy", "moe_strerror", "moe_route", "moe_route_
            "moe_expert_ffn_fp8_gather", "moe_combine", "moe_balance_lengths", "moe_debug_copy_hidden",
            "moe_reserve_gradients", "moe_add_rmsnorm", "moe_add_rmsnorm_backward", "moe_dispatch", "moe_dispatch_backward",
            "moe_combine_backward", "moe_policy_loss", "moe_linear_fp8_dgrad", "moe_linear_fp8_wgrad",
+           "moe_embed", "moe_embed_backward", "moe_token_logp", "moe_token_logp_backward", "moe_grad_norm", "moe_clip_grads",
            "moe_probe_copy", "moe_probe_fp8_mfma", "moe_profile_enable", "moe_profile_read", "moe_version")
 
 
@@ -79,6 +80,12 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.moe_policy_loss.argtypes = [vp, vp, i64, i32, i64, i32] + [vp] * 6 + [f32] * 5 + [vp] * 5 + [i64, i32]
     lib.moe_linear_fp8_dgrad.argtypes = [vp, vp, i64, i32, vp, vp, i32, vp, i32, vp]
     lib.moe_linear_fp8_wgrad.argtypes = [vp, vp, i64, i32, vp, vp, i32, vp, i32, i32, i32, vp]
+    lib.moe_embed.argtypes = [vp, vp, i64, vp, i32, i32, i64, i32, f32, vp, i64, i32]
+    lib.moe_embed_backward.argtypes = [vp, vp, vp, i64, i32, i32, i64, i32, f32, i32, vp, i64, i32]
+    lib.moe_token_logp.argtypes = [vp, vp, i64, i32, i64, i32, vp, i32, f32, vp, vp, i32, vp, vp, vp]
+    lib.moe_token_logp_backward.argtypes = [vp, vp, i64, i32, i64, i32, vp, i32, f32, vp, vp, vp, vp, vp, i64, i32]
+    lib.moe_grad_norm.argtypes = [vp, vp, vp, vp, i32, vp, vp]
+    lib.moe_clip_grads.argtypes = [vp, vp, vp, vp, i32, vp, f32, vp]
     lib.moe_probe_copy.argtypes = [vp, vp, vp, i64]
     lib.moe_probe_fp8_mfma.argtypes = [vp, i32, i32, i32, vp]
     lib.moe_profile_enable.argtypes = [vp, i32]
@@ -384,6 +391,117 @@ def moe_linear_fp8_wgrad(ctx, dy, xq, xs, offsets, dW, accumulate=False) -> None
                                   _of(offsets, _I32, (E + 1,)), E, 1 if accumulate else 0, _type(dW), _of(dW, dW.dtype, pre + (NOUT, K)))
     if rc:
         _check(rc, "moe_linear_fp8_wgrad")
+
+
+# ---- the two ends of a policy step
+def moe_embed(ctx, ids, table, scale, y) -> None:
+    """ids int32 of any shape, T in all; table [V, d]; y [T, d] (bf16 or f32 each, rows may be strided)."""
+    lib = _lib or load_library()
+    V, d = _two(table)
+    T = ids.numel()
+    code, out = _type(table), _type(y)
+    pt, ld = _rows_of(table, table.dtype, (V, d))
+    py, ld_y = _rows_of(y, y.dtype, (T, d))
+    rc = lib.moe_embed(ctx, _flat(ids, T), T, pt, V, d, ld, code, scale, py, ld_y, out)
+    if rc:
+        _check(rc, "moe_embed")
+
+
+def moe_embed_backward(ctx, dy, ids, scale, dtable, accumulate=False) -> None:
+    """dy [T, d]; ids int32 of any shape, T in all; dtable [V, d] (bf16 or f32 each, rows may be strided)."""
+    lib = _lib or load_library()
+    V, d = _two(dtable)
+    T = ids.numel()
+    code, out = _type(dy), _type(dtable)
+    py, ld = _rows_of(dy, dy.dtype, (T, d))
+    pg, ld_g = _rows_of(dtable, dtable.dtype, (V, d))
+    rc = lib.moe_embed_backward(ctx, py, _flat(ids, T), T, V, d, ld, code, scale, 1 if accumulate else 0, pg, ld_g, out)
+    if rc:
+        _check(rc, "moe_embed_backward")
+
+
+def _given(ids: Optional[torch.Tensor], rows: int):
+    """(m, shape) of the given tokens: [rows], [rows, m] or None."""
+    if ids is None:
+        return 0, (rows, 0)
+    shape = ids.shape
+    return (1 if len(shape) == 1 else shape[1] if len(shape) == 2 else -1), shape
+
+
+def moe_token_logp(ctx, logits, ids, logp, entropy=None, top_idx=None, top_logp=None, stats=None, *, temperature=1.0) -> None:
+    """logits [rows, V] (bf16 or f32, rows may be strided); ids, logp [rows] or [rows, m], or None; top_idx, top_logp [rows, n], or None; every output
+    given is written."""
+    lib = _lib or load_library()
+    shape = rows, V = _two(logits)
+    code = _type(logits)
+    pz, ld = _rows_of(logits, logits.dtype, shape)
+    m, given = _given(ids, rows)
+    n = 0 if top_idx is None else _two(top_idx)[1]
+    rc = lib.moe_token_logp(ctx, pz, ld, code, rows, V, _of(ids, _I32, (rows, *given[1:])), m, temperature, _of(logp, _F32, given),
+                            _of(entropy, _F32, (rows,)), n, _of(top_idx, _I32, (rows, n)), _of(top_logp, _F32, (rows, n)), _of(stats, _F32, (rows, 2)))
+    if rc:
+        _check(rc, "moe_token_logp")
+
+
+def moe_token_logp_backward(ctx, logits, ids, dlogp, dentropy, stats, entropy, dlogits, *, temperature=1.0) -> None:
+    """ids, dlogp [rows] or [rows, m], or None; dentropy None: entropy is not read; dlogits [rows, V] may be logits itself."""
+    lib = _lib or load_library()
+    shape = rows, V = _two(logits)
+    code, gcode = _type(logits), _type(dlogits)
+    pz, ld = _rows_of(logits, logits.dtype, shape)
+    pg, ld_g = _rows_of(dlogits, dlogits.dtype, shape)
+    m, given = _given(ids, rows)
+    row = (rows,)
+    rc = lib.moe_token_logp_backward(ctx, pz, ld, code, rows, V, _of(ids, _I32, (rows, *given[1:])), m, temperature, _of(dlogp, _F32, given),
+                                     _of(dentropy, _F32, row), _of(stats, _F32, (rows, 2)), _of(entropy, _F32, row), pg, ld_g, gcode)
+    if rc:
+        _check(rc, "moe_token_logp_backward")
+
+
+class GradList:
+    """Gradients (bf16 or f32, contiguous, apart from each other) as the list that moe_grad_norm and moe_clip_grads take: their addresses, counts and types,
+    read once.  It keeps the tensors; one that is given other memory later (set_, resize_) needs a new list."""
+
+    def __init__(self, tensors):
+        self.tensors = tensors = list(tensors)
+        self.n = n = len(tensors)
+        for t in tensors:
+            if not t.is_cuda or not t.is_contiguous():
+                raise MoEError(f"expected contiguous CUDA tensors, got {tuple(t.shape)} of {t.dtype}, strides {t.stride()}, on {t.device}")
+            if t.device != tensors[0].device:
+                raise MoEError("expected tensors on one device")
+        self.shapes = [(t.dtype, t.numel()) for t in tensors]
+        ends = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in tensors if t.numel())
+        if any(a[1] > b[0] for a, b in zip(ends, ends[1:])):
+            raise MoEError("two of the tensors share memory")
+        self.addresses = (ctypes.c_void_p * n)(*[t.data_ptr() for t in tensors])
+        self.counts = (ctypes.c_int64 * n)(*[t.numel() for t in tensors])
+        self.types = (ctypes.c_int32 * n)(*[_type(t) for t in tensors])
+
+
+def _list(grads) -> GradList:
+    return grads if isinstance(grads, GradList) else GradList(grads)
+
+
+def moe_grad_norm(ctx, grads, sum_sq, norm=None) -> None:
+    """grads: a GradList, or tensors to make one of; sum_sq [1] f64, norm [1] f32."""
+    lib = _lib or load_library()
+    g = _list(grads)
+    rc = lib.moe_grad_norm(ctx, g.addresses, g.counts, g.types, g.n, _of(sum_sq, torch.float64, (1,)), _of(norm, _F32, (1,)))
+    if rc:
+        _check(rc, "moe_grad_norm")
+
+
+def moe_clip_grads(ctx, grads, sum_sq, max_norm, outs=None) -> None:
+    """grads, outs: GradLists, or tensors to make them of, of the same types and sizes; outs None: in place."""
+    lib = _lib or load_library()
+    g = _list(grads)
+    o = None if outs is None else _list(outs)
+    if o is not None and o is not g and o.shapes != g.shapes:
+        raise MoEError("outs must have the types and sizes of grads")
+    rc = lib.moe_clip_grads(ctx, g.addresses, g.counts, g.types, g.n, _of(sum_sq, torch.float64, (1,)), max_norm, None if o is None else o.addresses)
+    if rc:
+        _check(rc, "moe_clip_grads")
 
 
 def moe_balance_lengths(pred_len, n_groups: int, equal_count: bool = True):

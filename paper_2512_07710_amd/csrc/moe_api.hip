@@ -70,6 +70,26 @@ bool linear_grad_ok(const moe_ctx* c, int64_t rows, int32_t NOUT, int32_t K, con
     return (rows / 128 + E) * (((int64_t)K + 255) / 256) < (int64_t)1 << 31 && (int64_t)E * (NOUT / 128) * (((int64_t)K + 255) / 256) < (int64_t)1 << 31;
 }
 
+bool embed_ok(int32_t V, int32_t d, int64_t ld, int32_t dtype, int64_t ld_out, int32_t out_dtype, float scale) {
+    return dtype_ok(dtype) && dtype_ok(out_dtype) && V >= 1 && d >= 1 && d <= EMBED_MAX_COLS && ld >= d && ld < (int64_t)1 << 31 && ld_out >= d &&
+           ld_out < (int64_t)1 << 31 && std::isfinite(scale);
+}
+
+bool logp_ok(int64_t ld, int32_t dtype, int64_t rows, int32_t V, int32_t m, float temperature) {
+    return dtype_ok(dtype) && rows >= 0 && rows <= (int64_t)1 << 30 && V >= 1 && ld >= V && ld < (int64_t)1 << 31 && m >= 0 && m <= LOGP_MAX_GIVEN &&
+           temperature >= 1e-6f && temperature <= 1e6f;
+}
+
+bool list_ok(const void* const* arrays, const int64_t* counts, const int32_t* dtypes, int32_t n) {
+    if (n < 0 || n > LIST_MAX_GRADS || (n > 0 && (!arrays || !counts || !dtypes))) return false;
+    int64_t total = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        if (counts[i] < 0 || counts[i] > (int64_t)1 << 40 || !dtype_ok(dtypes[i]) || (total += counts[i]) > (int64_t)1 << 40) return false;
+        if (counts[i] && (!arrays[i] || !aligned(arrays[i], type_bytes(dtypes[i])))) return false;
+    }
+    return true;
+}
+
 }  // namespace
 
 extern "C" {
@@ -358,6 +378,63 @@ int moe_linear_fp8_wgrad(moe_ctx* c, const uint16_t* dy, int64_t rows, int32_t N
     if (!linear_grad_ok(c, rows, NOUT, K, offsets, E) || !dtype_ok(dtype) || !dW || !aligned(dW, 16)) return MOE_EINVAL;
     if (rows > 0 && (!dy || !xq || !xs || !aligned(dy, 16) || !aligned(xq, 16) || !aligned(xs, 4))) return MOE_EINVAL;
     return hip_rc(launch_linear_wgrad(c, dy, rows, NOUT, xq, xs, K, offsets, E, accumulate != 0, dtype, dW));
+}
+
+int moe_embed(moe_ctx* c, const int32_t* ids, int64_t T, const void* table, int32_t V, int32_t d, int64_t ld, int32_t dtype, float scale, void* y,
+              int64_t ld_y, int32_t out_dtype) {
+    if (!c || !embed_ok(V, d, ld, dtype, ld_y, out_dtype, scale) || T < 0 || T > (int64_t)1 << 30) return MOE_EINVAL;
+    if (T == 0) return MOE_OK;
+    if (!ids || !table || !y || !aligned(ids, 4) || !aligned(table, type_bytes(dtype)) || !aligned(y, type_bytes(out_dtype))) return MOE_EINVAL;
+    return hip_rc(launch_embed(c->stream, ids, T, table, V, d, ld, dtype, scale, y, ld_y, out_dtype));
+}
+
+int moe_embed_backward(moe_ctx* c, const void* dy, const int32_t* ids, int64_t T, int32_t V, int32_t d, int64_t ld, int32_t dtype, float scale,
+                       int32_t accumulate, void* dtable, int64_t ld_grad, int32_t grad_dtype) {
+    if (!c || !c->grad_ws || !embed_ok(V, d, ld, dtype, ld_grad, grad_dtype, scale) || T < 0 || T > EMBED_MAX_TOKENS) return MOE_EINVAL;
+    if (!dtable || !aligned(dtable, type_bytes(grad_dtype))) return MOE_EINVAL;
+    if (T > 0 && (!dy || !ids || !aligned(ids, 4) || !aligned(dy, type_bytes(dtype)))) return MOE_EINVAL;
+    return hip_rc(launch_embed_backward(c, dy, ids, T, V, d, ld, dtype, scale, accumulate != 0, dtable, ld_grad, grad_dtype));
+}
+
+int moe_token_logp(moe_ctx* c, const void* logits, int64_t ld, int32_t dtype, int64_t rows, int32_t V, const int32_t* ids, int32_t m, float temperature,
+                   float* logp, float* entropy, int32_t n, int32_t* top_idx, float* top_logp, float* stats) {
+    if (!c || !c->grad_ws || !logp_ok(ld, dtype, rows, V, m, temperature) || n < 0 || n > LOGP_MAX_TOP) return MOE_EINVAL;
+    if (rows == 0) return MOE_OK;
+    if (!logits || !aligned(logits, type_bytes(dtype)) || (m && (!ids || !logp)) || (n && (!top_idx || !top_logp))) return MOE_EINVAL;
+    if (!m && !n && !entropy && !stats) return MOE_EINVAL;
+    for (const void* p : {(const void*)ids, (const void*)logp, (const void*)entropy, (const void*)top_idx, (const void*)top_logp, (const void*)stats})
+        if (!aligned(p, 4)) return MOE_EINVAL;
+    return hip_rc(launch_token_logp(c, logits, ld, dtype, rows, V, ids, m, temperature, logp, entropy, n, top_idx, top_logp, stats));
+}
+
+int moe_token_logp_backward(moe_ctx* c, const void* logits, int64_t ld, int32_t dtype, int64_t rows, int32_t V, const int32_t* ids, int32_t m,
+                            float temperature, const float* dlogp, const float* dentropy, const float* stats, const float* entropy, void* dlogits,
+                            int64_t ld_grad, int32_t grad_dtype) {
+    if (!c || !logp_ok(ld, dtype, rows, V, m, temperature) || !dtype_ok(grad_dtype) || ld_grad < V || ld_grad >= (int64_t)1 << 31) return MOE_EINVAL;
+    if (rows == 0) return MOE_OK;
+    if (!logits || !dlogits || !stats || (m && (!ids || !dlogp)) || (dentropy && !entropy)) return MOE_EINVAL;
+    if (!aligned(logits, type_bytes(dtype)) || !aligned(dlogits, type_bytes(grad_dtype))) return MOE_EINVAL;
+    for (const void* p : {(const void*)ids, (const void*)dlogp, (const void*)dentropy, (const void*)stats, (const void*)entropy})
+        if (!aligned(p, 4)) return MOE_EINVAL;
+    if (dlogits == logits && (grad_dtype != dtype || ld_grad != ld)) return MOE_EINVAL;
+    return hip_rc(launch_token_logp_backward(c->stream, logits, ld, dtype, rows, V, ids, m, temperature, dlogp, dentropy, stats, entropy, dlogits, ld_grad,
+                                             grad_dtype));
+}
+
+int moe_grad_norm(moe_ctx* c, const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n, double* sum_sq, float* norm) {
+    if (!c || !c->grad_ws || !list_ok(grads, counts, dtypes, n) || !sum_sq || !aligned(sum_sq, 8) || !aligned(norm, 4)) return MOE_EINVAL;
+    return hip_rc(launch_grad_norm(c, grads, counts, dtypes, n, sum_sq, norm));
+}
+
+int moe_clip_grads(moe_ctx* c, const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n, const double* sum_sq, float max_norm,
+                   void* const* outs) {
+    if (!c || !list_ok(grads, counts, dtypes, n) || !sum_sq || !aligned(sum_sq, 8) || !(max_norm >= 0.f) || !std::isfinite(max_norm)) return MOE_EINVAL;
+    if (outs && n > 0 && !list_ok(outs, counts, dtypes, n)) return MOE_EINVAL;
+    for (int32_t i = 0; outs && i < n; ++i) {                  // (a gradient that is shifted onto itself)
+        const uintptr_t a = (uintptr_t)grads[i], b = (uintptr_t)outs[i], bytes = (uintptr_t)counts[i] * type_bytes(dtypes[i]);
+        if (a != b && (a > b ? a - b : b - a) < bytes) return MOE_EINVAL;
+    }
+    return hip_rc(launch_clip_grads(c->stream, grads, counts, dtypes, n, sum_sq, max_norm, outs));
 }
 
 int moe_profile_enable(moe_ctx* c, int32_t on) {

@@ -20,6 +20,9 @@ constexpr size_t GRAD_WS_BYTES = (size_t)64 << 20;
 constexpr int GRAD_TICKET_INTS = 32, GRAD_GROUPS = 64, GRAD_MAX_SPLIT_ROWS = 512;
 constexpr int GRAD_TICKETS = (1 + GRAD_GROUPS + GRAD_MAX_SPLIT_ROWS) * GRAD_TICKET_INTS;
 constexpr int NORM_MAX_COLS = 65536;
+constexpr int EMBED_MAX_COLS = 65536, EMBED_MAX_TOKENS = 1 << 21;  // (tokens: of the gradient, whose keys are sorted in the workspace)
+constexpr int LOGP_MAX_GIVEN = 64, LOGP_MAX_TOP = 64;
+constexpr int LIST_MAX_GRADS = 65536;
 
 }  // namespace moe355
 
@@ -139,6 +142,19 @@ hipError_t launch_linear_dgrad(moe_ctx* c, const uint16_t* dy, int64_t rows, int
                                const int32_t* offsets, int32_t E, uint16_t* dx);
 hipError_t launch_linear_wgrad(moe_ctx* c, const uint16_t* dy, int64_t rows, int32_t NOUT, const uint8_t* xq, const float* xs, int32_t K,
                                const int32_t* offsets, int32_t E, int32_t accumulate, int32_t dtype, void* dW);
+// The two ends of a policy step (embed.hip, token_logp.hip, clip.hip)
+hipError_t launch_embed(hipStream_t s, const int32_t* ids, int64_t T, const void* table, int32_t V, int32_t d, int64_t ld, int32_t dtype, float scale,
+                        void* y, int64_t ld_y, int32_t out_dtype);
+hipError_t launch_embed_backward(moe_ctx* c, const void* dy, const int32_t* ids, int64_t T, int32_t V, int32_t d, int64_t ld, int32_t dtype, float scale,
+                                 int32_t accumulate, void* dtable, int64_t ld_grad, int32_t grad_dtype);
+hipError_t launch_token_logp(moe_ctx* c, const void* logits, int64_t ld, int32_t dtype, int64_t rows, int32_t V, const int32_t* ids, int32_t m,
+                             float temperature, float* logp, float* entropy, int32_t n, int32_t* top_idx, float* top_logp, float* stats);
+hipError_t launch_token_logp_backward(hipStream_t s, const void* logits, int64_t ld, int32_t dtype, int64_t rows, int32_t V, const int32_t* ids, int32_t m,
+                                      float temperature, const float* dlogp, const float* dentropy, const float* stats, const float* entropy,
+                                      void* dlogits, int64_t ld_grad, int32_t grad_dtype);
+hipError_t launch_grad_norm(moe_ctx* c, const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n, double* sum_sq, float* norm);
+hipError_t launch_clip_grads(hipStream_t s, const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n, const double* sum_sq,
+                             float max_norm, void* const* outs);
 size_t route_workspace_bytes(int E, int d);
 size_t route_partial_bytes(int T, int E);
 hipError_t launch_combine(moe_ctx* c, const float* y_perm, const int32_t* inv_perm,
