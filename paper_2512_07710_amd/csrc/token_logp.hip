@@ -1,11 +1,17 @@
 // Log-probabilities of given tokens, entropy and the most likely tokens of rows of logits; and the logits' gradient from those of the first two.
 #include "softmax_rows.hpp"
+#include "ticket.hpp"
 
 namespace moe355 {
 namespace {
 
 constexpr int LOGP_THREADS = 256;
 constexpr int64_t LOGP_MAX_GRID = 1 << 22;
+constexpr int ROW_THREADS = 512, PART_THREADS = 256, MAX_PARTS = 64;       // blocks of whole rows and of parts of rows
+constexpr int AT_ONCE = 4;                     // vectors that a thread works on together
+constexpr int TOP_GROUPS = 64;                 // groups of a block's threads, whose largest logits make the bound for alternatives: at least LOGP_MAX_TOP
+constexpr int TOP_HELD = 1088;                 // logits that a block holds: LOGP_MAX_TOP and one for each thread at least
+const float ABOVE_LOWEST = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, LOWEST) - 1);
 
 struct logp_args {
     const void* logits;
@@ -15,6 +21,11 @@ struct logp_args {
     float inv_temp;
     float *logp, *entropy, *top_logp, *stats;
     int32_t* top_idx;
+    // rows in parts (few rows): their number, a power of two, and length in vectors, the parts' sums and largest logits, the rows' tickets
+    int parts, part_vecs;
+    float* part_sums;                          // [rows][parts][3]
+    uint64_t* part_tops;                       // [rows][parts][n]
+    int32_t* tickets;
 };
 
 // (v - m) / temperature - log s to fp32's resolution: in fp64, the logits as they are
@@ -23,31 +34,111 @@ __device__ inline float logp_of(float v, const softmax_stats& st, double log_s, 
     return (float)(((double)v - (double)st.m) * (double)inv_temp - log_s);
 }
 
-// One block per row.  The alternatives one after the other, each the largest behind the one before
-template <bool BF16>
-__global__ __launch_bounds__(LOGP_THREADS) void logp_kernel(const logp_args a) {
-    typedef row_type<BF16> T;
-    constexpr int N = T::N;
-    __shared__ block_scratch s_scratch;
-    __shared__ float s_v[LOGP_THREADS / 64];
-    __shared__ int s_i[LOGP_THREADS / 64];
-    const int64_t r = a.first + blockIdx.x;
-    const int tid = threadIdx.x, vecs = a.V / N, rest = a.V % N;
-    const void* const z = row_of<BF16>(a.logits, r * a.ld);
-    running_sums<BF16> sums(a.inv_temp * LOG2E);
-    for (int i = tid; i < vecs; i += LOGP_THREADS) {
-        const u32x4 v[1] = {T::load(z, i)};
-        sums.add(v);
+// A logit and its place
+struct place {
+    float v;
+    int i;
+};
+__device__ inline bool before(const place& a, const place& b) { return a.v > b.v || (a.v == b.v && a.i < b.i); }
+
+struct top_scratch {
+    float groups[TOP_GROUPS];
+    float bound;
+    int count;
+    place held[TOP_HELD], best[LOGP_MAX_TOP];
+};
+// over the lanes of a group of SIZE consecutive ones, in each of them
+template <int SIZE, class F>
+__device__ inline int over_group(int v, F f) {
+    static_assert(SIZE == 4 || SIZE == 8 || SIZE == 16, "lanes that one instruction reaches");
+    v = f(v, __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, true));     // quad_perm 1 0 3 2
+    v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, true));     // quad_perm 2 3 0 1
+    if (SIZE > 4) v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, true));      // row_half_mirror
+    if (SIZE > 8) v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x140, 0xf, 0xf, true));      // row_mirror
+    return v;
+}
+// The n-th largest of s.groups: n different logits are not below it.  And no masked logit reaches it.  Called by the whole block, which has written groups.
+template <int THREADS>
+__device__ inline float nth_of_groups(int n, top_scratch& s) {
+    constexpr int SIZE = THREADS / TOP_GROUPS;
+    __syncthreads();
+    const int i = threadIdx.x / SIZE, j0 = threadIdx.x % SIZE * (TOP_GROUPS / SIZE);
+    const place mine{s.groups[i], i};
+    int rank = 0;
+#pragma unroll
+    for (int j = 0; j < TOP_GROUPS / SIZE; ++j) rank += before(place{s.groups[j0 + j], j0 + j}, mine);
+    rank = over_group<SIZE>(rank, [](int a, int b) { return a + b; });
+    if (rank == n - 1 && j0 == 0) s.bound = mine.v;
+    __syncthreads();
+    return fmaxf(s.bound, ABOVE_LOWEST);
+}
+// (in any order: what is held in the end is the same)
+__device__ inline void hold(const place& p, top_scratch& s) {
+    const int slot = atomicAdd(&s.count, 1);
+    if (slot < TOP_HELD) s.held[slot] = p;
+}
+// The n first of the held ones in s.best, in order.  Called by the whole block, with a barrier before and behind it
+template <int THREADS>
+__device__ inline void rank_held(int count, int n, top_scratch& s) {
+    for (int c = threadIdx.x; c < count; c += THREADS) {
+        const place mine = s.held[c];
+        int rank = 0;
+        for (int k = 0; k < count; ++k) rank += before(s.held[k], mine);
+        if (rank < n) s.best[rank] = mine;
     }
-    if (tid < rest) sums.add_one(load1<BF16>(z, vecs * N + tid));
-    const softmax_stats st = block_join(sums.st, sums.c, s_scratch);
+}
+// Where too many logits reach the bound, all of them once more, THREADS at a time, with the bound of those before: at(i), i < count, in an order in which
+// equal ones ascend.  Returns how many are in s.best.
+template <int THREADS, class At>
+__device__ inline int select_all(int64_t count, int n, At at, top_scratch& s) {
+    __syncthreads();
+    if (threadIdx.x == 0) s.count = 0;
+    float bound = LOWEST;
+    int held = 0;
+    for (int64_t i = threadIdx.x; i - threadIdx.x < count; i += THREADS) {
+        __syncthreads();
+        const place p = i < count ? at(i) : place{-INFINITY, -1};
+        if (p.v > bound) hold(p, s);
+        __syncthreads();
+        const int now = s.count;
+        if (now == held) continue;             // (the same for the whole block)
+        held = now < n ? now : n;
+        rank_held<THREADS>(now, n, s);
+        __syncthreads();
+        if (threadIdx.x < held) s.held[threadIdx.x] = s.best[threadIdx.x];
+        if (threadIdx.x == 0) s.count = held;
+        if (held == n) bound = s.best[n - 1].v;
+    }
+    __syncthreads();
+    return held;
+}
+// The n first of what was held, or where that were too many, of all; in s.best.  Returns their number.
+template <int THREADS, class At>
+__device__ inline int select_top(int64_t all, int n, At at, top_scratch& s) {
+    __syncthreads();
+    const int count = s.count;
+    if (count > TOP_HELD) return select_all<THREADS>(all, n, at, s);
+    rank_held<THREADS>(count, n, s);
+    __syncthreads();
+    return count < n ? count : n;
+}
+
+// A row's results, from its sums and from `found` alternatives in s.best
+template <bool BF16>
+__device__ inline void write_row(const logp_args& a, int64_t r, const softmax_stats& st, int found, const top_scratch& s) {
+    const int tid = threadIdx.x;
+    if (tid >= a.m && tid >= a.n && tid > 0) return;
     const bool empty = st.m == -INFINITY && st.s == 0.f;
     const double log_s = st.s > 0.f && st.s < INFINITY ? log2_of(st.s) * LN2 : (double)logf(st.s);
     if (tid < a.m) {
         const int id = a.ids[r * a.m + tid];
         float lp = 0.f;
-        if ((uint32_t)id < (uint32_t)a.V) lp = empty ? -INFINITY : logp_of(load1<BF16>(z, id), st, log_s, a.inv_temp);
+        if ((uint32_t)id < (uint32_t)a.V) lp = empty ? -INFINITY : logp_of(load1<BF16>(row_of<BF16>(a.logits, r * a.ld), id), st, log_s, a.inv_temp);
         a.logp[r * a.m + tid] = lp;
+    }
+    if (tid < a.n) {
+        a.top_idx[r * a.n + tid] = tid < found ? s.best[tid].i : -1;
+        a.top_logp[r * a.n + tid] = tid < found ? logp_of(s.best[tid].v, st, log_s, a.inv_temp) : -INFINITY;
     }
     if (tid == 0) {
         if (a.entropy) a.entropy[r] = empty ? 0.f : (float)(log_s - (double)(st.u / st.s) * LN2);
@@ -56,33 +147,117 @@ __global__ __launch_bounds__(LOGP_THREADS) void logp_kernel(const logp_args a) {
             a.stats[2 * r + 1] = st.s;
         }
     }
-    float last = INFINITY;                     // the alternative before: its logit and place
-    int last_i = -1;
-    for (int k = 0; k < a.n; ++k) {
-        float best = LOWEST;
-        int best_i = -1;
-        for (int i = tid; i < a.V; i += LOGP_THREADS) {
-            const float v = load1<BF16>(z, i);
-            if (v > best && (v < last || (v == last && i > last_i))) best = v, best_i = i;
+}
+
+// One pass over a row, or a part of it, for the sums and the alternatives.  The n-th largest of the largest logits that 64 groups of threads have among
+// their first vectors bounds the alternatives from below, closely; what reaches the bound, a few times n logits, is held in LDS and ranked in the end.
+template <bool BF16, int THREADS, bool PARTS>
+__global__ __launch_bounds__(THREADS) void logp_kernel(const logp_args a) {
+    typedef row_type<BF16> T;
+    constexpr int N = T::N;
+    __shared__ block_scratch s_scratch;
+    __shared__ top_scratch s_top;
+    __shared__ int32_t s_last;
+    const int64_t r = PARTS ? blockIdx.x / a.parts : a.first + blockIdx.x;
+    const int part = PARTS ? blockIdx.x % a.parts : 0, tid = threadIdx.x, n = a.n, vecs = a.V / N;
+    const void* const z = row_of<BF16>(a.logits, r * a.ld);
+    const int begin = PARTS ? min(part * a.part_vecs, vecs) : 0, end = PARTS ? min(begin + a.part_vecs, vecs) : vecs;
+    const int last = !PARTS || part == a.parts - 1 ? a.V : end * N;        // (the last part has the elements behind the vectors)
+    running_sums<BF16> sums(a.inv_temp * LOG2E);
+    float bound = NAN;                         // (without alternatives: nothing reaches it)
+    auto hold_above = [&](const u32x4(&v)[AT_ONCE], int i) {
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u)
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (T::at(v[u], j) >= bound) hold(place{T::at(v[u], j), (i + u * THREADS) * N + j}, s_top);
+    };
+    auto load = [&](u32x4(&v)[AT_ONCE], int i) {
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) v[u] = i + u * THREADS < end ? T::load(z, i + u * THREADS) : T::none();
+    };
+    int i = begin + tid;
+    u32x4 v[AT_ONCE];
+    load(v, i);
+    const float extra = end * N + tid < last ? load1<BF16>(z, end * N + tid) : -INFINITY;
+    float top = sums.largest(v);
+    if (n) {
+        const float g = __int_as_float(over_group<THREADS / TOP_GROUPS>(
+            __float_as_int(fmaxf(top, extra)), [](int x, int y) { return __float_as_int(fmaxf(__int_as_float(x), __int_as_float(y))); }));
+        if (tid % (THREADS / TOP_GROUPS) == 0) s_top.groups[tid / (THREADS / TOP_GROUPS)] = g;
+        if (tid == 0) s_top.count = 0;
+        bound = nth_of_groups<THREADS>(n, s_top);
+        if (extra >= bound) hold(place{extra, end * N + tid}, s_top);
+    }
+    for (;;) {
+        sums.take(top);
+        sums.sum(v);
+        if (top >= bound) hold_above(v, i);
+        i += AT_ONCE * THREADS;
+        if (i - tid >= end) break;
+        load(v, i);
+        top = sums.largest(v);
+    }
+    sums.add_one(extra);
+    softmax_stats st = block_join(sums.st, sums.c, s_scratch);
+    int found = n ? select_top<THREADS>(last - begin * N, n, [&](int64_t k) { return place{load1<BF16>(z, begin * N + k), (int)(begin * N + k)}; }, s_top) : 0;
+    if (PARTS) {
+        float* const mine = a.part_sums + (r * a.parts + part) * 3;
+        uint64_t* const tops = a.part_tops + r * a.parts * n;
+        if (tid == 0) {
+            __hip_atomic_store(mine, st.m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(mine + 1, st.s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(mine + 2, st.u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
-        auto better = [&](float v, int i) {
-            if (v > best || (v == best && i >= 0 && i < best_i)) best = v, best_i = i;
-        };
-        for (int o = 32; o > 0; o >>= 1) {
-            const float v = __shfl_xor(best, o);
-            better(v, __shfl_xor(best_i, o));
+        if (tid < n) {
+            const place p = tid < found ? s_top.best[tid] : place{-INFINITY, -1};
+            __hip_atomic_store(tops + part * n + tid, (uint64_t)__float_as_uint(p.v) << 32 | (uint32_t)p.i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
-        if ((tid & 63) == 0) s_v[tid >> 6] = best, s_i[tid >> 6] = best_i;
-        __syncthreads();
-        for (int w = 0; w < LOGP_THREADS / 64; ++w) better(s_v[w], s_i[w]);
+        if (!last_block(a.tickets + (1 + GRAD_GROUPS + r) * GRAD_TICKET_INTS, a.parts, s_last)) return;
+        const float* const all = a.part_sums + r * a.parts * 3;
+        if (tid < 64) {                        // (at most 64 parts: a lane has one)
+            st = softmax_stats{-INFINITY, 0.f, 0.f};
+            if (tid < a.parts)
+                st = softmax_stats{__hip_atomic_load(all + tid * 3, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
+                                   __hip_atomic_load(all + tid * 3 + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
+                                   __hip_atomic_load(all + tid * 3 + 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)};
+            const float m = wave_largest(st.m);
+            if (m > -INFINITY) rebase(st, m, sums.c);
+            st = softmax_stats{m, wave_total(st.s), wave_total(st.u)};
+        }
+        if (n) {
+            // the parts' lists as one: the bound from the first of each
+            auto at = [&](int64_t k) {
+                const uint64_t p = __hip_atomic_load(tops + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                return place{__uint_as_float((uint32_t)(p >> 32)), (int)(uint32_t)p};
+            };
+            const int firsts = TOP_GROUPS / a.parts;           // of each part
+            if (tid < TOP_GROUPS) s_top.groups[tid] = tid % firsts < n ? at(tid / firsts * n + tid % firsts).v : -INFINITY;
+            if (tid == 0) s_top.count = 0;
+            bound = nth_of_groups<THREADS>(n, s_top);
+            for (int k = tid; k < a.parts * n; k += THREADS) {
+                const place p = at(k);
+                if (p.v >= bound) hold(p, s_top);
+            }
+            found = select_top<THREADS>(a.parts * n, n, at, s_top);
+        }
         __syncthreads();
         if (tid == 0) {
-            a.top_idx[r * a.n + k] = best_i;
-            a.top_logp[r * a.n + k] = best_i < 0 ? -INFINITY : logp_of(best, st, log_s, a.inv_temp);
+            s_scratch.a[0] = st.m;
+            s_scratch.b[0] = st.s;
+            s_scratch.a[1] = st.u;
         }
-        last = best;
-        last_i = best_i;
+        __syncthreads();
+        st = softmax_stats{s_scratch.a[0], s_scratch.b[0], s_scratch.a[1]};
     }
+    write_row<BF16>(a, r, st, found, s_top);
+}
+
+// Parts of a row: long rows that alone leave much of the chip idle
+int logp_parts(int64_t rows, int vecs) {
+    int parts = 1;
+    while (parts < MAX_PARTS && rows * parts * 2 <= 1024 && vecs / (parts * 2) >= PART_THREADS && rows <= GRAD_MAX_SPLIT_ROWS) parts *= 2;
+    return parts;
 }
 
 struct logp_grad_args {
@@ -152,10 +327,10 @@ __global__ __launch_bounds__(LOGP_THREADS) void logp_grad_kernel(const logp_grad
     }
 }
 
-template <class Kernel, class Args>
+template <int THREADS, class Kernel, class Args>
 hipError_t launch_rows(hipStream_t s, Kernel kernel, Args a) {
     for (a.first = 0; a.first < a.rows; a.first += LOGP_MAX_GRID)
-        hipLaunchKernelGGL(kernel, dim3((unsigned)(a.rows - a.first < LOGP_MAX_GRID ? a.rows - a.first : LOGP_MAX_GRID)), dim3(LOGP_THREADS), 0, s, a);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(a.rows - a.first < LOGP_MAX_GRID ? a.rows - a.first : LOGP_MAX_GRID)), dim3(THREADS), 0, s, a);
     return hipGetLastError();
 }
 
@@ -163,16 +338,30 @@ hipError_t launch_rows(hipStream_t s, Kernel kernel, Args a) {
 
 hipError_t launch_token_logp(moe_ctx* c, const void* logits, int64_t ld, int32_t dtype, int64_t rows, int32_t V, const int32_t* ids, int32_t m,
                              float temperature, float* logp, float* entropy, int32_t n, int32_t* top_idx, float* top_logp, float* stats) {
-    const logp_args a{logits, ld, rows, 0, V, m, n, ids, 1.0f / temperature, logp, entropy, top_logp, stats, top_idx};
-    return dtype == MOE_BF16 ? launch_rows(c->stream, logp_kernel<true>, a) : launch_rows(c->stream, logp_kernel<false>, a);
+    logp_args a{logits, ld, rows, 0, V, m, n, ids, 1.0f / temperature, logp, entropy, top_logp, stats, top_idx};
+    const int vecs = V / (dtype == MOE_BF16 ? 8 : 4), parts = logp_parts(rows, vecs);
+    if (parts > 1) {
+        static_assert((size_t)GRAD_MAX_SPLIT_ROWS * MAX_PARTS * (3 * sizeof(float) + LOGP_MAX_TOP * sizeof(uint64_t)) <= GRAD_WS_BYTES, "room for all parts");
+        a.parts = parts;
+        a.part_vecs = (vecs + parts - 1) / parts;
+        a.part_tops = static_cast<uint64_t*>(c->grad_ws);
+        a.part_sums = reinterpret_cast<float*>(a.part_tops + (int64_t)GRAD_MAX_SPLIT_ROWS * MAX_PARTS * LOGP_MAX_TOP);
+        a.tickets = c->grad_tickets;
+        const unsigned grid = (unsigned)(rows * parts);
+        if (dtype == MOE_BF16) logp_kernel<true, PART_THREADS, true><<<grid, PART_THREADS, 0, c->stream>>>(a);
+        else logp_kernel<false, PART_THREADS, true><<<grid, PART_THREADS, 0, c->stream>>>(a);
+        return hipGetLastError();
+    }
+    return dtype == MOE_BF16 ? launch_rows<ROW_THREADS>(c->stream, logp_kernel<true, ROW_THREADS, false>, a)
+                             : launch_rows<ROW_THREADS>(c->stream, logp_kernel<false, ROW_THREADS, false>, a);
 }
 
 hipError_t launch_token_logp_backward(hipStream_t s, const void* logits, int64_t ld, int32_t dtype, int64_t rows, int32_t V, const int32_t* ids, int32_t m,
                                       float temperature, const float* dlogp, const float* dentropy, const float* stats, const float* entropy,
                                       void* dlogits, int64_t ld_grad, int32_t grad_dtype) {
     const logp_grad_args a{logits, ld, ld_grad, rows, 0, V, m, ids, 1.0f / temperature, dlogp, dentropy, stats, entropy, dlogits};
-    if (dtype == MOE_BF16) return grad_dtype == MOE_BF16 ? launch_rows(s, logp_grad_kernel<true, true>, a) : launch_rows(s, logp_grad_kernel<true, false>, a);
-    return grad_dtype == MOE_BF16 ? launch_rows(s, logp_grad_kernel<false, true>, a) : launch_rows(s, logp_grad_kernel<false, false>, a);
+    if (dtype == MOE_BF16) return grad_dtype == MOE_BF16 ? launch_rows<LOGP_THREADS>(s, logp_grad_kernel<true, true>, a) : launch_rows<LOGP_THREADS>(s, logp_grad_kernel<true, false>, a);
+    return grad_dtype == MOE_BF16 ? launch_rows<LOGP_THREADS>(s, logp_grad_kernel<false, true>, a) : launch_rows<LOGP_THREADS>(s, logp_grad_kernel<false, false>, a);
 }
 
 }  // namespace moe355
