@@ -7,7 +7,7 @@ namespace {
 
 constexpr int LOGP_THREADS = 256;
 constexpr int64_t LOGP_MAX_GRID = 1 << 22;
-constexpr int ROW_THREADS = 512, PART_THREADS = 256, MAX_PARTS = 64;       // blocks of whole rows and of parts of rows
+constexpr int PART_THREADS = 256, MAX_PARTS = 64;   // rows in parts: a block's threads, parts of a row at most
 constexpr int AT_ONCE = 4;                     // vectors that a thread works on together
 constexpr int TOP_GROUPS = 64;                 // groups of a block's threads, whose largest logits make the bound for alternatives: at least LOGP_MAX_TOP
 constexpr int TOP_HELD = 1088;                 // logits that a block holds: LOGP_MAX_TOP and one for each thread at least
@@ -34,6 +34,9 @@ __device__ inline float logp_of(float v, const softmax_stats& st, double log_s, 
     return (float)(((double)v - (double)st.m) * (double)inv_temp - log_s);
 }
 
+// the next fp32 number (+inf: NaN, which nothing reaches)
+__device__ inline float next_above(float v) { return __int_as_float(v == 0.f ? 1 : __float_as_int(v) + (v > 0.f ? 1 : -1)); }
+
 // A logit and its place
 struct place {
     float v;
@@ -50,42 +53,79 @@ struct top_scratch {
 // over the lanes of a group of SIZE consecutive ones, in each of them
 template <int SIZE, class F>
 __device__ inline int over_group(int v, F f) {
-    static_assert(SIZE == 4 || SIZE == 8 || SIZE == 16, "lanes that one instruction reaches");
-    v = f(v, __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, true));     // quad_perm 1 0 3 2
-    v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, true));     // quad_perm 2 3 0 1
+    static_assert(SIZE == 1 || SIZE == 2 || SIZE == 4 || SIZE == 8 || SIZE == 16, "lanes that one instruction reaches");
+    if (SIZE > 1) v = f(v, __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, true));       // quad_perm 1 0 3 2
+    if (SIZE > 2) v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, true));       // quad_perm 2 3 0 1
     if (SIZE > 4) v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, true));      // row_half_mirror
     if (SIZE > 8) v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x140, 0xf, 0xf, true));      // row_mirror
     return v;
 }
-// The n-th largest of s.groups: n different logits are not below it.  And no masked logit reaches it.  Called by the whole block, which has written groups.
+// Each group's largest into s.groups, from its threads'
+template <int THREADS>
+__device__ inline void group_largest(float v, top_scratch& s) {
+    constexpr int SIZE = THREADS / TOP_GROUPS;
+    const int g = over_group<SIZE>(__float_as_int(v), [](int x, int y) { return __float_as_int(fmaxf(__int_as_float(x), __int_as_float(y))); });
+    if (threadIdx.x % SIZE == 0) s.groups[threadIdx.x / SIZE] = __int_as_float(g);
+}
+// The n-th largest of s.groups: n different logits are not below it.  Called by the whole block, which has written groups.
 template <int THREADS>
 __device__ inline float nth_of_groups(int n, top_scratch& s) {
     constexpr int SIZE = THREADS / TOP_GROUPS;
     __syncthreads();
-    const int i = threadIdx.x / SIZE, j0 = threadIdx.x % SIZE * (TOP_GROUPS / SIZE);
+    const int i = threadIdx.x / SIZE, j0 = threadIdx.x % SIZE;
     const place mine{s.groups[i], i};
     int rank = 0;
 #pragma unroll
-    for (int j = 0; j < TOP_GROUPS / SIZE; ++j) rank += before(place{s.groups[j0 + j], j0 + j}, mine);
-    rank = over_group<SIZE>(rank, [](int a, int b) { return a + b; });
+    for (int j = 0; j < TOP_GROUPS; j += SIZE) rank += before(place{s.groups[j + j0], j + j0}, mine);
+    rank = over_group<SIZE>(rank, [](int x, int y) { return x + y; });
     if (rank == n - 1 && j0 == 0) s.bound = mine.v;
     __syncthreads();
-    return fmaxf(s.bound, ABOVE_LOWEST);
+    return s.bound;
 }
 // (in any order: what is held in the end is the same)
 __device__ inline void hold(const place& p, top_scratch& s) {
     const int slot = atomicAdd(&s.count, 1);
     if (slot < TOP_HELD) s.held[slot] = p;
 }
-// The n first of the held ones in s.best, in order.  Called by the whole block, with a barrier before and behind it
+// The n first of the held ones in s.best, in order: SIZE threads count who is before one.  Called by the whole block, with a barrier before and behind it
 template <int THREADS>
 __device__ inline void rank_held(int count, int n, top_scratch& s) {
-    for (int c = threadIdx.x; c < count; c += THREADS) {
-        const place mine = s.held[c];
+    constexpr int SIZE = THREADS / TOP_GROUPS;
+    const int i = threadIdx.x / SIZE, j0 = threadIdx.x % SIZE;
+    if (threadIdx.x < TOP_GROUPS && (count & -TOP_GROUPS) + (int)threadIdx.x >= count && count % TOP_GROUPS)
+        s.held[(count & -TOP_GROUPS) + threadIdx.x] = place{-INFINITY, 0x7FFFFFFF};        // (behind all)
+    __syncthreads();
+    for (int i0 = 0; i0 < count; i0 += TOP_GROUPS) {
+        const place mine = s.held[i0 + i];
         int rank = 0;
-        for (int k = 0; k < count; ++k) rank += before(s.held[k], mine);
-        if (rank < n) s.best[rank] = mine;
+        for (int k0 = 0; k0 < count; k0 += TOP_GROUPS)
+#pragma unroll
+            for (int k = 0; k < TOP_GROUPS; k += SIZE) rank += before(s.held[k0 + k + j0], mine);
+        rank = over_group<SIZE>(rank, [](int x, int y) { return x + y; });
+        if (j0 == 0 && rank < n && i0 + i < count) s.best[rank] = mine;
     }
+}
+// Many held ones: a bound from the largest of 64 groups of them leaves little more than n.  Returns how many.
+template <int THREADS>
+__device__ inline int thin_held(int count, int n, top_scratch& s) {
+    constexpr int EACH = (TOP_HELD + THREADS - 1) / THREADS;
+    place mine[EACH];
+    float top = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        const int k = threadIdx.x + e * THREADS;
+        mine[e] = k < count ? s.held[k] : place{-INFINITY, 0};
+        top = fmaxf(top, mine[e].v);
+    }
+    group_largest<THREADS>(top, s);
+    const float bound = fmaxf(nth_of_groups<THREADS>(n, s), ABOVE_LOWEST);
+    if (threadIdx.x == 0) s.count = 0;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+        if (mine[e].v >= bound) hold(mine[e], s);
+    __syncthreads();
+    return s.count;
 }
 // Where too many logits reach the bound, all of them once more, THREADS at a time, with the bound of those before: at(i), i < count, in an order in which
 // equal ones ascend.  Returns how many are in s.best.
@@ -103,6 +143,7 @@ __device__ inline int select_all(int64_t count, int n, At at, top_scratch& s) {
         const int now = s.count;
         if (now == held) continue;             // (the same for the whole block)
         held = now < n ? now : n;
+        __syncthreads();
         rank_held<THREADS>(now, n, s);
         __syncthreads();
         if (threadIdx.x < held) s.held[threadIdx.x] = s.best[threadIdx.x];
@@ -116,8 +157,10 @@ __device__ inline int select_all(int64_t count, int n, At at, top_scratch& s) {
 template <int THREADS, class At>
 __device__ inline int select_top(int64_t all, int n, At at, top_scratch& s) {
     __syncthreads();
-    const int count = s.count;
+    int count = s.count;
     if (count > TOP_HELD) return select_all<THREADS>(all, n, at, s);
+    if (count > 2 * TOP_GROUPS) count = thin_held<THREADS>(count, n, s);
+    __syncthreads();
     rank_held<THREADS>(count, n, s);
     __syncthreads();
     return count < n ? count : n;
@@ -152,7 +195,7 @@ __device__ inline void write_row(const logp_args& a, int64_t r, const softmax_st
 // One pass over a row, or a part of it, for the sums and the alternatives.  The n-th largest of the largest logits that 64 groups of threads have among
 // their first vectors bounds the alternatives from below, closely; what reaches the bound, a few times n logits, is held in LDS and ranked in the end.
 template <bool BF16, int THREADS, bool PARTS>
-__global__ __launch_bounds__(THREADS) void logp_kernel(const logp_args a) {
+__global__ __launch_bounds__(THREADS, 8) void logp_kernel(const logp_args a) {
     typedef row_type<BF16> T;
     constexpr int N = T::N;
     __shared__ block_scratch s_scratch;
@@ -164,7 +207,7 @@ __global__ __launch_bounds__(THREADS) void logp_kernel(const logp_args a) {
     const int begin = PARTS ? min(part * a.part_vecs, vecs) : 0, end = PARTS ? min(begin + a.part_vecs, vecs) : vecs;
     const int last = !PARTS || part == a.parts - 1 ? a.V : end * N;        // (the last part has the elements behind the vectors)
     running_sums<BF16> sums(a.inv_temp * LOG2E);
-    float bound = NAN;                         // (without alternatives: nothing reaches it)
+    float bound = NAN;                         // what an alternative reaches (without alternatives nothing does)
     auto hold_above = [&](const u32x4(&v)[AT_ONCE], int i) {
 #pragma unroll
         for (int u = 0; u < AT_ONCE; ++u)
@@ -182,17 +225,19 @@ __global__ __launch_bounds__(THREADS) void logp_kernel(const logp_args a) {
     const float extra = end * N + tid < last ? load1<BF16>(z, end * N + tid) : -INFINITY;
     float top = sums.largest(v);
     if (n) {
-        const float g = __int_as_float(over_group<THREADS / TOP_GROUPS>(
-            __float_as_int(fmaxf(top, extra)), [](int x, int y) { return __float_as_int(fmaxf(__int_as_float(x), __int_as_float(y))); }));
-        if (tid % (THREADS / TOP_GROUPS) == 0) s_top.groups[tid / (THREADS / TOP_GROUPS)] = g;
+        group_largest<THREADS>(top, s_top);
         if (tid == 0) s_top.count = 0;
         bound = nth_of_groups<THREADS>(n, s_top);
-        if (extra >= bound) hold(place{extra, end * N + tid}, s_top);
     }
+    // n of the first vectors' logits are not below the bound, so an equal one behind them has n before it
+    float behind = bound > LOWEST ? next_above(bound) : bound == bound ? ABOVE_LOWEST : bound;
+    bound = bound == bound ? fmaxf(bound, ABOVE_LOWEST) : bound;
+    if (extra >= behind) hold(place{extra, end * N + tid}, s_top);
     for (;;) {
         sums.take(top);
         sums.sum(v);
         if (top >= bound) hold_above(v, i);
+        bound = behind;
         i += AT_ONCE * THREADS;
         if (i - tid >= end) break;
         load(v, i);
@@ -234,7 +279,7 @@ __global__ __launch_bounds__(THREADS) void logp_kernel(const logp_args a) {
             const int firsts = TOP_GROUPS / a.parts;           // of each part
             if (tid < TOP_GROUPS) s_top.groups[tid] = tid % firsts < n ? at(tid / firsts * n + tid % firsts).v : -INFINITY;
             if (tid == 0) s_top.count = 0;
-            bound = nth_of_groups<THREADS>(n, s_top);
+            bound = fmaxf(nth_of_groups<THREADS>(n, s_top), ABOVE_LOWEST);
             for (int k = tid; k < a.parts * n; k += THREADS) {
                 const place p = at(k);
                 if (p.v >= bound) hold(p, s_top);
@@ -268,17 +313,20 @@ struct logp_grad_args {
     float inv_temp;
     const float *dlogp, *dentropy, *stats, *entropy;
     void* dlogits;
+    int parts, part_vecs;
 };
 
-// dz[v] = (sum_j dlogp_j (1[v = id_j] - p_v) - dH p_v (log p_v + H)) / temperature = 2^y (a y + b), and more at the given tokens.  One block per row
+// dz[v] = (sum_j dlogp_j (1[v = id_j] - p_v) - dH p_v (log p_v + H)) / temperature = 2^y (a y + b), and more at the given tokens.  A block has a row or, of
+// few rows, a part of one: the row's sums are there already.
 template <bool BF16, bool GRAD_BF16>
 __global__ __launch_bounds__(LOGP_THREADS) void logp_grad_kernel(const logp_grad_args a) {
     typedef row_type<BF16> T;
     constexpr int N = T::N;
     __shared__ float s_d[LOGP_MAX_GIVEN], s_v[LOGP_MAX_GIVEN];
     __shared__ int s_id[LOGP_MAX_GIVEN];
-    const int64_t r = a.first + blockIdx.x;
-    const int tid = threadIdx.x, vecs = a.V / N, rest = a.V % N;
+    const int64_t b = a.first + blockIdx.x, r = b / a.parts;
+    const int part = (int)(b % a.parts), tid = threadIdx.x, vecs = a.V / N;
+    const int begin = min(part * a.part_vecs, vecs), end = min(begin + a.part_vecs, vecs), last = part == a.parts - 1 ? a.V : end * N;
     const void* const z = row_of<BF16>(a.logits, r * a.ld);
     void* const out = row_of<GRAD_BF16>(a.dlogits, r * a.ld_grad);
     const float m = a.stats[2 * r], s = a.stats[2 * r + 1], dH = a.dentropy ? a.dentropy[r] : 0.f;
@@ -290,7 +338,8 @@ __global__ __launch_bounds__(LOGP_THREADS) void logp_grad_kernel(const logp_grad
         s_v[tid] = v;
         s_d[tid] = d;
     }
-    const float extra = tid < rest ? load1<BF16>(z, vecs * N + tid) : 0.f;
+    const int behind = end * N + tid;                          // an element behind the vectors
+    const float extra = behind < last ? load1<BF16>(z, behind) : 0.f;
     __syncthreads();
     float sum = 0.f;
     bool live = dH != 0.f;
@@ -299,6 +348,12 @@ __global__ __launch_bounds__(LOGP_THREADS) void logp_grad_kernel(const logp_grad
         live |= s_d[j] != 0.f;
     }
     live &= !(m == -INFINITY && s == 0.f);
+    if (!live) {                               // (the same for the whole block)
+        const float none[N] = {};
+        for (int i = begin + tid; i < end; i += LOGP_THREADS) store_grad<GRAD_BF16, N>(out, i, none);
+        if (behind < last) store1<GRAD_BF16>(out, behind, 0.f);
+        return;
+    }
     const float c = a.inv_temp * LOG2E, scale = a.inv_temp / s;
     const double log_s = s > 0.f && s < INFINITY ? log2_of(s) * LN2 : (double)logf(s), H = dH != 0.f ? (double)a.entropy[r] : 0.0;
     const float ka = (float)(-(double)dH * LN2) * scale, kb = (float)((double)dH * (log_s - H) - (double)sum) * scale;
@@ -306,21 +361,26 @@ __global__ __launch_bounds__(LOGP_THREADS) void logp_grad_kernel(const logp_grad
         const float y = (v - m) * c;
         return __builtin_amdgcn_exp2f(y) * fmaf(ka, fmaxf(y, Y_LOWEST), kb);
     };
-    for (int i = tid; i < vecs; i += LOGP_THREADS) {
-        float g[N] = {};
-        if (live) {
-            const u32x4 v = T::load(z, i);
+    auto put = [&](const u32x4& v, int i) {
+        float g[N];
 #pragma unroll
-            for (int j = 0; j < N; ++j) g[j] = of(T::at(v, j));
-        }
+        for (int j = 0; j < N; ++j) g[j] = of(T::at(v, j));
         store_grad<GRAD_BF16, N>(out, i, g);
+    };
+    int i = begin + tid;
+    for (; i + (AT_ONCE - 1) * LOGP_THREADS < end; i += AT_ONCE * LOGP_THREADS) {
+        u32x4 v[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) v[u] = T::load(z, i + u * LOGP_THREADS);
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) put(v[u], i + u * LOGP_THREADS);
     }
-    if (tid < rest) store1<GRAD_BF16>(out, vecs * N + tid, live ? of(extra) : 0.f);
-    if (!live) return;
+    for (; i < end; i += LOGP_THREADS) put(T::load(z, i), i);
+    if (behind < last) store1<GRAD_BF16>(out, behind, of(extra));
     // the given tokens, by the threads that have written their places: one with several gradients receives their sum as often
     for (int j = 0; j < a.m; ++j) {
         const int id = s_id[j];
-        if ((uint32_t)id >= (uint32_t)a.V || (id < vecs * N ? (id / N) % LOGP_THREADS : id - vecs * N) != tid || s_v[j] <= LOWEST) continue;
+        if (id < begin * N || id >= last || (id < end * N ? (id / N - begin) % LOGP_THREADS : id - end * N) != tid || s_v[j] <= LOWEST) continue;
         float d = 0.f;
         for (int k = 0; k < a.m; ++k) d += s_id[k] == id ? s_d[k] : 0.f;
         store1<GRAD_BF16>(out, id, fmaf(d, a.inv_temp, of(s_v[j])));
@@ -328,10 +388,17 @@ __global__ __launch_bounds__(LOGP_THREADS) void logp_grad_kernel(const logp_grad
 }
 
 template <int THREADS, class Kernel, class Args>
-hipError_t launch_rows(hipStream_t s, Kernel kernel, Args a) {
-    for (a.first = 0; a.first < a.rows; a.first += LOGP_MAX_GRID)
-        hipLaunchKernelGGL(kernel, dim3((unsigned)(a.rows - a.first < LOGP_MAX_GRID ? a.rows - a.first : LOGP_MAX_GRID)), dim3(THREADS), 0, s, a);
+hipError_t launch_rows(hipStream_t s, Kernel kernel, Args a, int64_t blocks) {
+    for (a.first = 0; a.first < blocks; a.first += LOGP_MAX_GRID)
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks - a.first < LOGP_MAX_GRID ? blocks - a.first : LOGP_MAX_GRID)), dim3(THREADS), 0, s, a);
     return hipGetLastError();
+}
+
+template <bool BF16>
+hipError_t launch_whole(hipStream_t s, const logp_args& a, int vecs) {
+    if (vecs <= 64 * AT_ONCE) return launch_rows<64>(s, logp_kernel<BF16, 64, false>, a, a.rows);
+    if (vecs <= 256 * AT_ONCE) return launch_rows<256>(s, logp_kernel<BF16, 256, false>, a, a.rows);
+    return launch_rows<512>(s, logp_kernel<BF16, 512, false>, a, a.rows);
 }
 
 }  // namespace
@@ -352,16 +419,26 @@ hipError_t launch_token_logp(moe_ctx* c, const void* logits, int64_t ld, int32_t
         else logp_kernel<false, PART_THREADS, true><<<grid, PART_THREADS, 0, c->stream>>>(a);
         return hipGetLastError();
     }
-    return dtype == MOE_BF16 ? launch_rows<ROW_THREADS>(c->stream, logp_kernel<true, ROW_THREADS, false>, a)
-                             : launch_rows<ROW_THREADS>(c->stream, logp_kernel<false, ROW_THREADS, false>, a);
+    return dtype == MOE_BF16 ? launch_whole<true>(c->stream, a, vecs) : launch_whole<false>(c->stream, a, vecs);
 }
 
 hipError_t launch_token_logp_backward(hipStream_t s, const void* logits, int64_t ld, int32_t dtype, int64_t rows, int32_t V, const int32_t* ids, int32_t m,
                                       float temperature, const float* dlogp, const float* dentropy, const float* stats, const float* entropy,
                                       void* dlogits, int64_t ld_grad, int32_t grad_dtype) {
-    const logp_grad_args a{logits, ld, ld_grad, rows, 0, V, m, ids, 1.0f / temperature, dlogp, dentropy, stats, entropy, dlogits};
-    if (dtype == MOE_BF16) return grad_dtype == MOE_BF16 ? launch_rows<LOGP_THREADS>(s, logp_grad_kernel<true, true>, a) : launch_rows<LOGP_THREADS>(s, logp_grad_kernel<true, false>, a);
-    return grad_dtype == MOE_BF16 ? launch_rows<LOGP_THREADS>(s, logp_grad_kernel<false, true>, a) : launch_rows<LOGP_THREADS>(s, logp_grad_kernel<false, false>, a);
+    logp_grad_args a{logits, ld, ld_grad, rows, 0, V, m, ids, 1.0f / temperature, dlogp, dentropy, stats, entropy, dlogits, 1, V};
+    const int vecs = V / (dtype == MOE_BF16 ? 8 : 4);
+    // parts of a row, each a round of vectors or more (in place a row's given tokens are read before any of the row is written, by one block)
+    if (dlogits != logits && rows < 2048) {
+        const int64_t parts = vecs / (AT_ONCE * LOGP_THREADS) < 2048 / rows ? vecs / (AT_ONCE * LOGP_THREADS) : 2048 / rows;
+        if (parts > 1) a.parts = (int)parts;
+        a.part_vecs = (vecs + a.parts - 1) / a.parts;
+    }
+    const int64_t n = rows * a.parts;
+    if (dtype == MOE_BF16)
+        return grad_dtype == MOE_BF16 ? launch_rows<LOGP_THREADS>(s, logp_grad_kernel<true, true>, a, n)
+                                      : launch_rows<LOGP_THREADS>(s, logp_grad_kernel<true, false>, a, n);
+    return grad_dtype == MOE_BF16 ? launch_rows<LOGP_THREADS>(s, logp_grad_kernel<false, true>, a, n)
+                                  : launch_rows<LOGP_THREADS>(s, logp_grad_kernel<false, false>, a, n);
 }
 
 }  // namespace moe355
