@@ -34,21 +34,27 @@ __device__ inline float logp_of(float v, const softmax_stats& st, double log_s, 
     return (float)(((double)v - (double)st.m) * (double)inv_temp - log_s);
 }
 
-// the next fp32 number (+inf: NaN, which nothing reaches)
-__device__ inline float next_above(float v) { return __int_as_float(v == 0.f ? 1 : __float_as_int(v) + (v > 0.f ? 1 : -1)); }
+// the next fp32 number (of +inf and NaN: NaN, which nothing reaches)
+__device__ inline float next_above(float v) { return v != v ? v : __int_as_float(v == 0.f ? 1 : __float_as_int(v) + (v > 0.f ? 1 : -1)); }
 
-// A logit and its place
-struct place {
-    float v;
-    int i;
-};
-__device__ inline bool before(const place& a, const place& b) { return a.v > b.v || (a.v == b.v && a.i < b.i); }
+// A logit and its place as one number: of two, the one that comes first among the alternatives is larger.  0 is below all
+__device__ inline uint32_t ordered(float v) {
+    const uint32_t b = __float_as_uint(v + 0.f);               // (-0 is equal to 0)
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ inline uint64_t key_of(float v, int i) { return (uint64_t)ordered(v) << 32 | (uint32_t)~i; }
+__device__ inline uint64_t key_unless_nan(float v, int i) { return v == v ? key_of(v, i) : 0; }
+__device__ inline float value_of(uint64_t key) {
+    const uint32_t o = (uint32_t)(key >> 32);
+    return __uint_as_float(o ^ (o >> 31 ? 0x80000000u : 0xFFFFFFFFu));
+}
+__device__ inline int index_of(uint64_t key) { return ~(int)(uint32_t)key; }
 
 struct top_scratch {
     float groups[TOP_GROUPS];
     float bound;
     int count;
-    place held[TOP_HELD], best[LOGP_MAX_TOP];
+    uint64_t held[TOP_HELD], best[LOGP_MAX_TOP];
 };
 // over the lanes of a group of SIZE consecutive ones, in each of them
 template <int SIZE, class F>
@@ -73,19 +79,24 @@ __device__ inline float nth_of_groups(int n, top_scratch& s) {
     constexpr int SIZE = THREADS / TOP_GROUPS;
     __syncthreads();
     const int i = threadIdx.x / SIZE, j0 = threadIdx.x % SIZE;
-    const place mine{s.groups[i], i};
+    const float mine = s.groups[i];
     int rank = 0;
 #pragma unroll
-    for (int j = 0; j < TOP_GROUPS; j += SIZE) rank += before(place{s.groups[j + j0], j + j0}, mine);
+    for (int j = 0; j < TOP_GROUPS; j += SIZE) {               // (no branches: the reads go out together)
+        const float v = s.groups[j + j0];
+        rank += (int)(v > mine) | ((int)(v == mine) & (int)(j + j0 < i));
+    }
     rank = over_group<SIZE>(rank, [](int x, int y) { return x + y; });
-    if (rank == n - 1 && j0 == 0) s.bound = mine.v;
+    if (rank == n - 1 && j0 == 0) s.bound = mine;
     __syncthreads();
     return s.bound;
 }
+// what keys of logits from a bound on are not below; masked ones never are
+__device__ inline uint64_t bound_key(float bound) { return (uint64_t)ordered(fmaxf(bound, ABOVE_LOWEST)) << 32; }
 // (in any order: what is held in the end is the same)
-__device__ inline void hold(const place& p, top_scratch& s) {
+__device__ inline void hold(uint64_t key, top_scratch& s) {
     const int slot = atomicAdd(&s.count, 1);
-    if (slot < TOP_HELD) s.held[slot] = p;
+    if (slot < TOP_HELD) s.held[slot] = key;
 }
 // The n first of the held ones in s.best, in order: SIZE threads count who is before one.  Called by the whole block, with a barrier before and behind it
 template <int THREADS>
@@ -93,14 +104,14 @@ __device__ inline void rank_held(int count, int n, top_scratch& s) {
     constexpr int SIZE = THREADS / TOP_GROUPS;
     const int i = threadIdx.x / SIZE, j0 = threadIdx.x % SIZE;
     if (threadIdx.x < TOP_GROUPS && (count & -TOP_GROUPS) + (int)threadIdx.x >= count && count % TOP_GROUPS)
-        s.held[(count & -TOP_GROUPS) + threadIdx.x] = place{-INFINITY, 0x7FFFFFFF};        // (behind all)
+        s.held[(count & -TOP_GROUPS) + threadIdx.x] = 0;
     __syncthreads();
     for (int i0 = 0; i0 < count; i0 += TOP_GROUPS) {
-        const place mine = s.held[i0 + i];
+        const uint64_t mine = s.held[i0 + i];
         int rank = 0;
         for (int k0 = 0; k0 < count; k0 += TOP_GROUPS)
 #pragma unroll
-            for (int k = 0; k < TOP_GROUPS; k += SIZE) rank += before(s.held[k0 + k + j0], mine);
+            for (int k = 0; k < TOP_GROUPS; k += SIZE) rank += s.held[k0 + k + j0] > mine;
         rank = over_group<SIZE>(rank, [](int x, int y) { return x + y; });
         if (j0 == 0 && rank < n && i0 + i < count) s.best[rank] = mine;
     }
@@ -108,37 +119,31 @@ __device__ inline void rank_held(int count, int n, top_scratch& s) {
 // Many held ones: a bound from the largest of 64 groups of them leaves little more than n.  Returns how many.
 template <int THREADS>
 __device__ inline int thin_held(int count, int n, top_scratch& s) {
-    constexpr int EACH = (TOP_HELD + THREADS - 1) / THREADS;
-    place mine[EACH];
-    float top = -INFINITY;
-#pragma unroll
-    for (int e = 0; e < EACH; ++e) {
-        const int k = threadIdx.x + e * THREADS;
-        mine[e] = k < count ? s.held[k] : place{-INFINITY, 0};
-        top = fmaxf(top, mine[e].v);
-    }
-    group_largest<THREADS>(top, s);
-    const float bound = fmaxf(nth_of_groups<THREADS>(n, s), ABOVE_LOWEST);
+    uint64_t top = 0;
+    for (int k = threadIdx.x; k < count; k += THREADS) top = s.held[k] > top ? s.held[k] : top;
+    group_largest<THREADS>(top ? value_of(top) : -INFINITY, s);
+    const uint64_t bound = bound_key(nth_of_groups<THREADS>(n, s));
     if (threadIdx.x == 0) s.count = 0;
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < EACH; ++e)
-        if (mine[e].v >= bound) hold(mine[e], s);
+    for (int k0 = 0; k0 < count; k0 += THREADS) {              // (into places that have been read)
+        const uint64_t key = k0 + (int)threadIdx.x < count ? s.held[k0 + threadIdx.x] : 0;
+        __syncthreads();
+        if (key >= bound) hold(key, s);
+    }
     __syncthreads();
     return s.count;
 }
-// Where too many logits reach the bound, all of them once more, THREADS at a time, with the bound of those before: at(i), i < count, in an order in which
-// equal ones ascend.  Returns how many are in s.best.
+// Where too many logits reach the bound, all of them once more, THREADS at a time, with the last of the n first before them as the bound: at(i), i < count.
+// Returns how many are in s.best.
 template <int THREADS, class At>
 __device__ inline int select_all(int64_t count, int n, At at, top_scratch& s) {
     __syncthreads();
     if (threadIdx.x == 0) s.count = 0;
-    float bound = LOWEST;
+    uint64_t bound = bound_key(LOWEST);
     int held = 0;
     for (int64_t i = threadIdx.x; i - threadIdx.x < count; i += THREADS) {
         __syncthreads();
-        const place p = i < count ? at(i) : place{-INFINITY, -1};
-        if (p.v > bound) hold(p, s);
+        const uint64_t key = i < count ? at(i) : 0;
+        if (key > bound) hold(key, s);
         __syncthreads();
         const int now = s.count;
         if (now == held) continue;             // (the same for the whole block)
@@ -148,7 +153,7 @@ __device__ inline int select_all(int64_t count, int n, At at, top_scratch& s) {
         __syncthreads();
         if (threadIdx.x < held) s.held[threadIdx.x] = s.best[threadIdx.x];
         if (threadIdx.x == 0) s.count = held;
-        if (held == n) bound = s.best[n - 1].v;
+        if (held == n) bound = s.best[n - 1];
     }
     __syncthreads();
     return held;
@@ -180,8 +185,8 @@ __device__ inline void write_row(const logp_args& a, int64_t r, const softmax_st
         a.logp[r * a.m + tid] = lp;
     }
     if (tid < a.n) {
-        a.top_idx[r * a.n + tid] = tid < found ? s.best[tid].i : -1;
-        a.top_logp[r * a.n + tid] = tid < found ? logp_of(s.best[tid].v, st, log_s, a.inv_temp) : -INFINITY;
+        a.top_idx[r * a.n + tid] = tid < found ? index_of(s.best[tid]) : -1;
+        a.top_logp[r * a.n + tid] = tid < found ? logp_of(value_of(s.best[tid]), st, log_s, a.inv_temp) : -INFINITY;
     }
     if (tid == 0) {
         if (a.entropy) a.entropy[r] = empty ? 0.f : (float)(log_s - (double)(st.u / st.s) * LN2);
@@ -208,44 +213,71 @@ __global__ __launch_bounds__(THREADS, 8) void logp_kernel(const logp_args a) {
     const int last = !PARTS || part == a.parts - 1 ? a.V : end * N;        // (the last part has the elements behind the vectors)
     running_sums<BF16> sums(a.inv_temp * LOG2E);
     float bound = NAN;                         // what an alternative reaches (without alternatives nothing does)
-    auto hold_above = [&](const u32x4(&v)[AT_ONCE], int i) {
+    // the logits of these vectors that reach the bound; tops: the largest of each
+    auto hold_above = [&](const u32x4(&v)[AT_ONCE], const float(&tops)[AT_ONCE], int i) {
 #pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u)
+        for (int u = 0; u < AT_ONCE; ++u) {
+            if (!(tops[u] >= bound)) continue;
+            uint32_t above = 0;                // a bit for each element.  Few lanes have one, seldom more
 #pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (T::at(v[u], j) >= bound) hold(place{T::at(v[u], j), (i + u * THREADS) * N + j}, s_top);
+            for (int e = 0; e < N; ++e) above |= (uint32_t)(T::at(v[u], e) >= bound) << e;
+            while (above) {
+                const int at = __builtin_ctz(above);
+                float x = T::at(v[u], 0);
+#pragma unroll
+                for (int e = 1; e < N; ++e) x = e == at ? T::at(v[u], e) : x;
+                hold(key_of(x, (i + u * THREADS) * N + at), s_top);
+                above &= above - 1;
+            }
+        }
+    };
+    auto largest = [&](const u32x4(&v)[AT_ONCE], float(&tops)[AT_ONCE]) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const u32x4 one[1] = {v[u]};
+            tops[u] = sums.largest(one);
+            top = fmaxf(top, tops[u]);
+        }
+        return top;
     };
     auto load = [&](u32x4(&v)[AT_ONCE], int i) {
 #pragma unroll
         for (int u = 0; u < AT_ONCE; ++u) v[u] = i + u * THREADS < end ? T::load(z, i + u * THREADS) : T::none();
     };
     int i = begin + tid;
-    u32x4 v[AT_ONCE];
-    load(v, i);
     const float extra = end * N + tid < last ? load1<BF16>(z, end * N + tid) : -INFINITY;
-    float top = sums.largest(v);
-    if (n) {
-        group_largest<THREADS>(top, s_top);
-        if (tid == 0) s_top.count = 0;
-        bound = nth_of_groups<THREADS>(n, s_top);
-    }
-    // n of the first vectors' logits are not below the bound, so an equal one behind them has n before it
-    float behind = bound > LOWEST ? next_above(bound) : bound == bound ? ABOVE_LOWEST : bound;
-    bound = bound == bound ? fmaxf(bound, ABOVE_LOWEST) : bound;
-    if (extra >= behind) hold(place{extra, end * N + tid}, s_top);
-    for (;;) {
+    {
+        u32x4 v[AT_ONCE];
+        float tops[AT_ONCE];
+        load(v, i);
+        const float top = largest(v, tops);
+        if (n) {
+            group_largest<THREADS>(top, s_top);
+            if (tid == 0) s_top.count = 0;
+            bound = fmaxf(nth_of_groups<THREADS>(n, s_top), LOWEST);
+        }
         sums.take(top);
         sums.sum(v);
-        if (top >= bound) hold_above(v, i);
+        // n of the first vectors' logits are not below the bound, so one behind them that equals it has n before it
+        const float behind = next_above(bound);
+        bound = bound > LOWEST ? bound : behind;
+        if (top >= bound) hold_above(v, tops, i);
         bound = behind;
-        i += AT_ONCE * THREADS;
-        if (i - tid >= end) break;
-        load(v, i);
-        top = sums.largest(v);
     }
+    for (i += AT_ONCE * THREADS; i - tid < end; i += AT_ONCE * THREADS) {
+        u32x4 v[AT_ONCE];
+        float tops[AT_ONCE];
+        load(v, i);
+        const float top = largest(v, tops);
+        sums.take(top);
+        sums.sum(v);
+        if (top >= bound) hold_above(v, tops, i);
+    }
+    if (extra >= bound) hold(key_of(extra, end * N + tid), s_top);
     sums.add_one(extra);
     softmax_stats st = block_join(sums.st, sums.c, s_scratch);
-    int found = n ? select_top<THREADS>(last - begin * N, n, [&](int64_t k) { return place{load1<BF16>(z, begin * N + k), (int)(begin * N + k)}; }, s_top) : 0;
+    int found = n ? select_top<THREADS>(last - begin * N, n, [&](int64_t k) { return key_unless_nan(load1<BF16>(z, begin * N + k), (int)(begin * N + k)); }, s_top) : 0;
     if (PARTS) {
         float* const mine = a.part_sums + (r * a.parts + part) * 3;
         uint64_t* const tops = a.part_tops + r * a.parts * n;
@@ -255,11 +287,16 @@ __global__ __launch_bounds__(THREADS, 8) void logp_kernel(const logp_args a) {
             __hip_atomic_store(mine + 2, st.u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
         if (tid < n) {
-            const place p = tid < found ? s_top.best[tid] : place{-INFINITY, -1};
-            __hip_atomic_store(tops + part * n + tid, (uint64_t)__float_as_uint(p.v) << 32 | (uint32_t)p.i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            const uint64_t key = tid < found ? s_top.best[tid] : 0;
+            __hip_atomic_store(tops + part * n + tid, key, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
         if (!last_block(a.tickets + (1 + GRAD_GROUPS + r) * GRAD_TICKET_INTS, a.parts, s_last)) return;
         const float* const all = a.part_sums + r * a.parts * 3;
+        auto at = [&](int64_t k) { return __hip_atomic_load(tops + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+        constexpr int EACH = MAX_PARTS * LOGP_MAX_TOP / THREADS;
+        uint64_t theirs[EACH];                 // (all on their way at a time)
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) theirs[e] = tid + e * THREADS < a.parts * n ? at(tid + e * THREADS) : 0;
         if (tid < 64) {                        // (at most 64 parts: a lane has one)
             st = softmax_stats{-INFINITY, 0.f, 0.f};
             if (tid < a.parts)
@@ -272,18 +309,19 @@ __global__ __launch_bounds__(THREADS, 8) void logp_kernel(const logp_args a) {
         }
         if (n) {
             // the parts' lists as one: the bound from the first of each
-            auto at = [&](int64_t k) {
-                const uint64_t p = __hip_atomic_load(tops + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                return place{__uint_as_float((uint32_t)(p >> 32)), (int)(uint32_t)p};
-            };
             const int firsts = TOP_GROUPS / a.parts;           // of each part
-            if (tid < TOP_GROUPS) s_top.groups[tid] = tid % firsts < n ? at(tid / firsts * n + tid % firsts).v : -INFINITY;
+            if (tid < TOP_GROUPS) s_top.groups[tid] = -INFINITY;
             if (tid == 0) s_top.count = 0;
-            bound = fmaxf(nth_of_groups<THREADS>(n, s_top), ABOVE_LOWEST);
-            for (int k = tid; k < a.parts * n; k += THREADS) {
-                const place p = at(k);
-                if (p.v >= bound) hold(p, s_top);
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                const int k = tid + e * THREADS;
+                if (k < a.parts * n && k % n < firsts) s_top.groups[k / n * firsts + k % n] = theirs[e] ? value_of(theirs[e]) : -INFINITY;
             }
+            const uint64_t first = bound_key(nth_of_groups<THREADS>(n, s_top));
+#pragma unroll
+            for (int e = 0; e < EACH; ++e)
+                if (theirs[e] >= first) hold(theirs[e], s_top);
             found = select_top<THREADS>(a.parts * n, n, at, s_top);
         }
         __syncthreads();
@@ -301,7 +339,7 @@ __global__ __launch_bounds__(THREADS, 8) void logp_kernel(const logp_args a) {
 // Parts of a row: long rows that alone leave much of the chip idle
 int logp_parts(int64_t rows, int vecs) {
     int parts = 1;
-    while (parts < MAX_PARTS && rows * parts * 2 <= 1024 && vecs / (parts * 2) >= PART_THREADS && rows <= GRAD_MAX_SPLIT_ROWS) parts *= 2;
+    while (parts < MAX_PARTS && rows * parts * 2 <= 1024 && vecs / (parts * 2) >= AT_ONCE * PART_THREADS && rows <= GRAD_MAX_SPLIT_ROWS) parts *= 2;
     return parts;
 }
 
