@@ -7,7 +7,8 @@ namespace {
 
 constexpr int LOGP_THREADS = 256;
 constexpr int64_t LOGP_MAX_GRID = 1 << 22;
-constexpr int PART_THREADS = 256, MAX_PARTS = 64;   // rows in parts: a block's threads, parts of a row at most
+constexpr int FEW_THREADS = 512, PART_THREADS = 1024, FEW_ROWS_IN_PARTS = 32, MAX_PARTS = 64; // rows in parts: a block's threads, parts of a row at most
+constexpr int MAX_SPLIT_ROWS = 128;            // (two parts or more in 256 blocks)
 constexpr int AT_ONCE = 4;                     // vectors that a thread works on together
 constexpr int TOP_GROUPS = 64;                 // groups of a block's threads, whose largest logits make the bound for alternatives: at least LOGP_MAX_TOP
 constexpr int TOP_HELD = 1088;                 // logits that a block holds: LOGP_MAX_TOP and one for each thread at least
@@ -336,10 +337,12 @@ __global__ __launch_bounds__(THREADS, 8) void logp_kernel(const logp_args a) {
     write_row<BF16>(a, r, st, found, s_top);
 }
 
-// Parts of a row: long rows that alone leave much of the chip idle
-int logp_parts(int64_t rows, int vecs) {
+// Parts of a row, for long rows that alone leave much of the chip idle; a row's end, its tickets and the joining, then comes twice, 4 us.  So only up to 128 rows
+// (n = 8, bf16 x 131072: 120 rows 16.5 whole, 14.8 in parts; 256 rows 18 and 24; 333 x 50001 f32 17.5 and 22), in one block for each CU; very few rows in
+// smaller blocks, which end sooner (n = 20, 4 x 131072 f32 9.6 -> 9.3, 16 x 131072 bf16 10.9 -> 9.9, but 40 rows 11.2 -> 11.9).
+int logp_parts(int64_t rows, int vecs, int threads) {
     int parts = 1;
-    while (parts < MAX_PARTS && rows * parts * 2 <= 1024 && vecs / (parts * 2) >= AT_ONCE * PART_THREADS && rows <= GRAD_MAX_SPLIT_ROWS) parts *= 2;
+    while (parts < MAX_PARTS && rows * parts * 2 <= (threads == FEW_THREADS ? 512 : 256) && vecs / (parts * 2) >= AT_ONCE * threads) parts *= 2;
     return parts;
 }
 
@@ -432,10 +435,13 @@ hipError_t launch_rows(hipStream_t s, Kernel kernel, Args a, int64_t blocks) {
     return hipGetLastError();
 }
 
+// Threads of a whole row's block: a vector or more each.  1024 where the blocks are about as many as the CUs hold at a time (256 x 131072 bf16, n = 8 18.3 us, with
+// 512 21.9; 2000 x 50001 61 and 53)
 template <bool BF16>
 hipError_t launch_whole(hipStream_t s, const logp_args& a, int vecs) {
     if (vecs <= 64 * AT_ONCE) return launch_rows<64>(s, logp_kernel<BF16, 64, false>, a, a.rows);
     if (vecs <= 256 * AT_ONCE) return launch_rows<256>(s, logp_kernel<BF16, 256, false>, a, a.rows);
+    if (vecs > 1024 * AT_ONCE && a.rows <= 640) return launch_rows<1024>(s, logp_kernel<BF16, 1024, false>, a, a.rows);
     return launch_rows<512>(s, logp_kernel<BF16, 512, false>, a, a.rows);
 }
 
@@ -444,18 +450,19 @@ hipError_t launch_whole(hipStream_t s, const logp_args& a, int vecs) {
 hipError_t launch_token_logp(moe_ctx* c, const void* logits, int64_t ld, int32_t dtype, int64_t rows, int32_t V, const int32_t* ids, int32_t m,
                              float temperature, float* logp, float* entropy, int32_t n, int32_t* top_idx, float* top_logp, float* stats) {
     logp_args a{logits, ld, rows, 0, V, m, n, ids, 1.0f / temperature, logp, entropy, top_logp, stats, top_idx};
-    const int vecs = V / (dtype == MOE_BF16 ? 8 : 4), parts = logp_parts(rows, vecs);
+    const int vecs = V / (dtype == MOE_BF16 ? 8 : 4), threads = rows <= FEW_ROWS_IN_PARTS ? FEW_THREADS : PART_THREADS, parts = logp_parts(rows, vecs, threads);
     if (parts > 1) {
-        static_assert((size_t)GRAD_MAX_SPLIT_ROWS * MAX_PARTS * (3 * sizeof(float) + LOGP_MAX_TOP * sizeof(uint64_t)) <= GRAD_WS_BYTES, "room for all parts");
+        static_assert((size_t)MAX_SPLIT_ROWS * MAX_PARTS * (3 * sizeof(float) + LOGP_MAX_TOP * sizeof(uint64_t)) <= GRAD_WS_BYTES && MAX_SPLIT_ROWS <= GRAD_MAX_SPLIT_ROWS, "room for all parts");
         a.parts = parts;
         a.part_vecs = (vecs + parts - 1) / parts;
         a.part_tops = static_cast<uint64_t*>(c->grad_ws);
-        a.part_sums = reinterpret_cast<float*>(a.part_tops + (int64_t)GRAD_MAX_SPLIT_ROWS * MAX_PARTS * LOGP_MAX_TOP);
+        a.part_sums = reinterpret_cast<float*>(a.part_tops + (int64_t)MAX_SPLIT_ROWS * MAX_PARTS * LOGP_MAX_TOP);
         a.tickets = c->grad_tickets;
-        const unsigned grid = (unsigned)(rows * parts);
-        if (dtype == MOE_BF16) logp_kernel<true, PART_THREADS, true><<<grid, PART_THREADS, 0, c->stream>>>(a);
-        else logp_kernel<false, PART_THREADS, true><<<grid, PART_THREADS, 0, c->stream>>>(a);
-        return hipGetLastError();
+        if (threads == FEW_THREADS)
+            return dtype == MOE_BF16 ? launch_rows<FEW_THREADS>(c->stream, logp_kernel<true, FEW_THREADS, true>, a, rows * parts)
+                                     : launch_rows<FEW_THREADS>(c->stream, logp_kernel<false, FEW_THREADS, true>, a, rows * parts);
+        return dtype == MOE_BF16 ? launch_rows<PART_THREADS>(c->stream, logp_kernel<true, PART_THREADS, true>, a, rows * parts)
+                                 : launch_rows<PART_THREADS>(c->stream, logp_kernel<false, PART_THREADS, true>, a, rows * parts);
     }
     return dtype == MOE_BF16 ? launch_whole<true>(c->stream, a, vecs) : launch_whole<false>(c->stream, a, vecs);
 }
