@@ -11,7 +11,7 @@ constexpr int FEW_THREADS = 512, PART_THREADS = 1024, FEW_ROWS_IN_PARTS = 32, MA
 constexpr int MAX_SPLIT_ROWS = 128;            // (two parts or more in 256 blocks)
 constexpr int AT_ONCE = 4;                     // vectors that a thread works on together
 constexpr int TOP_GROUPS = 64;                 // groups of a block's threads, whose largest logits make the bound for alternatives: at least LOGP_MAX_TOP
-constexpr int TOP_HELD = 1088;                 // logits that a block holds: LOGP_MAX_TOP and one for each thread at least
+constexpr int top_held(int threads) { return threads > 64 ? 1088 : 320; }  // logits that a block holds: LOGP_MAX_TOP and one for each thread at least
 const float ABOVE_LOWEST = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, LOWEST) - 1);
 
 struct logp_args {
@@ -51,11 +51,13 @@ __device__ inline float value_of(uint64_t key) {
 }
 __device__ inline int index_of(uint64_t key) { return ~(int)(uint32_t)key; }
 
+template <int THREADS>
 struct top_scratch {
+    static constexpr int HELD = top_held(THREADS);
     float groups[TOP_GROUPS];
     float bound;
     int count;
-    uint64_t held[TOP_HELD], best[LOGP_MAX_TOP];
+    uint64_t held[HELD], best[LOGP_MAX_TOP];
 };
 // over the lanes of a group of SIZE consecutive ones, in each of them
 template <int SIZE, class F>
@@ -69,14 +71,14 @@ __device__ inline int over_group(int v, F f) {
 }
 // Each group's largest into s.groups, from its threads'
 template <int THREADS>
-__device__ inline void group_largest(float v, top_scratch& s) {
+__device__ inline void group_largest(float v, top_scratch<THREADS>& s) {
     constexpr int SIZE = THREADS / TOP_GROUPS;
     const int g = over_group<SIZE>(__float_as_int(v), [](int x, int y) { return __float_as_int(fmaxf(__int_as_float(x), __int_as_float(y))); });
     if (threadIdx.x % SIZE == 0) s.groups[threadIdx.x / SIZE] = __int_as_float(g);
 }
 // The n-th largest of s.groups: n different logits are not below it.  Called by the whole block, which has written groups.
 template <int THREADS>
-__device__ inline float nth_of_groups(int n, top_scratch& s) {
+__device__ inline float nth_of_groups(int n, top_scratch<THREADS>& s) {
     constexpr int SIZE = THREADS / TOP_GROUPS;
     __syncthreads();
     const int i = threadIdx.x / SIZE, j0 = threadIdx.x % SIZE;
@@ -95,13 +97,14 @@ __device__ inline float nth_of_groups(int n, top_scratch& s) {
 // what keys of logits from a bound on are not below; masked ones never are
 __device__ inline uint64_t bound_key(float bound) { return (uint64_t)ordered(fmaxf(bound, ABOVE_LOWEST)) << 32; }
 // (in any order: what is held in the end is the same)
-__device__ inline void hold(uint64_t key, top_scratch& s) {
+template <int THREADS>
+__device__ inline void hold(uint64_t key, top_scratch<THREADS>& s) {
     const int slot = atomicAdd(&s.count, 1);
-    if (slot < TOP_HELD) s.held[slot] = key;
+    if (slot < s.HELD) s.held[slot] = key;
 }
 // The n first of the held ones in s.best, in order: SIZE threads count who is before one.  Called by the whole block, with a barrier before and behind it
 template <int THREADS>
-__device__ inline void rank_held(int count, int n, top_scratch& s) {
+__device__ inline void rank_held(int count, int n, top_scratch<THREADS>& s) {
     constexpr int SIZE = THREADS / TOP_GROUPS;
     const int i = threadIdx.x / SIZE, j0 = threadIdx.x % SIZE;
     if (threadIdx.x < TOP_GROUPS && (count & -TOP_GROUPS) + (int)threadIdx.x >= count && count % TOP_GROUPS)
@@ -119,7 +122,7 @@ __device__ inline void rank_held(int count, int n, top_scratch& s) {
 }
 // Many held ones: a bound from the largest of 64 groups of them leaves little more than n.  Returns how many.
 template <int THREADS>
-__device__ inline int thin_held(int count, int n, top_scratch& s) {
+__device__ inline int thin_held(int count, int n, top_scratch<THREADS>& s) {
     uint64_t top = 0;
     for (int k = threadIdx.x; k < count; k += THREADS) top = s.held[k] > top ? s.held[k] : top;
     group_largest<THREADS>(top ? value_of(top) : -INFINITY, s);
@@ -136,7 +139,7 @@ __device__ inline int thin_held(int count, int n, top_scratch& s) {
 // Where too many logits reach the bound, all of them once more, THREADS at a time, with the last of the n first before them as the bound: at(i), i < count.
 // Returns how many are in s.best.
 template <int THREADS, class At>
-__device__ inline int select_all(int64_t count, int n, At at, top_scratch& s) {
+__device__ inline int select_all(int64_t count, int n, At at, top_scratch<THREADS>& s) {
     __syncthreads();
     if (threadIdx.x == 0) s.count = 0;
     uint64_t bound = bound_key(LOWEST);
@@ -161,10 +164,10 @@ __device__ inline int select_all(int64_t count, int n, At at, top_scratch& s) {
 }
 // The n first of what was held, or where that were too many, of all; in s.best.  Returns their number.
 template <int THREADS, class At>
-__device__ inline int select_top(int64_t all, int n, At at, top_scratch& s) {
+__device__ inline int select_top(int64_t all, int n, At at, top_scratch<THREADS>& s) {
     __syncthreads();
     int count = s.count;
-    if (count > TOP_HELD) return select_all<THREADS>(all, n, at, s);
+    if (count > s.HELD) return select_all<THREADS>(all, n, at, s);
     if (count > 2 * TOP_GROUPS) count = thin_held<THREADS>(count, n, s);
     __syncthreads();
     rank_held<THREADS>(count, n, s);
@@ -173,8 +176,8 @@ __device__ inline int select_top(int64_t all, int n, At at, top_scratch& s) {
 }
 
 // A row's results, from its sums and from `found` alternatives in s.best
-template <bool BF16>
-__device__ inline void write_row(const logp_args& a, int64_t r, const softmax_stats& st, int found, const top_scratch& s) {
+template <bool BF16, int THREADS>
+__device__ inline void write_row(const logp_args& a, int64_t r, const softmax_stats& st, int found, const top_scratch<THREADS>& s) {
     const int tid = threadIdx.x;
     if (tid >= a.m && tid >= a.n && tid > 0) return;
     const bool empty = st.m == -INFINITY && st.s == 0.f;
@@ -205,7 +208,7 @@ __global__ __launch_bounds__(THREADS, 8) void logp_kernel(const logp_args a) {
     typedef row_type<BF16> T;
     constexpr int N = T::N;
     __shared__ block_scratch s_scratch;
-    __shared__ top_scratch s_top;
+    __shared__ top_scratch<THREADS> s_top;
     __shared__ int32_t s_last;
     const int64_t r = PARTS ? blockIdx.x / a.parts : a.first + blockIdx.x;
     const int part = PARTS ? blockIdx.x % a.parts : 0, tid = threadIdx.x, n = a.n, vecs = a.V / N;
@@ -382,12 +385,10 @@ __global__ __launch_bounds__(LOGP_THREADS) void logp_grad_kernel(const logp_grad
     const int behind = end * N + tid;                          // an element behind the vectors
     const float extra = behind < last ? load1<BF16>(z, behind) : 0.f;
     __syncthreads();
-    float sum = 0.f;
-    bool live = dH != 0.f;
-    for (int j = 0; j < a.m; ++j) {
-        sum += s_d[j];
-        live |= s_d[j] != 0.f;
-    }
+    const int lane = tid & 63;                                 // (each wave has the given tokens, one to a lane)
+    const int id = lane < a.m ? s_id[lane] : -1;
+    const float d = lane < a.m ? s_d[lane] : 0.f, v_id = lane < a.m ? s_v[lane] : 0.f, sum = wave_total(d);
+    bool live = dH != 0.f || __ballot(d != 0.f) != 0;          // (NaN is not zero)
     live &= !(m == -INFINITY && s == 0.f);
     if (!live) {                               // (the same for the whole block)
         const float none[N] = {};
@@ -419,12 +420,12 @@ __global__ __launch_bounds__(LOGP_THREADS) void logp_grad_kernel(const logp_grad
     for (; i < end; i += LOGP_THREADS) put(T::load(z, i), i);
     if (behind < last) store1<GRAD_BF16>(out, behind, of(extra));
     // the given tokens, by the threads that have written their places: one with several gradients receives their sum as often
-    for (int j = 0; j < a.m; ++j) {
-        const int id = s_id[j];
-        if (id < begin * N || id >= last || (id < end * N ? (id / N - begin) % LOGP_THREADS : id - end * N) != tid || s_v[j] <= LOWEST) continue;
-        float d = 0.f;
-        for (int k = 0; k < a.m; ++k) d += s_id[k] == id ? s_d[k] : 0.f;
-        store1<GRAD_BF16>(out, id, fmaf(d, a.inv_temp, of(s_v[j])));
+    const int owner = id < end * N ? (id / N - begin) % LOGP_THREADS : id - end * N;
+    const bool here = id >= begin * N && id < last && owner >> 6 == tid >> 6 && !(v_id <= LOWEST);
+    for (uint64_t left = __ballot(here); left; left &= left - 1) {
+        const int j = __builtin_ctzll(left), to = __builtin_amdgcn_readlane(id, j);
+        const float more = wave_total(id == to ? d : 0.f), v = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v_id), j));
+        if (tid == __builtin_amdgcn_readlane(owner, j)) store1<GRAD_BF16>(out, to, fmaf(more, a.inv_temp, of(v)));
     }
 }
 
