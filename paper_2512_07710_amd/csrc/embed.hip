@@ -1,82 +1,315 @@
 // Rows of an embedding table for token ids, and the table's gradient by sorted tokens.
 #include "grad_common.hpp"
+#include "ticket.hpp"
 
 namespace moe355 {
 namespace {
 
-constexpr int EMBED_THREADS = 256, EMBED_MAX_GRID = 1 << 22;
-constexpr int SORT_CHUNK = 1024, MERGE_WAYS = 32;
-constexpr uint64_t NO_KEY = ~(uint64_t)0;      // behind every key
-constexpr uint32_t NO_ID = 0xFFFFFFFFu;        // of the keys of tokens outside the table: behind the others
+constexpr int EMBED_THREADS = 256;
+constexpr int64_t EMBED_MAX_GRID = 1 << 22;
+constexpr int FEW_TOKENS = 1024, FEW_RUN = 64;         // tokens that need no sorting, rows of one token that one block adds up
+constexpr int SORT_THREADS = 1024, SORT_EACH = 4, SORT_CHUNK = SORT_THREADS * SORT_EACH, MERGE_WAYS = 32;
+constexpr int ZERO_BITS = 4096;                        // rows that a block clears at most
+constexpr uint32_t NO_ID = 0xFFFFFFFFu;                // of tokens outside the table: behind the others
 
-// Eight columns of a row from column i on, those that there are
-template <bool BF16>
-__device__ inline vec8 row_load8(const void* row, int64_t i, int d) {
-    if (i + 8 <= d) {
-        raw8<BF16> r;
-        r.load(row, i);
-        vec8 v;
+// W columns of a row, as they lie in memory, at any element.  Rows are read once: past the caches
+typedef u32x2 __attribute__((aligned(2))) u32x2_odd;
+template <bool BF16, int W>
+struct columns {
+    static constexpr int WORDS = W * (BF16 ? 2 : 4) / 4;
+    uint32_t w[WORDS];
+    template <bool PAST = true>
+    __device__ void load(const void* row, int64_t i, int d) {
+        const char* const at = static_cast<const char*>(row) + i * (BF16 ? 2 : 4);
+        if (i + W <= d) {
+            if (WORDS == 4) {
+                const u32x4_any* const p = reinterpret_cast<const u32x4_any*>(at);
+                const u32x4 v = PAST ? __builtin_nontemporal_load(p) : *p;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v.v[j] = r.at(j);
-        return v;
+                for (int j = 0; j < WORDS; ++j) w[j] = v[j & 3];
+            } else {
+                const u32x2_odd* const p = reinterpret_cast<const u32x2_odd*>(at);
+                const u32x2 v = PAST ? __builtin_nontemporal_load(p) : *p;
+#pragma unroll
+                for (int j = 0; j < WORDS; ++j) w[j] = v[j & 1];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < WORDS; ++j) w[j] = 0;
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                if (i + j < d) {
+                    const uint32_t b = BF16 ? (uint32_t) static_cast<const uint16_t*>(row)[i + j] << (j & 1) * 16 : static_cast<const uint32_t*>(row)[i + j];
+                    w[BF16 ? j / 2 : j] |= b;
+                }
+        }
     }
-    vec8 v = {};
-    for (int j = 0; i + j < d; ++j) v.v[j] = load1<BF16>(row, i + j);
-    return v;
+    __device__ float at(int j) const { return BF16 ? (j & 1 ? bf16hi(w[j >> 1]) : bf16lo(w[j >> 1])) : __uint_as_float(w[j % WORDS]); }
+};
+template <bool BF16, int W>
+__device__ inline void store_columns(void* row, int64_t i, int d, const float (&v)[W]) {
+    char* const at = static_cast<char*>(row) + i * (BF16 ? 2 : 4);
+    if (i + W <= d) {
+        if (BF16 && W == 8)
+            __builtin_nontemporal_store(u32x4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])}, reinterpret_cast<u32x4_any*>(at));
+        else if (BF16) __builtin_nontemporal_store(u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])}, reinterpret_cast<u32x2_odd*>(at));
+        else
+#pragma unroll
+            for (int h = 0; h < W; h += 4)
+                __builtin_nontemporal_store(u32x4{__float_as_uint(v[h]), __float_as_uint(v[h + 1]), __float_as_uint(v[h + 2]), __float_as_uint(v[h + 3])},
+                                            reinterpret_cast<u32x4_any*>(at + h * 4));
+    } else {
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+            if (i + j < d) store1<BF16>(row, i + j, v[j]);
+    }
 }
-template <bool BF16>
-__device__ inline void row_store8(void* row, int64_t i, int d, const vec8& v) {
-    if (i + 8 <= d) store8_any<BF16>(row, i, v);
-    else
-        for (int j = 0; i + j < d; ++j) store1<BF16>(row, i + j, v.v[j]);
-}
+// Columns of a thread: 16 bytes of the wider of the two rows
+constexpr int width_of(bool a_bf16, bool b_bf16) { return a_bf16 && b_bf16 ? 8 : 4; }
 
 struct embed_args {
     const int32_t* ids;
     const void* table;
     void* y;
-    int64_t ld, ld_y, first;
+    int64_t T, ld, ld_y, first;
     int V, d, parts;
     float scale;
 };
-// y[t] = scale table[ids[t]]: a copy, one block per token and part of its columns
+// y[t] = scale table[ids[t]]: a copy.  A block has a part of the columns of AT_ONCE tokens, all on their way at a time; rows of the table are kept in the caches,
+// tokens come again, y is written past them
 template <bool BF16, bool OUT_BF16>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_kernel(const embed_args a) {
-    const int64_t b = a.first + blockIdx.x, t = b / a.parts;
-    const int i = ((int)(b % a.parts) * EMBED_THREADS + threadIdx.x) * 8;
+    constexpr int W = width_of(BF16, OUT_BF16), AT_ONCE = 4;
+    const int64_t b = a.first + blockIdx.x, t0 = b / a.parts * AT_ONCE;
+    const int i = ((int)(b % a.parts) * blockDim.x + threadIdx.x) * W;
     if (i >= a.d) return;
-    const int id = a.ids[t];
-    vec8 v = {};
-    if ((uint32_t)id < (uint32_t)a.V) {
-        v = row_load8<BF16>(row_of<BF16>(a.table, id * a.ld), i, a.d);
+    columns<BF16, W> v[AT_ONCE];
+    bool there[AT_ONCE];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v.v[j] *= a.scale;
+    for (int u = 0; u < AT_ONCE; ++u) {
+        const int id = t0 + u < a.T ? a.ids[t0 + u] : -1;
+        there[u] = (uint32_t)id < (uint32_t)a.V;
+        if (there[u]) v[u].template load<false>(row_of<BF16>(a.table, id * a.ld), i, a.d);
     }
-    row_store8<OUT_BF16>(row_of<OUT_BF16>(a.y, t * a.ld_y), i, a.d, v);
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+        if (t0 + u >= a.T) return;
+        float y[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) y[j] = there[u] ? v[u].at(j) * a.scale : 0.f;
+        store_columns<OUT_BF16, W>(row_of<OUT_BF16>(a.y, (t0 + u) * a.ld_y), i, a.d, y);
+    }
 }
 
-// Keys (id, token) in ascending order: tokens of one id stand together in the order of the batch.  Each block sorts SORT_CHUNK tokens
-__global__ __launch_bounds__(SORT_CHUNK) void sort_tokens_kernel(const int32_t* __restrict__ ids, int64_t T, int V, uint64_t* __restrict__ keys) {
-    __shared__ uint64_t s[SORT_CHUNK];
-    const int i = threadIdx.x;
-    const int64_t t = (int64_t)blockIdx.x * SORT_CHUNK + i;
-    uint64_t mine = NO_KEY;
-    if (t < T) {
-        const uint32_t id = (uint32_t)ids[t];
-        mine = (uint64_t)(id < (uint32_t)V ? id : NO_ID) << 32 | (uint32_t)t;
-    }
-    s[i] = mine;
+struct embed_back_args {
+    const void* dy;
+    const int32_t* ids;
+    void* dtable;
+    int64_t ld, ld_grad, T, first;
+    int V, d, parts, threads;                  // (threads of the blocks that add up, each W columns)
+    float scale;
+    int zero_rows, zero_blocks;                // rows that a block clears; 0: dtable is added to
+    // few tokens: the blocks that add up; rows of many occurrences in parts
+    int64_t sum_blocks;
+    float* partial;                            // [slots][width]
+    int width;
+    int32_t* tickets;
+    // sorted tokens in runs of `run`
+    const uint64_t* keys;
+    int run;
+};
+__device__ inline uint32_t id_of(uint64_t key) { return (uint32_t)(key >> 32); }
+
+// Rows of tokens that do not occur: each block looks through the batch for those of its rows that do
+template <bool OUT_BF16>
+__device__ inline void clear_rows(const embed_back_args& a, int block, uint32_t* seen) {
+    const int v0 = block * a.zero_rows, rows = min(a.zero_rows, a.V - v0);
+    for (int i = threadIdx.x; i < (rows + 31) / 32; i += blockDim.x) seen[i] = 0;
     __syncthreads();
-    for (int size = 2; size <= SORT_CHUNK; size *= 2)
-        for (int step = size / 2; step > 0; step /= 2) {
-            const uint64_t other = s[i ^ step];
-            const bool up = !(i & size), low = !(i & step);
-            mine = (mine < other) == (up == low) ? mine : other;
-            __syncthreads();
-            s[i] = mine;
-            __syncthreads();
+    for (int64_t t = threadIdx.x; t < a.T; t += blockDim.x) {
+        const int id = a.ids[t];
+        const uint32_t at = (uint32_t)id - (uint32_t)v0;       // (ids in front of v0 wrap to large numbers)
+        if (at < (uint32_t)rows && id >= 0) atomicOr(&seen[at / 32], 1u << at % 32);
+    }
+    __syncthreads();
+    constexpr int W = OUT_BF16 ? 8 : 4;
+    const int pieces = (a.d + W - 1) / W, row_step = blockDim.x / pieces, piece_step = blockDim.x % pieces;
+    int row = threadIdx.x / pieces, piece = threadIdx.x % pieces;
+    const float none[W] = {};
+    while (row < rows) {
+        if (!(seen[row / 32] >> row % 32 & 1)) store_columns<OUT_BF16, W>(row_of<OUT_BF16>(a.dtable, (v0 + row) * a.ld_grad), piece * W, a.d, none);
+        row += row_step;
+        piece += piece_step;
+        if (piece >= pieces) piece -= pieces, ++row;
+    }
+}
+
+// A token's finished sum into its row
+template <bool OUT_BF16, bool ADD, int W>
+__device__ inline void finish(const embed_back_args& a, uint32_t id, int i, const columns<OUT_BF16, W>& was, const float (&sum)[W]) {
+    float g[W];
+#pragma unroll
+    for (int j = 0; j < W; ++j) g[j] = ADD ? fmaf(sum[j], a.scale, was.at(j)) : sum[j] * a.scale;
+    store_columns<OUT_BF16, W>(row_of<OUT_BF16>(a.dtable, id * a.ld_grad), i, a.d, g);
+}
+
+// Few tokens in one launch, without sorting: a block looks through the ids for the others of its token, and has work if FEW_RUN divides the number of those in
+// front of it; the runs of a frequent token are joined by the last of their blocks.
+template <bool BF16, bool OUT_BF16, bool ADD>
+__global__ __launch_bounds__(EMBED_THREADS) void embed_few_kernel(const embed_back_args a) {
+    constexpr int W = width_of(BF16, OUT_BF16), MASKS = FEW_TOKENS / 64, AT_ONCE = 8;
+    __shared__ uint64_t s_same[MASKS];
+    __shared__ uint32_t s_seen[ZERO_BITS / 32];
+    __shared__ int32_t s_last;
+    if (blockIdx.x >= a.sum_blocks) {
+        if (!ADD) clear_rows<OUT_BF16>(a, (int)(blockIdx.x - a.sum_blocks), s_seen);
+        return;
+    }
+    const int t = (int)(blockIdx.x / a.parts), part = (int)(blockIdx.x % a.parts), T = (int)a.T;
+    const int i = (part * a.threads + threadIdx.x) * W;
+    const int id = a.ids[t];
+    if ((uint32_t)id >= (uint32_t)a.V) return;
+    for (int k = threadIdx.x; k < FEW_TOKENS; k += blockDim.x) {           // (a wave has 64 consecutive ones)
+        const uint64_t same = __ballot(k < T && a.ids[k < T ? k : 0] == id);
+        if ((threadIdx.x & 63) == 0) s_same[k / 64] = same;
+    }
+    __syncthreads();
+    int ahead = 0, total = 0, first = -1;      // occurrences in front of t, all, and the first one
+    for (int m = 0; m < MASKS; ++m) {
+        const uint64_t same = s_same[m];
+        if (first < 0 && same) first = m * 64 + __builtin_ctzll(same);
+        total += __popcll(same);
+        if (m < t / 64) ahead += __popcll(same);
+        else if (m == t / 64) ahead += __popcll(same & (((uint64_t)1 << t % 64) - 1));
+    }
+    if (ahead % FEW_RUN) return;
+    const bool whole = total <= FEW_RUN, in_row = i < a.d;
+    columns<OUT_BF16, W> was;
+    if (ADD && whole && in_row) was.load(row_of<OUT_BF16>(a.dtable, id * a.ld_grad), i, a.d);
+    int m = t / 64, left = min(FEW_RUN, total - ahead);
+    uint64_t same = s_same[m] & ~(((uint64_t)1 << t % 64) - 1);
+    float sum[W] = {};
+    while (left > 0) {
+        columns<BF16, W> v[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            if (u >= left) continue;
+            while (!same) same = s_same[++m];
+            const int64_t row = m * 64 + __builtin_ctzll(same);
+            same &= same - 1;
+            if (in_row) v[u].load(row_of<BF16>(a.dy, row * a.ld), i, a.d);
         }
-    if (t < T) keys[t] = mine;
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u)
+            if (u < left && in_row)
+#pragma unroll
+                for (int j = 0; j < W; ++j) sum[j] += v[u].at(j);
+        left -= AT_ONCE;
+    }
+    if (whole) {
+        if (in_row) finish<OUT_BF16, ADD, W>(a, id, i, was, sum);
+        return;
+    }
+    const int runs = (total + FEW_RUN - 1) / FEW_RUN;
+    if (in_row) {
+        float* const mine = a.partial + (int64_t)t * a.width + i;
+#pragma unroll
+        for (int j = 0; j < W; ++j) __hip_atomic_store(mine + j, sum[j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (!last_block(a.tickets + first * a.parts + part, runs, s_last) || !in_row) return;
+    if (ADD) was.load(row_of<OUT_BF16>(a.dtable, id * a.ld_grad), i, a.d);
+#pragma unroll
+    for (int j = 0; j < W; ++j) sum[j] = 0.f;
+    int n = 0;
+    for (int k = 0; k < MASKS; ++k)
+        for (uint64_t rest = s_same[k]; rest; rest &= rest - 1)
+            if (n++ % FEW_RUN == 0) {
+                const float* const theirs = a.partial + (int64_t)(k * 64 + __builtin_ctzll(rest)) * a.width + i;
+#pragma unroll
+                for (int j = 0; j < W; ++j) sum[j] += __hip_atomic_load(theirs + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+    finish<OUT_BF16, ADD, W>(a, id, i, was, sum);
+}
+
+// Keys (id, token) in ascending order: tokens of one id stand together in the order of the batch.  A block sorts SORT_CHUNK tokens by a bitonic network, a thread
+// has four in a row; the other blocks of the launch clear rows.
+template <class Key>
+__device__ inline void order(Key& a, Key& b, bool up) {
+    const bool swap = (a > b) == up;
+    const Key low = swap ? b : a, high = swap ? a : b;
+    a = low;
+    b = high;
+}
+__device__ inline uint32_t from_lane(uint32_t v, int mask) { return (uint32_t)__shfl_xor((int)v, mask); }
+__device__ inline uint64_t from_lane(uint64_t v, int mask) {
+    return (uint64_t)(uint32_t)__shfl_xor((int)(uint32_t)(v >> 32), mask) << 32 | (uint32_t)__shfl_xor((int)(uint32_t)v, mask);
+}
+template <class Key>
+__device__ inline void sort_chunk(const embed_back_args& a, int chunk, Key* s, uint64_t* out) {
+    constexpr bool SMALL = sizeof(Key) == 4;   // id and place in the chunk in 32 bits
+    constexpr int PLACE_BITS = 12;
+    static_assert(SORT_CHUNK == 1 << PLACE_BITS, "bits of a place");
+    const int64_t first = (int64_t)chunk * SORT_CHUNK;
+    Key k[SORT_EACH];
+#pragma unroll
+    for (int e = 0; e < SORT_EACH; ++e) {
+        const int at = threadIdx.x * SORT_EACH + e;
+        const uint32_t id = first + at < a.T ? (uint32_t)a.ids[first + at] : NO_ID;
+        const uint32_t none = SMALL ? (uint32_t)a.V : NO_ID;   // (behind all ids; places behind the batch come last, their own are the largest)
+        k[e] = (Key)(id < (uint32_t)a.V ? id : none) << (SMALL ? PLACE_BITS : 32) | (uint32_t)at;
+    }
+    for (int size = 2; size <= SORT_CHUNK; size *= 2) {
+        const auto up = [&](int at) { return !(at & size); };
+        int step = size / 2;
+        if (step >= 64 * SORT_EACH) {          // over waves
+            for (; step >= 64 * SORT_EACH; step /= 2) {
+                __syncthreads();
+#pragma unroll
+                for (int e = 0; e < SORT_EACH; ++e) s[e * SORT_THREADS + threadIdx.x] = k[e];
+                __syncthreads();
+                const int other = threadIdx.x ^ (step / SORT_EACH);
+                const bool low = other > (int)threadIdx.x;
+#pragma unroll
+                for (int e = 0; e < SORT_EACH; ++e) {
+                    const Key theirs = s[e * SORT_THREADS + other];
+                    k[e] = (k[e] < theirs) == (up(threadIdx.x * SORT_EACH + e) == low) ? k[e] : theirs;
+                }
+            }
+        }
+        for (; step >= SORT_EACH; step /= 2) { // over lanes
+            const bool low = !(threadIdx.x & (step / SORT_EACH));
+#pragma unroll
+            for (int e = 0; e < SORT_EACH; ++e) {
+                const Key theirs = from_lane(k[e], step / SORT_EACH);
+                k[e] = (k[e] < theirs) == (up(threadIdx.x * SORT_EACH + e) == low) ? k[e] : theirs;
+            }
+        }
+        if (size == 2) {
+            order(k[0], k[1], true);
+            order(k[2], k[3], false);
+        } else {
+            const bool u = up(threadIdx.x * SORT_EACH);
+            order(k[0], k[2], u);
+            order(k[1], k[3], u);
+            order(k[0], k[1], u);
+            order(k[2], k[3], u);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < SORT_EACH; ++e) {
+        const int at = threadIdx.x * SORT_EACH + e;
+        if (first + at >= a.T) continue;
+        uint32_t id = (uint32_t)(k[e] >> (SMALL ? PLACE_BITS : 32));
+        const uint32_t place = (uint32_t)k[e] & (SORT_CHUNK - 1);
+        if (id >= (uint32_t)a.V) id = NO_ID;
+        out[first + at] = (uint64_t)id << 32 | (uint32_t)(first + place);
+    }
+}
+template <class Key, bool OUT_BF16>
+__global__ __launch_bounds__(SORT_THREADS) void sort_tokens_kernel(const embed_back_args a, int chunks, uint64_t* __restrict__ out) {
+    __shared__ Key s[SORT_CHUNK];
+    if ((int)blockIdx.x < chunks) sort_chunk<Key>(a, blockIdx.x, s, out);
+    else clear_rows<OUT_BF16>(a, blockIdx.x - chunks, reinterpret_cast<uint32_t*>(s));
 }
 
 // Sorted runs of `run` keys, MERGE_WAYS of them to one: a key's place is the number of keys in the runs that are smaller (no two are equal)
@@ -98,82 +331,193 @@ __global__ __launch_bounds__(EMBED_THREADS) void merge_tokens_kernel(const uint6
     out[place] = mine;
 }
 
-struct embed_back_args {
-    const void* dy;
-    const uint64_t* keys;
-    void* dtable;
-    int64_t ld, ld_grad, T, first;
-    int V, d, parts, accumulate;
-    float scale;
-};
-template <bool GRAD_BF16>
-__global__ __launch_bounds__(EMBED_THREADS) void embed_zero_kernel(const embed_back_args a) {
-    const int64_t b = a.first + blockIdx.x;
-    const int i = ((int)(b % a.parts) * EMBED_THREADS + threadIdx.x) * 8;
-    if (i < a.d) row_store8<GRAD_BF16>(row_of<GRAD_BF16>(a.dtable, b / a.parts * a.ld_grad), i, a.d, vec8{});
-}
-// One block per sorted token and part of the columns; that of a token's first occurrence adds up all of them
-template <bool BF16, bool GRAD_BF16>
+// A run of sorted tokens and a part of the columns to a block, whatever the tokens' frequencies.  A token whose rows all lie in the run is finished here; the
+// sum of one that goes on from the run before, or into the next, is a partial one: places 2 run and 2 run + 1.
+template <bool BF16, bool OUT_BF16, bool ADD>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(const embed_back_args a) {
-    const int64_t b = a.first + blockIdx.x, p = b / a.parts;
-    const int i = ((int)(b % a.parts) * EMBED_THREADS + threadIdx.x) * 8;
-    const uint32_t id = (uint32_t)(a.keys[p] >> 32);
-    if (i >= a.d || id == NO_ID || (p > 0 && (uint32_t)(a.keys[p - 1] >> 32) == id)) return;
-    vec8 sum = {};
-    for (int64_t q = p; q < a.T && (uint32_t)(a.keys[q] >> 32) == id; ++q) {
-        const vec8 v = row_load8<BF16>(row_of<BF16>(a.dy, (int64_t)(uint32_t)a.keys[q] * a.ld), i, a.d);
+    constexpr int W = width_of(BF16, OUT_BF16), AT_ONCE = ADD && !OUT_BF16 ? 4 : 8;
+    const int64_t b = a.first + blockIdx.x, r = b / a.parts, begin = r * a.run, end = begin + a.run < a.T ? begin + a.run : a.T;
+    const int i = ((int)(b % a.parts) * a.threads + threadIdx.x) * W, lane = threadIdx.x & 63;
+    if (i - lane * W >= a.d) return;           // (whole waves: the lanes below hold keys)
+    const bool in_row = i < a.d;
+    float sum[W] = {};
+    bool open = begin > 0 && id_of(a.keys[begin - 1]) == id_of(a.keys[begin]);         // the present token began in an earlier run
+    float* const head = a.partial + 2 * r * a.width + i;
+    for (int64_t p = begin; p < end; p += 64) {
+        const int rows = (int)(end - p < 64 ? end - p : 64);
+        const uint64_t key = lane < rows ? a.keys[p + lane] : ~(uint64_t)0;
+        const uint32_t id = id_of(key), token = (uint32_t)key, next = lane < rows && p + lane + 1 < a.T ? id_of(a.keys[p + lane + 1]) : NO_ID;
+        const int known = __popcll(__ballot(id != NO_ID));     // (the others are the last ones)
+        const uint64_t ends = __ballot(id != NO_ID && id != next);
+        for (int q = 0; q < known; q += AT_ONCE) {
+            columns<BF16, W> v[AT_ONCE];
+            columns<OUT_BF16, W> was[AT_ONCE];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum.v[j] += v.v[j];
+            for (int u = 0; u < AT_ONCE; ++u) {
+                if (q + u >= known) continue;
+                if (in_row) v[u].load(row_of<BF16>(a.dy, (int64_t)(uint32_t)__builtin_amdgcn_readlane(token, q + u) * a.ld), i, a.d);
+                if (ADD && ends >> (q + u) & 1 && in_row)
+                    was[u].load(row_of<OUT_BF16>(a.dtable, (int64_t)(uint32_t)__builtin_amdgcn_readlane(id, q + u) * a.ld_grad), i, a.d);
+            }
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                if (q + u >= known) continue;
+#pragma unroll
+                for (int j = 0; j < W; ++j) sum[j] += in_row ? v[u].at(j) : 0.f;
+                if (!(ends >> (q + u) & 1)) continue;
+                if (open) {
+#pragma unroll
+                    for (int j = 0; j < W; ++j)
+                        if (in_row) head[j] = sum[j];
+                } else if (in_row) {
+                    finish<OUT_BF16, ADD, W>(a, (uint32_t)__builtin_amdgcn_readlane(id, q + u), i, was[u], sum);
+                }
+                open = false;
+#pragma unroll
+                for (int j = 0; j < W; ++j) sum[j] = 0.f;
+            }
+        }
+        if (known < rows) return;
     }
-    void* const row = row_of<GRAD_BF16>(a.dtable, id * a.ld_grad);
-    const vec8 was = a.accumulate ? row_load8<GRAD_BF16>(row, i, a.d) : vec8{};
+    if (end < a.T && in_row && id_of(a.keys[end]) == id_of(a.keys[end - 1])) {
+        float* const at = open ? head : head + a.width;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum.v[j] = fmaf(sum.v[j], a.scale, was.v[j]);
-    row_store8<GRAD_BF16>(row, i, a.d, sum);
+        for (int j = 0; j < W; ++j) at[j] = sum[j];
+    }
+}
+
+// Tokens whose rows lie in several runs: the block of the run in which one begins adds up the runs' sums, its waves a quarter of them each
+template <bool OUT_BF16, bool ADD>
+__global__ __launch_bounds__(EMBED_THREADS) void embed_join_kernel(const embed_back_args a) {
+    constexpr int W = 4, AT_ONCE = 8, WAVES = EMBED_THREADS / 64;
+    __shared__ float s_sum[WAVES][64 * W];
+    const int64_t b = a.first + blockIdx.x, r = b / a.parts, begin = r * a.run, end = begin + a.run;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, i = ((int)(b % a.parts) * 64 + lane) * W;
+    const uint32_t id = id_of(a.keys[end - 1]);
+    if (id == NO_ID || id_of(a.keys[end]) != id || (begin > 0 && id_of(a.keys[begin]) == id && id_of(a.keys[begin - 1]) == id)) return;
+    // the last run that begins with this token, by 64 at a time
+    const int64_t runs = (a.T + a.run - 1) / a.run;
+    int64_t last = r + 1;
+    for (;;) {
+        const int64_t at = last + 1 + lane;
+        const uint64_t same = __ballot(at < runs && id_of(a.keys[at * a.run]) == id);
+        last += __popcll(same);
+        if (~same) break;
+    }
+    // sums r: 2 r + 1, then 2 q of the runs q behind it
+    const int64_t n = last - r + 1, each = (n + WAVES - 1) / WAVES, from = wave * each, to = from + each < n ? from + each : n;
+    const bool in_row = i < a.d;
+    float sum[W] = {};
+    for (int64_t q = from; q < to; q += AT_ONCE) {
+        f32x4 v[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u)
+            if (q + u < to && in_row) v[u] = *reinterpret_cast<const f32x4*>(a.partial + (q + u == 0 ? 2 * r + 1 : 2 * (r + q + u)) * a.width + i);
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u)
+            if (q + u < to && in_row)
+#pragma unroll
+                for (int j = 0; j < W; ++j) sum[j] += v[u][j];
+    }
+#pragma unroll
+    for (int j = 0; j < W; ++j) s_sum[wave][lane * W + j] = sum[j];
+    __syncthreads();
+    if (wave || !in_row) return;
+    columns<OUT_BF16, W> was;
+    if (ADD) was.load(row_of<OUT_BF16>(a.dtable, id * a.ld_grad), i, a.d);
+    for (int w = 1; w < WAVES; ++w)
+#pragma unroll
+        for (int j = 0; j < W; ++j) sum[j] += s_sum[w][lane * W + j];
+    finish<OUT_BF16, ADD, W>(a, id, i, was, sum);
 }
 
 // blocks 0 .. n-1 in launches that a grid holds
 template <class Kernel, class Args>
-hipError_t launch_blocks(hipStream_t s, Kernel kernel, Args a, int64_t n) {
+hipError_t launch_blocks(hipStream_t s, Kernel kernel, Args a, int64_t n, int threads) {
     for (a.first = 0; a.first < n; a.first += EMBED_MAX_GRID)
-        hipLaunchKernelGGL(kernel, dim3((unsigned)(n - a.first < EMBED_MAX_GRID ? n - a.first : EMBED_MAX_GRID)), dim3(EMBED_THREADS), 0, s, a);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(n - a.first < EMBED_MAX_GRID ? n - a.first : EMBED_MAX_GRID)), dim3(threads), 0, s, a);
     return hipGetLastError();
+}
+// Parts of a row of `pieces` threads and their blocks' threads
+void cut_row(int pieces, int& parts, int& threads) {
+    parts = (pieces + EMBED_THREADS - 1) / EMBED_THREADS;
+    threads = ((pieces + parts - 1) / parts + 63) / 64 * 64;
+}
+
+template <bool BF16, bool OUT_BF16, bool ADD>
+hipError_t launch_embed_sums(moe_ctx* c, embed_back_args a) {
+    const int pieces = (a.d + width_of(BF16, OUT_BF16) - 1) / width_of(BF16, OUT_BF16);
+    cut_row(pieces, a.parts, a.threads);
+    a.width = (a.d + 7) / 8 * 8;
+    if (!ADD) {
+        // rows to a block: enough to make light of looking through the batch, and blocks for all CUs
+        int64_t rows = (a.V + 2047) / 2048;
+        if (rows > ZERO_BITS) rows = ZERO_BITS;
+        a.zero_rows = (int)rows;
+        a.zero_blocks = (int)((a.V + rows - 1) / rows);
+    }
+    if (a.T <= FEW_TOKENS && a.T * a.parts <= GRAD_TICKETS && a.T * a.width * sizeof(float) <= GRAD_WS_BYTES && a.zero_blocks <= EMBED_MAX_GRID / 2) {
+        a.sum_blocks = a.T * a.parts;
+        a.partial = static_cast<float*>(c->grad_ws);
+        a.tickets = c->grad_tickets;
+        const unsigned grid = (unsigned)(a.sum_blocks + a.zero_blocks);
+        if (grid) embed_few_kernel<BF16, OUT_BF16, ADD><<<grid, a.threads, 0, c->stream>>>(a);
+        return hipGetLastError();
+    }
+    uint64_t *keys = static_cast<uint64_t*>(c->grad_ws), *other = keys + a.T;
+    const int chunks = (int)((a.T + SORT_CHUNK - 1) / SORT_CHUNK);
+    if (a.V < 1 << 20) sort_tokens_kernel<uint32_t, OUT_BF16><<<chunks + a.zero_blocks, SORT_THREADS, 0, c->stream>>>(a, chunks, keys);
+    else sort_tokens_kernel<uint64_t, OUT_BF16><<<chunks + a.zero_blocks, SORT_THREADS, 0, c->stream>>>(a, chunks, keys);
+    for (int64_t run = SORT_CHUNK; run < a.T; run *= MERGE_WAYS) {
+        merge_tokens_kernel<<<(unsigned)((a.T + EMBED_THREADS - 1) / EMBED_THREADS), EMBED_THREADS, 0, c->stream>>>(keys, a.T, run, other);
+        uint64_t* const sorted = other;
+        other = keys;
+        keys = sorted;
+    }
+    a.keys = keys;
+    a.partial = reinterpret_cast<float*>(static_cast<uint64_t*>(c->grad_ws) + (2 * a.T + 1) / 2 * 2);
+    const int64_t room = (GRAD_WS_BYTES - 16 * (a.T + 1)) / (2 * sizeof(float) * a.width);
+    a.run = 8;
+    while ((a.T + a.run - 1) / a.run > room || (a.run < 32 && a.T / a.run * a.parts > 4096)) a.run *= 2;
+    const int64_t runs = (a.T + a.run - 1) / a.run;
+    const hipError_t e = launch_blocks(c->stream, embed_sum_kernel<BF16, OUT_BF16, ADD>, a, runs * a.parts, a.threads);
+    if (e != hipSuccess || runs == 1) return e;
+    a.parts = (a.d + 255) / 256;
+    return launch_blocks(c->stream, embed_join_kernel<OUT_BF16, ADD>, a, (runs - 1) * a.parts, EMBED_THREADS);
 }
 
 }  // namespace
 
 hipError_t launch_embed(hipStream_t s, const int32_t* ids, int64_t T, const void* table, int32_t V, int32_t d, int64_t ld, int32_t dtype, float scale,
                         void* y, int64_t ld_y, int32_t out_dtype) {
-    const int parts = (d + EMBED_THREADS * 8 - 1) / (EMBED_THREADS * 8);
-    const embed_args a{ids, table, y, ld, ld_y, 0, V, d, parts, scale};
-    if (dtype == MOE_BF16) return out_dtype == MOE_BF16 ? launch_blocks(s, embed_kernel<true, true>, a, T * parts) : launch_blocks(s, embed_kernel<true, false>, a, T * parts);
-    return out_dtype == MOE_BF16 ? launch_blocks(s, embed_kernel<false, true>, a, T * parts) : launch_blocks(s, embed_kernel<false, false>, a, T * parts);
+    const bool bf16 = dtype == MOE_BF16, out_bf16 = out_dtype == MOE_BF16;
+    const int W = width_of(bf16, out_bf16);
+    int parts, threads;
+    cut_row((d + W - 1) / W, parts, threads);
+    const embed_args a{ids, table, y, T, ld, ld_y, 0, V, d, parts, scale};
+    const int64_t n = (T + 3) / 4 * parts;
+    if (bf16) return out_bf16 ? launch_blocks(s, embed_kernel<true, true>, a, n, threads) : launch_blocks(s, embed_kernel<true, false>, a, n, threads);
+    return out_bf16 ? launch_blocks(s, embed_kernel<false, true>, a, n, threads) : launch_blocks(s, embed_kernel<false, false>, a, n, threads);
 }
 
 hipError_t launch_embed_backward(moe_ctx* c, const void* dy, const int32_t* ids, int64_t T, int32_t V, int32_t d, int64_t ld, int32_t dtype, float scale,
                                  int32_t accumulate, void* dtable, int64_t ld_grad, int32_t grad_dtype) {
-    const int parts = (d + EMBED_THREADS * 8 - 1) / (EMBED_THREADS * 8);
-    uint64_t* keys = static_cast<uint64_t*>(c->grad_ws);
-    uint64_t* other = keys + EMBED_MAX_TOKENS;
-    embed_back_args a{dy, keys, dtable, ld, ld_grad, T, 0, V, d, parts, accumulate, scale};
-    hipError_t e = hipSuccess;
-    if (!accumulate)
-        e = grad_dtype == MOE_BF16 ? launch_blocks(c->stream, embed_zero_kernel<true>, a, (int64_t)V * parts)
-                                   : launch_blocks(c->stream, embed_zero_kernel<false>, a, (int64_t)V * parts);
-    if (e != hipSuccess || T == 0) return e;
-    sort_tokens_kernel<<<(unsigned)((T + SORT_CHUNK - 1) / SORT_CHUNK), SORT_CHUNK, 0, c->stream>>>(ids, T, V, keys);
-    for (int64_t run = SORT_CHUNK; run < T; run *= MERGE_WAYS) {
-        merge_tokens_kernel<<<(unsigned)((T + EMBED_THREADS - 1) / EMBED_THREADS), EMBED_THREADS, 0, c->stream>>>(keys, T, run, other);
-        uint64_t* const sorted = other;
-        other = keys;
-        keys = sorted;
+    embed_back_args a{};
+    a.dy = dy;
+    a.ids = ids;
+    a.dtable = dtable;
+    a.ld = ld;
+    a.ld_grad = ld_grad;
+    a.T = T;
+    a.V = V;
+    a.d = d;
+    a.scale = scale;
+    if (dtype == MOE_BF16) {
+        if (grad_dtype == MOE_BF16) return accumulate ? launch_embed_sums<true, true, true>(c, a) : launch_embed_sums<true, true, false>(c, a);
+        return accumulate ? launch_embed_sums<true, false, true>(c, a) : launch_embed_sums<true, false, false>(c, a);
     }
-    a.keys = keys;
-    if (dtype == MOE_BF16)
-        return grad_dtype == MOE_BF16 ? launch_blocks(c->stream, embed_sum_kernel<true, true>, a, T * parts)
-                                      : launch_blocks(c->stream, embed_sum_kernel<true, false>, a, T * parts);
-    return grad_dtype == MOE_BF16 ? launch_blocks(c->stream, embed_sum_kernel<false, true>, a, T * parts)
-                                  : launch_blocks(c->stream, embed_sum_kernel<false, false>, a, T * parts);
+    if (grad_dtype == MOE_BF16) return accumulate ? launch_embed_sums<false, true, true>(c, a) : launch_embed_sums<false, true, false>(c, a);
+    return accumulate ? launch_embed_sums<false, false, true>(c, a) : launch_embed_sums<false, false, false>(c, a);
 }
 
 }  // namespace moe355
