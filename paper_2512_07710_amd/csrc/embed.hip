@@ -1,5 +1,6 @@
 // Rows of an embedding table for token ids, and the table's gradient by sorted tokens.
 #include "grad_common.hpp"
+#include "lanes.hpp"
 #include "ticket.hpp"
 
 namespace moe355 {
@@ -7,8 +8,8 @@ namespace {
 
 constexpr int EMBED_THREADS = 256;
 constexpr int64_t EMBED_MAX_GRID = 1 << 22;
-constexpr int FEW_TOKENS = 1024, FEW_RUN = 64;         // tokens that need no sorting, rows of one token that one block adds up
-constexpr int SORT_THREADS = 1024, SORT_EACH = 4, SORT_CHUNK = SORT_THREADS * SORT_EACH, MERGE_WAYS = 32;
+constexpr int FEW_TOKENS = 1024, FEW_RUN = 16;         // tokens that need no sorting, rows of one token that one block adds up
+constexpr int RANK_THREADS = 1024, RANK_CHUNK = 4096, RANK_ALONE = 8192, MERGE_WAYS = 32, MERGE_AT_ONCE = 8;
 constexpr int ZERO_BITS = 4096;                        // rows that a block clears at most
 constexpr uint32_t NO_ID = 0xFFFFFFFFu;                // of tokens outside the table: behind the others
 
@@ -159,6 +160,7 @@ template <bool BF16, bool OUT_BF16, bool ADD>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_few_kernel(const embed_back_args a) {
     constexpr int W = width_of(BF16, OUT_BF16), MASKS = FEW_TOKENS / 64, AT_ONCE = 8;
     __shared__ uint64_t s_same[MASKS];
+    __shared__ uint16_t s_list[FEW_TOKENS];
     __shared__ uint32_t s_seen[ZERO_BITS / 32];
     __shared__ int32_t s_last;
     if (blockIdx.x >= a.sum_blocks) {
@@ -174,37 +176,35 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_few_kernel(const embed_ba
         if ((threadIdx.x & 63) == 0) s_same[k / 64] = same;
     }
     __syncthreads();
-    int ahead = 0, total = 0, first = -1;      // occurrences in front of t, all, and the first one
-    for (int m = 0; m < MASKS; ++m) {
-        const uint64_t same = s_same[m];
-        if (first < 0 && same) first = m * 64 + __builtin_ctzll(same);
-        total += __popcll(same);
-        if (m < t / 64) ahead += __popcll(same);
-        else if (m == t / 64) ahead += __popcll(same & (((uint64_t)1 << t % 64) - 1));
-    }
+    // a lane has 64 tokens: how many occurrences there are up to them
+    const int lane = threadIdx.x & 63;
+    const uint64_t mine = lane < MASKS ? s_same[lane] : 0;
+    const int upto = wave_scan(__popcll(mine)), total = __builtin_amdgcn_readlane(upto, 63);
+    const int ahead = __builtin_amdgcn_readlane(upto - __popcll(mine >> t % 64), t / 64);
     if (ahead % FEW_RUN) return;
+    const int group = __builtin_ctzll(__ballot(mine != 0)), first = group * 64 + __builtin_ctzll(s_same[group]);
+    // the occurrences in their order
+    for (int k = threadIdx.x; k < FEW_TOKENS; k += blockDim.x) {
+        const uint64_t same = s_same[k / 64];
+        if (same >> lane & 1)
+            s_list[__builtin_amdgcn_readlane(upto, k / 64) - __popcll(same >> lane)] = (uint16_t)k;
+    }
+    __syncthreads();
     const bool whole = total <= FEW_RUN, in_row = i < a.d;
+    const int left = min(FEW_RUN, total - ahead);
     columns<OUT_BF16, W> was;
     if (ADD && whole && in_row) was.load(row_of<OUT_BF16>(a.dtable, id * a.ld_grad), i, a.d);
-    int m = t / 64, left = min(FEW_RUN, total - ahead);
-    uint64_t same = s_same[m] & ~(((uint64_t)1 << t % 64) - 1);
     float sum[W] = {};
-    while (left > 0) {
+    for (int q = 0; q < left; q += AT_ONCE) {
         columns<BF16, W> v[AT_ONCE];
 #pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
-            if (u >= left) continue;
-            while (!same) same = s_same[++m];
-            const int64_t row = m * 64 + __builtin_ctzll(same);
-            same &= same - 1;
-            if (in_row) v[u].load(row_of<BF16>(a.dy, row * a.ld), i, a.d);
-        }
+        for (int u = 0; u < AT_ONCE; ++u)
+            if (q + u < left && in_row) v[u].load(row_of<BF16>(a.dy, __builtin_amdgcn_readfirstlane(s_list[ahead + q + u]) * a.ld), i, a.d);
 #pragma unroll
         for (int u = 0; u < AT_ONCE; ++u)
-            if (u < left && in_row)
+            if (q + u < left && in_row)
 #pragma unroll
                 for (int j = 0; j < W; ++j) sum[j] += v[u].at(j);
-        left -= AT_ONCE;
     }
     if (whole) {
         if (in_row) finish<OUT_BF16, ADD, W>(a, id, i, was, sum);
@@ -220,113 +220,79 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_few_kernel(const embed_ba
     if (ADD) was.load(row_of<OUT_BF16>(a.dtable, id * a.ld_grad), i, a.d);
 #pragma unroll
     for (int j = 0; j < W; ++j) sum[j] = 0.f;
-    int n = 0;
-    for (int k = 0; k < MASKS; ++k)
-        for (uint64_t rest = s_same[k]; rest; rest &= rest - 1)
-            if (n++ % FEW_RUN == 0) {
-                const float* const theirs = a.partial + (int64_t)(k * 64 + __builtin_ctzll(rest)) * a.width + i;
+    for (int q = 0; q < runs; q += AT_ONCE) {
+        float v[AT_ONCE][W];
 #pragma unroll
-                for (int j = 0; j < W; ++j) sum[j] += __hip_atomic_load(theirs + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        for (int u = 0; u < AT_ONCE; ++u)
+            if (q + u < runs) {
+                const float* const theirs = a.partial + (int64_t)s_list[(q + u) * FEW_RUN] * a.width + i;
+#pragma unroll
+                for (int j = 0; j < W; ++j) v[u][j] = __hip_atomic_load(theirs + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u)
+            if (q + u < runs)
+#pragma unroll
+                for (int j = 0; j < W; ++j) sum[j] += v[u][j];
+    }
     finish<OUT_BF16, ADD, W>(a, id, i, was, sum);
 }
 
-// Keys (id, token) in ascending order: tokens of one id stand together in the order of the batch.  A block sorts SORT_CHUNK tokens by a bitonic network, a thread
-// has four in a row; the other blocks of the launch clear rows.
-template <class Key>
-__device__ inline void order(Key& a, Key& b, bool up) {
-    const bool swap = (a > b) == up;
-    const Key low = swap ? b : a, high = swap ? a : b;
-    a = low;
-    b = high;
-}
-__device__ inline uint32_t from_lane(uint32_t v, int mask) { return (uint32_t)__shfl_xor((int)v, mask); }
-__device__ inline uint64_t from_lane(uint64_t v, int mask) {
-    return (uint64_t)(uint32_t)__shfl_xor((int)(uint32_t)(v >> 32), mask) << 32 | (uint32_t)__shfl_xor((int)(uint32_t)v, mask);
-}
-template <class Key>
-__device__ inline void sort_chunk(const embed_back_args& a, int chunk, Key* s, uint64_t* out) {
-    constexpr bool SMALL = sizeof(Key) == 4;   // id and place in the chunk in 32 bits
-    constexpr int PLACE_BITS = 12;
-    static_assert(SORT_CHUNK == 1 << PLACE_BITS, "bits of a place");
-    const int64_t first = (int64_t)chunk * SORT_CHUNK;
-    Key k[SORT_EACH];
-#pragma unroll
-    for (int e = 0; e < SORT_EACH; ++e) {
-        const int at = threadIdx.x * SORT_EACH + e;
-        const uint32_t id = first + at < a.T ? (uint32_t)a.ids[first + at] : NO_ID;
-        const uint32_t none = SMALL ? (uint32_t)a.V : NO_ID;   // (behind all ids; places behind the batch come last, their own are the largest)
-        k[e] = (Key)(id < (uint32_t)a.V ? id : none) << (SMALL ? PLACE_BITS : 32) | (uint32_t)at;
+// Keys (id, token) in ascending order: tokens of one id stand together in the order of the batch.  A token's place in its chunk is the number of tokens there that
+// come before it: 64 tokens to a block, one to a lane, and the chunk's ids, the same for all lanes, dealt to the 16 waves.  Two instructions for 64 comparisons on
+// all CUs take less than a sorting network on few: 4096 tokens 3 us, the network 17.  The other blocks of the launch clear rows.
+template <bool OUT_BF16>
+__global__ __launch_bounds__(RANK_THREADS) void rank_tokens_kernel(const embed_back_args a, const int32_t* __restrict__ ids, int blocks, int chunk,
+                                                                   uint64_t* __restrict__ out) {
+    constexpr int WAVES = RANK_THREADS / 64;
+    __shared__ uint32_t s[ZERO_BITS / 32 > WAVES * 64 ? ZERO_BITS / 32 : WAVES * 64];
+    if ((int)blockIdx.x >= blocks) {
+        clear_rows<OUT_BF16>(a, blockIdx.x - blocks, s);
+        return;
     }
-    for (int size = 2; size <= SORT_CHUNK; size *= 2) {
-        const auto up = [&](int at) { return !(at & size); };
-        int step = size / 2;
-        if (step >= 64 * SORT_EACH) {          // over waves
-            for (; step >= 64 * SORT_EACH; step /= 2) {
-                __syncthreads();
-#pragma unroll
-                for (int e = 0; e < SORT_EACH; ++e) s[e * SORT_THREADS + threadIdx.x] = k[e];
-                __syncthreads();
-                const int other = threadIdx.x ^ (step / SORT_EACH);
-                const bool low = other > (int)threadIdx.x;
-#pragma unroll
-                for (int e = 0; e < SORT_EACH; ++e) {
-                    const Key theirs = s[e * SORT_THREADS + other];
-                    k[e] = (k[e] < theirs) == (up(threadIdx.x * SORT_EACH + e) == low) ? k[e] : theirs;
-                }
-            }
-        }
-        for (; step >= SORT_EACH; step /= 2) { // over lanes
-            const bool low = !(threadIdx.x & (step / SORT_EACH));
-#pragma unroll
-            for (int e = 0; e < SORT_EACH; ++e) {
-                const Key theirs = from_lane(k[e], step / SORT_EACH);
-                k[e] = (k[e] < theirs) == (up(threadIdx.x * SORT_EACH + e) == low) ? k[e] : theirs;
-            }
-        }
-        if (size == 2) {
-            order(k[0], k[1], true);
-            order(k[2], k[3], false);
-        } else {
-            const bool u = up(threadIdx.x * SORT_EACH);
-            order(k[0], k[2], u);
-            order(k[1], k[3], u);
-            order(k[0], k[1], u);
-            order(k[2], k[3], u);
-        }
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int T = (int)a.T, t0 = blockIdx.x * 64, t = t0 + lane, begin = t0 / chunk * chunk, end = min(begin + chunk, T);
+    const uint32_t V = (uint32_t)a.V, own = t < T ? (uint32_t)ids[t] : NO_ID, id = own < V ? own : NO_ID;
+    const int each = (end - begin + WAVES - 1) / WAVES, from = begin + wave * each, to = min(from + each, end);
+    uint32_t rank = 0;
+    auto at = [&](int j) {
+        const uint32_t o = (uint32_t)ids[j];
+        return o < V ? o : NO_ID;
+    };
+    int j = from;
+#pragma unroll 8
+    for (; j < min(to, t0); ++j) rank += at(j) <= id;          // (in front: an equal one comes before)
+    for (; j < min(to, t0 + 64); ++j) {
+        const uint32_t o = at(j);
+        rank += (int)(o < id) | ((int)(o == id) & (int)(j < t));
     }
-#pragma unroll
-    for (int e = 0; e < SORT_EACH; ++e) {
-        const int at = threadIdx.x * SORT_EACH + e;
-        if (first + at >= a.T) continue;
-        uint32_t id = (uint32_t)(k[e] >> (SMALL ? PLACE_BITS : 32));
-        const uint32_t place = (uint32_t)k[e] & (SORT_CHUNK - 1);
-        if (id >= (uint32_t)a.V) id = NO_ID;
-        out[first + at] = (uint64_t)id << 32 | (uint32_t)(first + place);
-    }
-}
-template <class Key, bool OUT_BF16>
-__global__ __launch_bounds__(SORT_THREADS) void sort_tokens_kernel(const embed_back_args a, int chunks, uint64_t* __restrict__ out) {
-    __shared__ Key s[SORT_CHUNK];
-    if ((int)blockIdx.x < chunks) sort_chunk<Key>(a, blockIdx.x, s, out);
-    else clear_rows<OUT_BF16>(a, blockIdx.x - chunks, reinterpret_cast<uint32_t*>(s));
+#pragma unroll 8
+    for (; j < to; ++j) rank += at(j) < id;
+    s[wave * 64 + lane] = rank;
+    __syncthreads();
+    if (wave || t >= T) return;
+    for (int w = 1; w < WAVES; ++w) rank += s[w * 64 + lane];
+    out[begin + rank] = (uint64_t)id << 32 | (uint32_t)t;
 }
 
-// Sorted runs of `run` keys, MERGE_WAYS of them to one: a key's place is the number of keys in the runs that are smaller (no two are equal)
+// Sorted runs of `run` keys, MERGE_WAYS of them to one: a key's place is the number of keys in the runs that are smaller (no two are equal).  The searches of
+// eight runs go side by side, each step waits for the memory once.
 __global__ __launch_bounds__(EMBED_THREADS) void merge_tokens_kernel(const uint64_t* __restrict__ keys, int64_t T, int64_t run, uint64_t* __restrict__ out) {
     const int64_t i = (int64_t)blockIdx.x * EMBED_THREADS + threadIdx.x;
     if (i >= T) return;
     const uint64_t mine = keys[i];
     const int64_t first = i / (run * MERGE_WAYS) * (run * MERGE_WAYS);
     int64_t place = first;
-    for (int64_t at = first; at < T && at < first + run * MERGE_WAYS; at += run) {
-        int64_t lo = at, hi = at + run < T ? at + run : T;
-        while (lo < hi) {
-            const int64_t mid = (lo + hi) / 2;
-            if (keys[mid] < mine) lo = mid + 1;
-            else hi = mid;
-        }
-        place += lo - at;
+    for (int64_t at = first; at < T && at < first + run * MERGE_WAYS; at += run * MERGE_AT_ONCE) {
+        int64_t below[MERGE_AT_ONCE] = {};     // of each run
+        for (int64_t step = run; step > 0; step /= 2)          // (run: a power of two)
+#pragma unroll
+            for (int u = 0; u < MERGE_AT_ONCE; ++u) {
+                const int64_t to = at + u * run + below[u] + step;
+                if (below[u] + step <= run && to <= T && keys[to - 1] < mine) below[u] += step;
+            }
+#pragma unroll
+        for (int u = 0; u < MERGE_AT_ONCE; ++u) place += below[u];
     }
     out[place] = mine;
 }
@@ -465,10 +431,9 @@ hipError_t launch_embed_sums(moe_ctx* c, embed_back_args a) {
         return hipGetLastError();
     }
     uint64_t *keys = static_cast<uint64_t*>(c->grad_ws), *other = keys + a.T;
-    const int chunks = (int)((a.T + SORT_CHUNK - 1) / SORT_CHUNK);
-    if (a.V < 1 << 20) sort_tokens_kernel<uint32_t, OUT_BF16><<<chunks + a.zero_blocks, SORT_THREADS, 0, c->stream>>>(a, chunks, keys);
-    else sort_tokens_kernel<uint64_t, OUT_BF16><<<chunks + a.zero_blocks, SORT_THREADS, 0, c->stream>>>(a, chunks, keys);
-    for (int64_t run = SORT_CHUNK; run < a.T; run *= MERGE_WAYS) {
+    const int chunk = a.T <= RANK_ALONE ? RANK_ALONE : RANK_CHUNK, blocks = (int)((a.T + 63) / 64);
+    rank_tokens_kernel<OUT_BF16><<<blocks + a.zero_blocks, RANK_THREADS, 0, c->stream>>>(a, a.ids, blocks, chunk, keys);
+    for (int64_t run = chunk; run < a.T; run *= MERGE_WAYS) {
         merge_tokens_kernel<<<(unsigned)((a.T + EMBED_THREADS - 1) / EMBED_THREADS), EMBED_THREADS, 0, c->stream>>>(keys, a.T, run, other);
         uint64_t* const sorted = other;
         other = keys;
@@ -478,7 +443,7 @@ hipError_t launch_embed_sums(moe_ctx* c, embed_back_args a) {
     a.partial = reinterpret_cast<float*>(static_cast<uint64_t*>(c->grad_ws) + (2 * a.T + 1) / 2 * 2);
     const int64_t room = (GRAD_WS_BYTES - 16 * (a.T + 1)) / (2 * sizeof(float) * a.width);
     a.run = 8;
-    while ((a.T + a.run - 1) / a.run > room || (a.run < 32 && a.T / a.run * a.parts > 4096)) a.run *= 2;
+    while ((a.T + a.run - 1) / a.run > room || a.T / (2 * a.run) * a.parts >= 1024) a.run *= 2;
     const int64_t runs = (a.T + a.run - 1) / a.run;
     const hipError_t e = launch_blocks(c->stream, embed_sum_kernel<BF16, OUT_BF16, ADD>, a, runs * a.parts, a.threads);
     if (e != hipSuccess || runs == 1) return e;
