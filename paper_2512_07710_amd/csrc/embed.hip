@@ -10,19 +10,36 @@ constexpr int EMBED_THREADS = 256;
 constexpr int64_t EMBED_MAX_GRID = 1 << 22;
 constexpr int FEW_TOKENS = 1024, FEW_RUN = 16;         // tokens that need no sorting, rows of one token that one block adds up
 constexpr int RANK_THREADS = 1024, RANK_CHUNK = 4096, RANK_ALONE = 8192, MERGE_WAYS = 32, MERGE_AT_ONCE = 8;
+constexpr int SUM_AT_ONCE = 8;                         // sorted rows that a thread has on their way
+constexpr int EMBED_BLOCKS = 1024;                     // that add up sorted tokens, about
 constexpr int ZERO_BITS = 4096;                        // rows that a block clears at most
 constexpr uint32_t NO_ID = 0xFFFFFFFFu;                // of tokens outside the table: behind the others
 
-// W columns of a row, as they lie in memory, at any element.  Rows are read once: past the caches
+// A thread's W columns of a row of d.  TAIL: d need not be a multiple of W; the last thread then reads the last W columns, and `skip` of them are its neighbour's,
+// which it leaves alone.  A thread behind the row reads what the last one does and writes nothing.  So no load has a condition: one in a branch of its own waits
+// for the one before it.
+template <int W, bool TAIL>
+struct piece {
+    int nominal, at, skip;
+    bool in_row;
+    __device__ piece(int thread, int d) {
+        const int last = (d - 1) / W;
+        in_row = thread <= last;
+        nominal = (in_row ? thread : last) * W;
+        at = TAIL && nominal + W > d ? (d > W ? d - W : 0) : nominal;
+        skip = nominal - at;
+    }
+};
+// They lie in memory at any element.  PAST: past the caches
 typedef u32x2 __attribute__((aligned(2))) u32x2_odd;
-template <bool BF16, int W>
+template <bool BF16, int W, bool TAIL>
 struct columns {
     static constexpr int WORDS = W * (BF16 ? 2 : 4) / 4;
     uint32_t w[WORDS];
-    template <bool PAST = true>
-    __device__ void load(const void* row, int64_t i, int d) {
-        const char* const at = static_cast<const char*>(row) + i * (BF16 ? 2 : 4);
-        if (i + W <= d) {
+    template <bool PAST = false>
+    __device__ void load(const void* row, int i, int d) {
+        const char* const at = static_cast<const char*>(row) + (int64_t)i * (BF16 ? 2 : 4);
+        if (!TAIL || d >= W) {
             if (WORDS == 4) {
                 const u32x4_any* const p = reinterpret_cast<const u32x4_any*>(at);
                 const u32x4 v = PAST ? __builtin_nontemporal_load(p) : *p;
@@ -34,23 +51,27 @@ struct columns {
 #pragma unroll
                 for (int j = 0; j < WORDS; ++j) w[j] = v[j & 1];
             }
-        } else {
+        } else {                               // (rows shorter than W)
 #pragma unroll
             for (int j = 0; j < WORDS; ++j) w[j] = 0;
+            for (int j = 0; j < d; ++j) {
+                const uint32_t b = BF16 ? (uint32_t) static_cast<const uint16_t*>(row)[i + j] << (j & 1) * 16 : static_cast<const uint32_t*>(row)[i + j];
 #pragma unroll
-            for (int j = 0; j < W; ++j)
-                if (i + j < d) {
-                    const uint32_t b = BF16 ? (uint32_t) static_cast<const uint16_t*>(row)[i + j] << (j & 1) * 16 : static_cast<const uint32_t*>(row)[i + j];
-                    w[BF16 ? j / 2 : j] |= b;
-                }
+                for (int k = 0; k < WORDS; ++k) w[k] |= k == (BF16 ? j / 2 : j) ? b : 0;
+            }
         }
+    }
+    __device__ void here() {                   // (a load is not put off into the branch that uses it)
+#pragma unroll
+        for (int j = 0; j < WORDS; ++j) asm volatile("" : "+v"(w[j]));
     }
     __device__ float at(int j) const { return BF16 ? (j & 1 ? bf16hi(w[j >> 1]) : bf16lo(w[j >> 1])) : __uint_as_float(w[j % WORDS]); }
 };
-template <bool BF16, int W>
-__device__ inline void store_columns(void* row, int64_t i, int d, const float (&v)[W]) {
-    char* const at = static_cast<char*>(row) + i * (BF16 ? 2 : 4);
-    if (i + W <= d) {
+template <bool BF16, int W, bool TAIL>
+__device__ inline void store_columns(void* row, const piece<W, TAIL>& p, int d, const float (&v)[W]) {
+    if (!p.in_row) return;
+    char* const at = static_cast<char*>(row) + (int64_t)p.at * (BF16 ? 2 : 4);
+    if (!TAIL || (p.skip == 0 && d >= W)) {
         if (BF16 && W == 8)
             __builtin_nontemporal_store(u32x4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])}, reinterpret_cast<u32x4_any*>(at));
         else if (BF16) __builtin_nontemporal_store(u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])}, reinterpret_cast<u32x2_odd*>(at));
@@ -62,7 +83,7 @@ __device__ inline void store_columns(void* row, int64_t i, int d, const float (&
     } else {
 #pragma unroll
         for (int j = 0; j < W; ++j)
-            if (i + j < d) store1<BF16>(row, i + j, v[j]);
+            if (j >= p.skip && j < d) store1<BF16>(row, p.at + j, v[j]);
     }
 }
 // Columns of a thread: 16 bytes of the wider of the two rows
@@ -78,19 +99,18 @@ struct embed_args {
 };
 // y[t] = scale table[ids[t]]: a copy.  A block has a part of the columns of AT_ONCE tokens, all on their way at a time; rows of the table are kept in the caches,
 // tokens come again, y is written past them
-template <bool BF16, bool OUT_BF16>
+template <bool BF16, bool OUT_BF16, bool TAIL>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_kernel(const embed_args a) {
     constexpr int W = width_of(BF16, OUT_BF16), AT_ONCE = 4;
     const int64_t b = a.first + blockIdx.x, t0 = b / a.parts * AT_ONCE;
-    const int i = ((int)(b % a.parts) * blockDim.x + threadIdx.x) * W;
-    if (i >= a.d) return;
-    columns<BF16, W> v[AT_ONCE];
+    const piece<W, TAIL> p((int)(b % a.parts) * blockDim.x + threadIdx.x, a.d);
+    columns<BF16, W, TAIL> v[AT_ONCE];
     bool there[AT_ONCE];
 #pragma unroll
     for (int u = 0; u < AT_ONCE; ++u) {
-        const int id = t0 + u < a.T ? a.ids[t0 + u] : -1;
+        const int id = a.ids[t0 + u < a.T ? t0 + u : a.T - 1];
         there[u] = (uint32_t)id < (uint32_t)a.V;
-        if (there[u]) v[u].template load<false>(row_of<BF16>(a.table, id * a.ld), i, a.d);
+        v[u].load(row_of<BF16>(a.table, (there[u] ? id : 0) * a.ld), p.at, a.d);
     }
 #pragma unroll
     for (int u = 0; u < AT_ONCE; ++u) {
@@ -98,7 +118,7 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_kernel(const embed_args a
         float y[W];
 #pragma unroll
         for (int j = 0; j < W; ++j) y[j] = there[u] ? v[u].at(j) * a.scale : 0.f;
-        store_columns<OUT_BF16, W>(row_of<OUT_BF16>(a.y, (t0 + u) * a.ld_y), i, a.d, y);
+        store_columns<OUT_BF16>(row_of<OUT_BF16>(a.y, (t0 + u) * a.ld_y), p, a.d, y);
     }
 }
 
@@ -134,29 +154,57 @@ __device__ inline void clear_rows(const embed_back_args& a, int block, uint32_t*
     }
     __syncthreads();
     constexpr int W = OUT_BF16 ? 8 : 4;
-    const int pieces = (a.d + W - 1) / W, row_step = blockDim.x / pieces, piece_step = blockDim.x % pieces;
-    int row = threadIdx.x / pieces, piece = threadIdx.x % pieces;
+    const int pieces = (a.d + W - 1) / W, row_step = blockDim.x / pieces, at_step = blockDim.x % pieces;
+    int row = threadIdx.x / pieces, at = threadIdx.x % pieces;
     const float none[W] = {};
     while (row < rows) {
-        if (!(seen[row / 32] >> row % 32 & 1)) store_columns<OUT_BF16, W>(row_of<OUT_BF16>(a.dtable, (v0 + row) * a.ld_grad), piece * W, a.d, none);
+        if (!(seen[row / 32] >> row % 32 & 1)) store_columns<OUT_BF16>(row_of<OUT_BF16>(a.dtable, (v0 + row) * a.ld_grad), piece<W, true>(at, a.d), a.d, none);
         row += row_step;
-        piece += piece_step;
-        if (piece >= pieces) piece -= pieces, ++row;
+        at += at_step;
+        if (at >= pieces) at -= pieces, ++row;
     }
 }
 
 // A token's finished sum into its row
-template <bool OUT_BF16, bool ADD, int W>
-__device__ inline void finish(const embed_back_args& a, uint32_t id, int i, const columns<OUT_BF16, W>& was, const float (&sum)[W]) {
+template <bool OUT_BF16, bool ADD, int W, bool TAIL>
+__device__ inline void finish(const embed_back_args& a, uint32_t id, const piece<W, TAIL>& p, const columns<OUT_BF16, W, TAIL>& was, const float (&sum)[W]) {
     float g[W];
 #pragma unroll
     for (int j = 0; j < W; ++j) g[j] = ADD ? fmaf(sum[j], a.scale, was.at(j)) : sum[j] * a.scale;
-    store_columns<OUT_BF16, W>(row_of<OUT_BF16>(a.dtable, id * a.ld_grad), i, a.d, g);
+    store_columns<OUT_BF16>(row_of<OUT_BF16>(a.dtable, id * a.ld_grad), p, a.d, g);
+}
+// A thread's sums in the workspace, past the L2 caches of an XCD: another block will read them
+template <int W>
+__device__ inline void store_partial(float* at, const float (&sum)[W]) {
+#pragma unroll
+    for (int j = 0; j < W; j += 2)
+        __hip_atomic_store(reinterpret_cast<uint64_t*>(at) + j / 2, (uint64_t)__float_as_uint(sum[j + 1]) << 32 | __float_as_uint(sum[j]), __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+}
+// The sum of n of them, at(q)
+template <int W, class At>
+__device__ inline void join_partials(int64_t n, At at, float (&total)[W]) {
+    constexpr int AT_ONCE = 8;
+#pragma unroll
+    for (int j = 0; j < W; ++j) total[j] = 0.f;
+    for (int64_t q = 0; q < n; q += AT_ONCE) {
+        uint64_t v[AT_ONCE][W / 2];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const uint64_t* const theirs = reinterpret_cast<const uint64_t*>(at(q + u < n ? q + u : n - 1));
+#pragma unroll
+            for (int j = 0; j < W / 2; ++j) v[u][j] = __hip_atomic_load(theirs + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u)
+#pragma unroll
+            for (int j = 0; j < W; ++j) total[j] += q + u < n ? __uint_as_float((uint32_t)(v[u][j / 2] >> j % 2 * 32)) : 0.f;
+    }
 }
 
 // Few tokens in one launch, without sorting: a block looks through the ids for the others of its token, and has work if FEW_RUN divides the number of those in
 // front of it; the runs of a frequent token are joined by the last of their blocks.
-template <bool BF16, bool OUT_BF16, bool ADD>
+template <bool BF16, bool OUT_BF16, bool ADD, bool TAIL>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_few_kernel(const embed_back_args a) {
     constexpr int W = width_of(BF16, OUT_BF16), MASKS = FEW_TOKENS / 64, AT_ONCE = 8;
     __shared__ uint64_t s_same[MASKS];
@@ -168,7 +216,7 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_few_kernel(const embed_ba
         return;
     }
     const int t = (int)(blockIdx.x / a.parts), part = (int)(blockIdx.x % a.parts), T = (int)a.T;
-    const int i = (part * a.threads + threadIdx.x) * W;
+    const piece<W, TAIL> p(part * a.threads + threadIdx.x, a.d);
     const int id = a.ids[t];
     if ((uint32_t)id >= (uint32_t)a.V) return;
     for (int k = threadIdx.x; k < FEW_TOKENS; k += blockDim.x) {           // (a wave has 64 consecutive ones)
@@ -190,52 +238,31 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_few_kernel(const embed_ba
             s_list[__builtin_amdgcn_readlane(upto, k / 64) - __popcll(same >> lane)] = (uint16_t)k;
     }
     __syncthreads();
-    const bool whole = total <= FEW_RUN, in_row = i < a.d;
+    const bool whole = total <= FEW_RUN;
     const int left = min(FEW_RUN, total - ahead);
-    columns<OUT_BF16, W> was;
-    if (ADD && whole && in_row) was.load(row_of<OUT_BF16>(a.dtable, id * a.ld_grad), i, a.d);
+    columns<OUT_BF16, W, TAIL> was;
+    if (ADD && whole) was.load(row_of<OUT_BF16>(a.dtable, id * a.ld_grad), p.at, a.d);
     float sum[W] = {};
     for (int q = 0; q < left; q += AT_ONCE) {
-        columns<BF16, W> v[AT_ONCE];
+        columns<BF16, W, TAIL> v[AT_ONCE];
 #pragma unroll
         for (int u = 0; u < AT_ONCE; ++u)
-            if (q + u < left && in_row) v[u].load(row_of<BF16>(a.dy, __builtin_amdgcn_readfirstlane(s_list[ahead + q + u]) * a.ld), i, a.d);
+            v[u].load(row_of<BF16>(a.dy, __builtin_amdgcn_readfirstlane(s_list[ahead + min(q + u, left - 1)]) * a.ld), p.at, a.d);
 #pragma unroll
         for (int u = 0; u < AT_ONCE; ++u)
-            if (q + u < left && in_row)
 #pragma unroll
-                for (int j = 0; j < W; ++j) sum[j] += v[u].at(j);
+            for (int j = 0; j < W; ++j) sum[j] += q + u < left ? v[u].at(j) : 0.f;
     }
     if (whole) {
-        if (in_row) finish<OUT_BF16, ADD, W>(a, id, i, was, sum);
+        finish<OUT_BF16, ADD>(a, id, p, was, sum);
         return;
     }
     const int runs = (total + FEW_RUN - 1) / FEW_RUN;
-    if (in_row) {
-        float* const mine = a.partial + (int64_t)t * a.width + i;
-#pragma unroll
-        for (int j = 0; j < W; ++j) __hip_atomic_store(mine + j, sum[j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    if (!last_block(a.tickets + first * a.parts + part, runs, s_last) || !in_row) return;
-    if (ADD) was.load(row_of<OUT_BF16>(a.dtable, id * a.ld_grad), i, a.d);
-#pragma unroll
-    for (int j = 0; j < W; ++j) sum[j] = 0.f;
-    for (int q = 0; q < runs; q += AT_ONCE) {
-        float v[AT_ONCE][W];
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u)
-            if (q + u < runs) {
-                const float* const theirs = a.partial + (int64_t)s_list[(q + u) * FEW_RUN] * a.width + i;
-#pragma unroll
-                for (int j = 0; j < W; ++j) v[u][j] = __hip_atomic_load(theirs + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u)
-            if (q + u < runs)
-#pragma unroll
-                for (int j = 0; j < W; ++j) sum[j] += v[u][j];
-    }
-    finish<OUT_BF16, ADD, W>(a, id, i, was, sum);
+    if (p.in_row) store_partial(a.partial + (int64_t)t * a.width + p.nominal, sum);
+    if (!last_block(a.tickets + first * a.parts + part, runs, s_last)) return;
+    if (ADD) was.load(row_of<OUT_BF16>(a.dtable, id * a.ld_grad), p.at, a.d);
+    join_partials(runs, [&](int64_t q) { return a.partial + (int64_t)s_list[q * FEW_RUN] * a.width + p.nominal; }, sum);
+    finish<OUT_BF16, ADD>(a, id, p, was, sum);
 }
 
 // Keys (id, token) in ascending order: tokens of one id stand together in the order of the batch.  A token's place in its chunk is the number of tokens there that
@@ -245,156 +272,163 @@ template <bool OUT_BF16>
 __global__ __launch_bounds__(RANK_THREADS) void rank_tokens_kernel(const embed_back_args a, const int32_t* __restrict__ ids, int blocks, int chunk,
                                                                    uint64_t* __restrict__ out) {
     constexpr int WAVES = RANK_THREADS / 64;
-    __shared__ uint32_t s[ZERO_BITS / 32 > WAVES * 64 ? ZERO_BITS / 32 : WAVES * 64];
+    static_assert(RANK_ALONE >= RANK_CHUNK && RANK_ALONE % RANK_THREADS == 0 && RANK_ALONE >= ZERO_BITS / 32, "a wave's ids in whole groups of 64");
+    __shared__ u32x4 s_ids[RANK_ALONE / 4];
+    __shared__ uint32_t s_rank[WAVES][64];
     if ((int)blockIdx.x >= blocks) {
-        clear_rows<OUT_BF16>(a, blockIdx.x - blocks, s);
+        clear_rows<OUT_BF16>(a, blockIdx.x - blocks, reinterpret_cast<uint32_t*>(s_ids));
         return;
     }
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int T = (int)a.T, t0 = blockIdx.x * 64, t = t0 + lane, begin = t0 / chunk * chunk, end = min(begin + chunk, T);
-    const uint32_t V = (uint32_t)a.V, own = t < T ? (uint32_t)ids[t] : NO_ID, id = own < V ? own : NO_ID;
-    const int each = (end - begin + WAVES - 1) / WAVES, from = begin + wave * each, to = min(from + each, end);
-    uint32_t rank = 0;
-    auto at = [&](int j) {
-        const uint32_t o = (uint32_t)ids[j];
-        return o < V ? o : NO_ID;
+    const uint32_t V = (uint32_t)a.V;
+    auto known = [&](int j) {
+        const uint32_t id = j < end ? (uint32_t)ids[j] : NO_ID;
+        return id < V ? id : NO_ID;
     };
-    int j = from;
-#pragma unroll 8
-    for (; j < min(to, t0); ++j) rank += at(j) <= id;          // (in front: an equal one comes before)
-    for (; j < min(to, t0 + 64); ++j) {
-        const uint32_t o = at(j);
-        rank += (int)(o < id) | ((int)(o == id) & (int)(j < t));
+    const int each = ((end - begin + WAVES - 1) / WAVES + 63) / 64 * 64, from = begin + wave * each;
+    constexpr int GROUPS = RANK_ALONE / RANK_THREADS;
+    uint32_t theirs[GROUPS];                   // (all on their way at a time)
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) theirs[g] = known(g * 64 < each ? from + g * 64 + lane : end);
+    const uint32_t id = known(t);
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g)
+        if (g * 64 < each) reinterpret_cast<uint32_t*>(s_ids)[wave * each + g * 64 + lane] = theirs[g];
+    uint32_t rank = 0;
+    for (int g = 0; g < each; g += 64) {       // (a wave reads what it has written)
+        const u32x4* const of = s_ids + (wave * each + g) / 4;
+        const int j0 = from + g;
+        if (j0 < t0) {                         // in front: an equal one comes before
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) rank += of[q][k] <= id;
+        } else if (j0 > t0) {
+#pragma unroll
+            for (int q = 0; q < 16; ++q)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) rank += of[q][k] < id;
+        } else {
+            for (int q = 0; q < 16; ++q)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) rank += (int)(of[q][k] < id) | ((int)(of[q][k] == id) & (int)(q * 4 + k < lane));
+        }
     }
-#pragma unroll 8
-    for (; j < to; ++j) rank += at(j) < id;
-    s[wave * 64 + lane] = rank;
+    s_rank[wave][lane] = rank;
     __syncthreads();
     if (wave || t >= T) return;
-    for (int w = 1; w < WAVES; ++w) rank += s[w * 64 + lane];
+    for (int w = 1; w < WAVES; ++w) rank += s_rank[w][lane];
     out[begin + rank] = (uint64_t)id << 32 | (uint32_t)t;
 }
 
 // Sorted runs of `run` keys, MERGE_WAYS of them to one: a key's place is the number of keys in the runs that are smaller (no two are equal).  The searches of
 // eight runs go side by side, each step waits for the memory once.
-__global__ __launch_bounds__(EMBED_THREADS) void merge_tokens_kernel(const uint64_t* __restrict__ keys, int64_t T, int64_t run, uint64_t* __restrict__ out) {
-    const int64_t i = (int64_t)blockIdx.x * EMBED_THREADS + threadIdx.x;
+__global__ __launch_bounds__(EMBED_THREADS) void merge_tokens_kernel(const uint64_t* __restrict__ keys, int T, int run, uint64_t* __restrict__ out) {
+    const int i = blockIdx.x * EMBED_THREADS + threadIdx.x;
     if (i >= T) return;
     const uint64_t mine = keys[i];
-    const int64_t first = i / (run * MERGE_WAYS) * (run * MERGE_WAYS);
-    int64_t place = first;
-    for (int64_t at = first; at < T && at < first + run * MERGE_WAYS; at += run * MERGE_AT_ONCE) {
-        int64_t below[MERGE_AT_ONCE] = {};     // of each run
-        for (int64_t step = run; step > 0; step /= 2)          // (run: a power of two)
+    const int first = i / (run * MERGE_WAYS) * (run * MERGE_WAYS);
+    int place = first;
+    for (int at = first; at < T && at < first + run * MERGE_WAYS; at += run * MERGE_AT_ONCE) {
+        int below[MERGE_AT_ONCE] = {};         // of each run
+        for (int step = run; step > 0; step /= 2) {            // (run: a power of two)
+            uint64_t there[MERGE_AT_ONCE];
 #pragma unroll
-            for (int u = 0; u < MERGE_AT_ONCE; ++u) {
-                const int64_t to = at + u * run + below[u] + step;
-                if (below[u] + step <= run && to <= T && keys[to - 1] < mine) below[u] += step;
+            for (int u = 0; u < MERGE_AT_ONCE; ++u) there[u] = keys[min(at + u * run + below[u] + step, T) - 1];
+#pragma unroll
+            for (int u = 0; u < MERGE_AT_ONCE; ++u) {          // (no branches: the reads go out together)
+                const int to = below[u] + step;
+                below[u] = (int)(to <= run) & (int)(at + u * run + to <= T) & (int)(there[u] < mine) ? to : below[u];
             }
+        }
 #pragma unroll
         for (int u = 0; u < MERGE_AT_ONCE; ++u) place += below[u];
     }
     out[place] = mine;
 }
 
-// A run of sorted tokens and a part of the columns to a block, whatever the tokens' frequencies.  A token whose rows all lie in the run is finished here; the
-// sum of one that goes on from the run before, or into the next, is a partial one: places 2 run and 2 run + 1.
-template <bool BF16, bool OUT_BF16, bool ADD>
+// A run of sorted tokens and a part of the columns to a block, whatever the tokens' frequencies.  A token whose rows all lie in the run is finished here; of one
+// that goes on from the run before, or into the next, there are sums in several runs, places 2 run and 2 run + 1, which the last of their blocks joins.
+template <bool BF16, bool OUT_BF16, bool ADD, bool TAIL>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(const embed_back_args a) {
-    constexpr int W = width_of(BF16, OUT_BF16), AT_ONCE = ADD && !OUT_BF16 ? 4 : 8;
-    const int64_t b = a.first + blockIdx.x, r = b / a.parts, begin = r * a.run, end = begin + a.run < a.T ? begin + a.run : a.T;
-    const int i = ((int)(b % a.parts) * a.threads + threadIdx.x) * W, lane = threadIdx.x & 63;
-    if (i - lane * W >= a.d) return;           // (whole waves: the lanes below hold keys)
-    const bool in_row = i < a.d;
-    float sum[W] = {};
-    bool open = begin > 0 && id_of(a.keys[begin - 1]) == id_of(a.keys[begin]);         // the present token began in an earlier run
-    float* const head = a.partial + 2 * r * a.width + i;
-    for (int64_t p = begin; p < end; p += 64) {
-        const int rows = (int)(end - p < 64 ? end - p : 64);
-        const uint64_t key = lane < rows ? a.keys[p + lane] : ~(uint64_t)0;
-        const uint32_t id = id_of(key), token = (uint32_t)key, next = lane < rows && p + lane + 1 < a.T ? id_of(a.keys[p + lane + 1]) : NO_ID;
+    constexpr int W = width_of(BF16, OUT_BF16), AT_ONCE = SUM_AT_ONCE;
+    __shared__ int32_t s_last;
+    const int64_t r = blockIdx.x / a.parts, begin = r * a.run, end = begin + a.run < a.T ? begin + a.run : a.T;
+    const int part = (int)(blockIdx.x % a.parts), lane = threadIdx.x & 63;
+    const piece<W, TAIL> p(part * a.threads + threadIdx.x, a.d);
+    float sum[W] = {}, head[W] = {};
+    const uint32_t first_id = id_of(a.keys[begin]), last_id = id_of(a.keys[end - 1]);
+    const bool from_before = begin > 0 && first_id != NO_ID && id_of(a.keys[begin - 1]) == first_id;
+    const bool goes_on = end < a.T && last_id != NO_ID && id_of(a.keys[end]) == last_id;
+    bool open = from_before;                   // the present token began in an earlier run
+    for (int64_t k0 = begin; k0 < end; k0 += 64) {
+        const int rows = (int)(end - k0 < 64 ? end - k0 : 64);
+        const uint64_t key = lane < rows ? a.keys[k0 + lane] : ~(uint64_t)0;
+        const uint32_t id = id_of(key), token = (uint32_t)key, next = lane < rows && k0 + lane + 1 < a.T ? id_of(a.keys[k0 + lane + 1]) : NO_ID;
         const int known = __popcll(__ballot(id != NO_ID));     // (the others are the last ones)
         const uint64_t ends = __ballot(id != NO_ID && id != next);
         for (int q = 0; q < known; q += AT_ONCE) {
-            columns<BF16, W> v[AT_ONCE];
-            columns<OUT_BF16, W> was[AT_ONCE];
+            columns<BF16, W, TAIL> v[AT_ONCE];
+            columns<OUT_BF16, W, TAIL> was[AT_ONCE];
 #pragma unroll
             for (int u = 0; u < AT_ONCE; ++u) {
-                if (q + u >= known) continue;
-                if (in_row) v[u].load(row_of<BF16>(a.dy, (int64_t)(uint32_t)__builtin_amdgcn_readlane(token, q + u) * a.ld), i, a.d);
-                if (ADD && ends >> (q + u) & 1 && in_row)
-                    was[u].load(row_of<OUT_BF16>(a.dtable, (int64_t)(uint32_t)__builtin_amdgcn_readlane(id, q + u) * a.ld_grad), i, a.d);
+                const int k = min(q + u, known - 1);
+                v[u].load(row_of<BF16>(a.dy, (int64_t)(uint32_t)__builtin_amdgcn_readlane(token, k) * a.ld), p.at, a.d);
+                if (ADD) {                     // (of other rows than a token's last one, something near by)
+                    const bool wanted = ends >> k & 1;
+                    const void* const row = row_of<OUT_BF16>(a.dtable, (int64_t)(uint32_t)__builtin_amdgcn_readlane(id, k) * a.ld_grad);
+                    was[u].load(wanted ? row : a.keys, wanted ? p.at : lane * W, a.d);
+                }
             }
 #pragma unroll
             for (int u = 0; u < AT_ONCE; ++u) {
-                if (q + u >= known) continue;
 #pragma unroll
-                for (int j = 0; j < W; ++j) sum[j] += in_row ? v[u].at(j) : 0.f;
-                if (!(ends >> (q + u) & 1)) continue;
+                for (int j = 0; j < W; ++j) sum[j] += q + u < known ? v[u].at(j) : 0.f;
+                if (ADD) was[u].here();
+                if (!(ends >> (q + u) & 1)) continue;          // (no bits from `known` on)
                 if (open) {
 #pragma unroll
-                    for (int j = 0; j < W; ++j)
-                        if (in_row) head[j] = sum[j];
-                } else if (in_row) {
-                    finish<OUT_BF16, ADD, W>(a, (uint32_t)__builtin_amdgcn_readlane(id, q + u), i, was[u], sum);
+                    for (int j = 0; j < W; ++j) head[j] = sum[j];
+                } else {
+                    finish<OUT_BF16, ADD>(a, (uint32_t)__builtin_amdgcn_readlane(id, q + u), p, was[u], sum);
                 }
                 open = false;
 #pragma unroll
                 for (int j = 0; j < W; ++j) sum[j] = 0.f;
             }
         }
-        if (known < rows) return;
     }
-    if (end < a.T && in_row && id_of(a.keys[end]) == id_of(a.keys[end - 1])) {
-        float* const at = open ? head : head + a.width;
-#pragma unroll
-        for (int j = 0; j < W; ++j) at[j] = sum[j];
-    }
-}
+    auto place = [&](int64_t n) { return a.partial + n * a.width + p.nominal; };
+    if (from_before && !open && p.in_row) store_partial(place(2 * r), head);
+    if (goes_on && p.in_row) store_partial(place(open ? 2 * r : 2 * r + 1), sum);
 
-// Tokens whose rows lie in several runs: the block of the run in which one begins adds up the runs' sums, its waves a quarter of them each
-template <bool OUT_BF16, bool ADD>
-__global__ __launch_bounds__(EMBED_THREADS) void embed_join_kernel(const embed_back_args a) {
-    constexpr int W = 4, AT_ONCE = 8, WAVES = EMBED_THREADS / 64;
-    __shared__ float s_sum[WAVES][64 * W];
-    const int64_t b = a.first + blockIdx.x, r = b / a.parts, begin = r * a.run, end = begin + a.run;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, i = ((int)(b % a.parts) * 64 + lane) * W;
-    const uint32_t id = id_of(a.keys[end - 1]);
-    if (id == NO_ID || id_of(a.keys[end]) != id || (begin > 0 && id_of(a.keys[begin]) == id && id_of(a.keys[begin - 1]) == id)) return;
-    // the last run that begins with this token, by 64 at a time
-    const int64_t runs = (a.T + a.run - 1) / a.run;
-    int64_t last = r + 1;
-    for (;;) {
-        const int64_t at = last + 1 + lane;
-        const uint64_t same = __ballot(at < runs && id_of(a.keys[at * a.run]) == id);
-        last += __popcll(same);
-        if (~same) break;
-    }
-    // sums r: 2 r + 1, then 2 q of the runs q behind it
-    const int64_t n = last - r + 1, each = (n + WAVES - 1) / WAVES, from = wave * each, to = from + each < n ? from + each : n;
-    const bool in_row = i < a.d;
-    float sum[W] = {};
-    for (int64_t q = from; q < to; q += AT_ONCE) {
-        f32x4 v[AT_ONCE];
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u)
-            if (q + u < to && in_row) v[u] = *reinterpret_cast<const f32x4*>(a.partial + (q + u == 0 ? 2 * r + 1 : 2 * (r + q + u)) * a.width + i);
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u)
-            if (q + u < to && in_row)
-#pragma unroll
-                for (int j = 0; j < W; ++j) sum[j] += v[u][j];
-    }
-#pragma unroll
-    for (int j = 0; j < W; ++j) s_sum[wave][lane * W + j] = sum[j];
-    __syncthreads();
-    if (wave || !in_row) return;
-    columns<OUT_BF16, W> was;
-    if (ADD) was.load(row_of<OUT_BF16>(a.dtable, id * a.ld_grad), i, a.d);
-    for (int w = 1; w < WAVES; ++w)
-#pragma unroll
-        for (int j = 0; j < W; ++j) sum[j] += s_sum[w][lane * W + j];
-    finish<OUT_BF16, ADD, W>(a, id, i, was, sum);
+    // runs that this token goes through: from the one in which it begins to the one in which it ends, 64 looked at together
+    auto join = [&](uint32_t id, bool before, bool behind) {
+        int64_t from = r, to = r;
+        while (before) {
+            const int64_t q = from - 1 - lane; // whose last token is this one
+            const uint64_t same = __ballot(q >= 0 && id_of(a.keys[q >= 0 ? (q + 1) * a.run - 1 : 0]) == id);
+            from -= __popcll(same);
+            before = !~same;
+        }
+        const int64_t runs = (a.T + a.run - 1) / a.run;
+        while (behind) {
+            const int64_t q = to + 1 + lane;   // whose first token is this one
+            const uint64_t same = __ballot(q < runs && id_of(a.keys[q < runs ? q * a.run : 0]) == id);
+            to += __popcll(same);
+            behind = !~same;
+        }
+        if (!last_block(a.tickets + from * a.parts + part, (int)(to - from + 1), s_last)) return;
+        columns<OUT_BF16, W, TAIL> was;
+        if (ADD) was.load(row_of<OUT_BF16>(a.dtable, id * a.ld_grad), p.at, a.d);
+        float total[W];
+        join_partials(to - from + 1, [&](int64_t q) { return place(q == 0 ? 2 * from + 1 : 2 * (from + q)); }, total);
+        finish<OUT_BF16, ADD>(a, id, p, was, total);
+    };
+    const bool through = from_before && goes_on && first_id == last_id;
+    if (from_before) join(first_id, true, through);
+    if (goes_on && !through) join(last_id, false, true);
 }
 
 // blocks 0 .. n-1 in launches that a grid holds
@@ -427,14 +461,16 @@ hipError_t launch_embed_sums(moe_ctx* c, embed_back_args a) {
         a.partial = static_cast<float*>(c->grad_ws);
         a.tickets = c->grad_tickets;
         const unsigned grid = (unsigned)(a.sum_blocks + a.zero_blocks);
-        if (grid) embed_few_kernel<BF16, OUT_BF16, ADD><<<grid, a.threads, 0, c->stream>>>(a);
+        if (!grid) return hipSuccess;
+        if (a.d % width_of(BF16, OUT_BF16)) embed_few_kernel<BF16, OUT_BF16, ADD, true><<<grid, a.threads, 0, c->stream>>>(a);
+        else embed_few_kernel<BF16, OUT_BF16, ADD, false><<<grid, a.threads, 0, c->stream>>>(a);
         return hipGetLastError();
     }
     uint64_t *keys = static_cast<uint64_t*>(c->grad_ws), *other = keys + a.T;
     const int chunk = a.T <= RANK_ALONE ? RANK_ALONE : RANK_CHUNK, blocks = (int)((a.T + 63) / 64);
     rank_tokens_kernel<OUT_BF16><<<blocks + a.zero_blocks, RANK_THREADS, 0, c->stream>>>(a, a.ids, blocks, chunk, keys);
-    for (int64_t run = chunk; run < a.T; run *= MERGE_WAYS) {
-        merge_tokens_kernel<<<(unsigned)((a.T + EMBED_THREADS - 1) / EMBED_THREADS), EMBED_THREADS, 0, c->stream>>>(keys, a.T, run, other);
+    for (int run = chunk; run < a.T; run *= MERGE_WAYS) {
+        merge_tokens_kernel<<<(unsigned)((a.T + EMBED_THREADS - 1) / EMBED_THREADS), EMBED_THREADS, 0, c->stream>>>(keys, (int)a.T, run, other);
         uint64_t* const sorted = other;
         other = keys;
         keys = sorted;
@@ -443,12 +479,12 @@ hipError_t launch_embed_sums(moe_ctx* c, embed_back_args a) {
     a.partial = reinterpret_cast<float*>(static_cast<uint64_t*>(c->grad_ws) + (2 * a.T + 1) / 2 * 2);
     const int64_t room = (GRAD_WS_BYTES - 16 * (a.T + 1)) / (2 * sizeof(float) * a.width);
     a.run = 8;
-    while ((a.T + a.run - 1) / a.run > room || a.T / (2 * a.run) * a.parts >= 1024) a.run *= 2;
-    const int64_t runs = (a.T + a.run - 1) / a.run;
-    const hipError_t e = launch_blocks(c->stream, embed_sum_kernel<BF16, OUT_BF16, ADD>, a, runs * a.parts, a.threads);
-    if (e != hipSuccess || runs == 1) return e;
-    a.parts = (a.d + 255) / 256;
-    return launch_blocks(c->stream, embed_join_kernel<OUT_BF16, ADD>, a, (runs - 1) * a.parts, EMBED_THREADS);
+    while ((a.T + a.run - 1) / a.run > room || a.T / (2 * a.run) * a.parts >= EMBED_BLOCKS || (a.T + a.run - 1) / a.run * a.parts > GRAD_TICKETS) a.run *= 2;
+    a.tickets = c->grad_tickets;
+    const unsigned grid = (unsigned)((a.T + a.run - 1) / a.run * a.parts);
+    if (a.d % width_of(BF16, OUT_BF16)) embed_sum_kernel<BF16, OUT_BF16, ADD, true><<<grid, a.threads, 0, c->stream>>>(a);
+    else embed_sum_kernel<BF16, OUT_BF16, ADD, false><<<grid, a.threads, 0, c->stream>>>(a);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -461,8 +497,9 @@ hipError_t launch_embed(hipStream_t s, const int32_t* ids, int64_t T, const void
     cut_row((d + W - 1) / W, parts, threads);
     const embed_args a{ids, table, y, T, ld, ld_y, 0, V, d, parts, scale};
     const int64_t n = (T + 3) / 4 * parts;
-    if (bf16) return out_bf16 ? launch_blocks(s, embed_kernel<true, true>, a, n, threads) : launch_blocks(s, embed_kernel<true, false>, a, n, threads);
-    return out_bf16 ? launch_blocks(s, embed_kernel<false, true>, a, n, threads) : launch_blocks(s, embed_kernel<false, false>, a, n, threads);
+    auto launch = [&](auto kernel, auto tail_kernel) { return d % W ? launch_blocks(s, tail_kernel, a, n, threads) : launch_blocks(s, kernel, a, n, threads); };
+    if (bf16) return out_bf16 ? launch(embed_kernel<true, true, false>, embed_kernel<true, true, true>) : launch(embed_kernel<true, false, false>, embed_kernel<true, false, true>);
+    return out_bf16 ? launch(embed_kernel<false, true, false>, embed_kernel<false, true, true>) : launch(embed_kernel<false, false, false>, embed_kernel<false, false, true>);
 }
 
 hipError_t launch_embed_backward(moe_ctx* c, const void* dy, const int32_t* ids, int64_t T, int32_t V, int32_t d, int64_t ld, int32_t dtype, float scale,
