@@ -11,7 +11,7 @@ constexpr int64_t EMBED_MAX_GRID = 1 << 22;
 constexpr int FEW_TOKENS = 1024, FEW_RUN = 16;         // tokens that need no sorting, rows of one token that one block adds up
 constexpr int RANK_THREADS = 1024, RANK_CHUNK = 4096, RANK_ALONE = 8192, MERGE_WAYS = 32, MERGE_AT_ONCE = 8;
 constexpr int SUM_AT_ONCE = 8;                         // sorted rows that a thread has on their way
-constexpr int EMBED_BLOCKS = 1024;                     // that add up sorted tokens, about
+constexpr int EMBED_BLOCKS = 512;                      // that add up sorted tokens, about, of 2048 columns
 constexpr int ZERO_BITS = 4096;                        // rows that a block clears at most
 constexpr uint32_t NO_ID = 0xFFFFFFFFu;                // of tokens outside the table: behind the others
 
@@ -67,19 +67,22 @@ struct columns {
     }
     __device__ float at(int j) const { return BF16 ? (j & 1 ? bf16hi(w[j >> 1]) : bf16lo(w[j >> 1])) : __uint_as_float(w[j % WORDS]); }
 };
+template <class V>
+__device__ inline void store_any(const V& v, void* at) {
+    typedef V __attribute__((aligned(2))) any;
+    __builtin_nontemporal_store(v, static_cast<any*>(at));
+}
 template <bool BF16, int W, bool TAIL>
 __device__ inline void store_columns(void* row, const piece<W, TAIL>& p, int d, const float (&v)[W]) {
     if (!p.in_row) return;
     char* const at = static_cast<char*>(row) + (int64_t)p.at * (BF16 ? 2 : 4);
     if (!TAIL || (p.skip == 0 && d >= W)) {
-        if (BF16 && W == 8)
-            __builtin_nontemporal_store(u32x4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])}, reinterpret_cast<u32x4_any*>(at));
-        else if (BF16) __builtin_nontemporal_store(u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])}, reinterpret_cast<u32x2_odd*>(at));
+        if constexpr (BF16 && W == 8) store_any(u32x4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])}, at);
+        else if constexpr (BF16) store_any(u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])}, at);
         else
 #pragma unroll
             for (int h = 0; h < W; h += 4)
-                __builtin_nontemporal_store(u32x4{__float_as_uint(v[h]), __float_as_uint(v[h + 1]), __float_as_uint(v[h + 2]), __float_as_uint(v[h + 3])},
-                                            reinterpret_cast<u32x4_any*>(at + h * 4));
+                store_any(u32x4{__float_as_uint(v[h]), __float_as_uint(v[h + 1]), __float_as_uint(v[h + 2]), __float_as_uint(v[h + 3])}, at + h * 4);
     } else {
 #pragma unroll
         for (int j = 0; j < W; ++j)
@@ -142,27 +145,38 @@ struct embed_back_args {
 __device__ inline uint32_t id_of(uint64_t key) { return (uint32_t)(key >> 32); }
 
 // Rows of tokens that do not occur: each block looks through the batch for those of its rows that do
-template <bool OUT_BF16>
-__device__ inline void clear_rows(const embed_back_args& a, int block, uint32_t* seen) {
-    const int v0 = block * a.zero_rows, rows = min(a.zero_rows, a.V - v0);
-    for (int i = threadIdx.x; i < (rows + 31) / 32; i += blockDim.x) seen[i] = 0;
-    __syncthreads();
-    for (int64_t t = threadIdx.x; t < a.T; t += blockDim.x) {
-        const int id = a.ids[t];
-        const uint32_t at = (uint32_t)id - (uint32_t)v0;       // (ids in front of v0 wrap to large numbers)
-        if (at < (uint32_t)rows && id >= 0) atomicOr(&seen[at / 32], 1u << at % 32);
-    }
-    __syncthreads();
+template <bool OUT_BF16, bool TAIL>
+__device__ inline void clear_absent(const embed_back_args& a, int64_t v0, int rows, const uint32_t* seen) {
     constexpr int W = OUT_BF16 ? 8 : 4;
     const int pieces = (a.d + W - 1) / W, row_step = blockDim.x / pieces, at_step = blockDim.x % pieces;
     int row = threadIdx.x / pieces, at = threadIdx.x % pieces;
     const float none[W] = {};
     while (row < rows) {
-        if (!(seen[row / 32] >> row % 32 & 1)) store_columns<OUT_BF16>(row_of<OUT_BF16>(a.dtable, (v0 + row) * a.ld_grad), piece<W, true>(at, a.d), a.d, none);
+        if (!(seen[row / 32] >> row % 32 & 1)) store_columns<OUT_BF16, W, TAIL>(row_of<OUT_BF16>(a.dtable, (v0 + row) * a.ld_grad), piece<W, TAIL>(at, a.d), a.d, none);
         row += row_step;
         at += at_step;
         if (at >= pieces) at -= pieces, ++row;
     }
+}
+template <bool OUT_BF16>
+__device__ inline void clear_rows(const embed_back_args& a, int block, uint32_t* seen) {
+    const int v0 = block * a.zero_rows, rows = min(a.zero_rows, a.V - v0);
+    for (int i = threadIdx.x; i < (rows + 31) / 32; i += blockDim.x) seen[i] = 0;
+    __syncthreads();
+    constexpr int AT_ONCE = 8;
+    for (int64_t t = threadIdx.x; t < a.T; t += AT_ONCE * blockDim.x) {
+        int id[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) id[u] = a.ids[t + u * blockDim.x < a.T ? t + u * blockDim.x : t];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const uint32_t at = (uint32_t)id[u] - (uint32_t)v0;                // (ids in front of v0 wrap to large numbers)
+            if (at < (uint32_t)rows && id[u] >= 0) atomicOr(&seen[at / 32], 1u << at % 32);
+        }
+    }
+    __syncthreads();
+    if (a.d % 8) clear_absent<OUT_BF16, true>(a, v0, rows, seen);
+    else clear_absent<OUT_BF16, false>(a, v0, rows, seen);
 }
 
 // A token's finished sum into its row
@@ -266,60 +280,63 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_few_kernel(const embed_ba
 }
 
 // Keys (id, token) in ascending order: tokens of one id stand together in the order of the batch.  A token's place in its chunk is the number of tokens there that
-// come before it: 64 tokens to a block, one to a lane, and the chunk's ids, the same for all lanes, dealt to the 16 waves.  Two instructions for 64 comparisons on
-// all CUs take less than a sorting network on few: 4096 tokens 3 us, the network 17.  The other blocks of the launch clear rows.
-template <bool OUT_BF16>
-__global__ __launch_bounds__(RANK_THREADS) void rank_tokens_kernel(const embed_back_args a, const int32_t* __restrict__ ids, int blocks, int chunk,
-                                                                   uint64_t* __restrict__ out) {
-    constexpr int WAVES = RANK_THREADS / 64;
-    static_assert(RANK_ALONE >= RANK_CHUNK && RANK_ALONE % RANK_THREADS == 0 && RANK_ALONE >= ZERO_BITS / 32, "a wave's ids in whole groups of 64");
-    __shared__ u32x4 s_ids[RANK_ALONE / 4];
-    __shared__ uint32_t s_rank[WAVES][64];
+// come before it: TOKENS of them to a block, the chunk's ids dealt to the 16 waves and to 64 / TOKENS groups of lanes.  Two instructions for 64 comparisons on all
+// CUs take less than a sorting network on few: 4096 tokens FILL_RANK_US us, the network 17.  The other blocks of the launch clear rows.
+template <bool OUT_BF16, int TOKENS>
+__global__ __launch_bounds__(RANK_THREADS, 8) void rank_tokens_kernel(const embed_back_args a, const int32_t* __restrict__ ids, int blocks, int chunk,
+                                                                      uint64_t* __restrict__ out) {
+    constexpr int WAVES = RANK_THREADS / 64, SLICES = 64 / TOKENS, PAD = 4, LOADS = RANK_ALONE / RANK_THREADS;
+    constexpr uint32_t LAST = 0x7FFFFFFFu;     // in place of ids outside the table; one more is a number still
+    static_assert(RANK_ALONE >= RANK_CHUNK && RANK_ALONE % (RANK_THREADS * SLICES) == 0 && RANK_ALONE >= ZERO_BITS / 32, "whole groups of ids for each lane");
+    __shared__ u32x4 s_ids[(RANK_ALONE + WAVES * SLICES * PAD) / 4];
+    __shared__ uint32_t s_rank[WAVES][TOKENS];
     if ((int)blockIdx.x >= blocks) {
         clear_rows<OUT_BF16>(a, blockIdx.x - blocks, reinterpret_cast<uint32_t*>(s_ids));
         return;
     }
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int T = (int)a.T, t0 = blockIdx.x * 64, t = t0 + lane, begin = t0 / chunk * chunk, end = min(begin + chunk, T);
+    const int T = (int)a.T, t0 = blockIdx.x * TOKENS, t = t0 + lane % TOKENS, begin = t0 / chunk * chunk, end = min(begin + chunk, T);
     const uint32_t V = (uint32_t)a.V;
     auto known = [&](int j) {
-        const uint32_t id = j < end ? (uint32_t)ids[j] : NO_ID;
-        return id < V ? id : NO_ID;
+        const uint32_t id = j < end ? (uint32_t)ids[j] : LAST;
+        return id < V ? id : LAST;
     };
-    const int each = ((end - begin + WAVES - 1) / WAVES + 63) / 64 * 64, from = begin + wave * each;
-    constexpr int GROUPS = RANK_ALONE / RANK_THREADS;
-    uint32_t theirs[GROUPS];                   // (all on their way at a time)
+    const int each = ((end - begin + WAVES * SLICES - 1) / (WAVES * SLICES) + TOKENS - 1) / TOKENS * TOKENS, from = begin + wave * SLICES * each;
+    uint32_t theirs[LOADS];                    // (all on their way at a time)
 #pragma unroll
-    for (int g = 0; g < GROUPS; ++g) theirs[g] = known(g * 64 < each ? from + g * 64 + lane : end);
+    for (int g = 0; g < LOADS; ++g) theirs[g] = known(g * 64 + lane < SLICES * each ? from + g * 64 + lane : end);
     const uint32_t id = known(t);
+    uint32_t* const mine = reinterpret_cast<uint32_t*>(s_ids) + wave * SLICES * (each + PAD);
 #pragma unroll
-    for (int g = 0; g < GROUPS; ++g)
-        if (g * 64 < each) reinterpret_cast<uint32_t*>(s_ids)[wave * each + g * 64 + lane] = theirs[g];
+    for (int g = 0; g < LOADS; ++g) {
+        const int j = g * 64 + lane;
+        if (j < SLICES * each) mine[j + j / each * PAD] = theirs[g];
+    }
     uint32_t rank = 0;
-    for (int g = 0; g < each; g += 64) {       // (a wave reads what it has written)
-        const u32x4* const of = s_ids + (wave * each + g) / 4;
-        const int j0 = from + g;
-        if (j0 < t0) {                         // in front: an equal one comes before
+    const int slice = lane / TOKENS;
+    for (int g = 0; g < each; g += TOKENS) {   // (a wave reads what it has written)
+        const u32x4* const of = reinterpret_cast<const u32x4*>(mine + slice * (each + PAD) + g);
+        const int j0 = from + slice * each + g;
+        const uint32_t bound = j0 < t0 ? id + 1 : j0 > t0 ? id : 0;            // in front of this block's tokens an equal id comes before
+#pragma unroll 4
+        for (int q = 0; q < TOKENS / 4; ++q)
 #pragma unroll
-            for (int q = 0; q < 16; ++q)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) rank += of[q][k] <= id;
-        } else if (j0 > t0) {
-#pragma unroll
-            for (int q = 0; q < 16; ++q)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) rank += of[q][k] < id;
-        } else {
-            for (int q = 0; q < 16; ++q)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) rank += (int)(of[q][k] < id) | ((int)(of[q][k] == id) & (int)(q * 4 + k < lane));
+            for (int k = 0; k < 4; ++k) rank += of[q][k] < bound;
+    }
+    if (wave == 0 && lane < TOKENS) {          // this block's own
+        for (int k = 0; k < TOKENS; ++k) {
+            const uint32_t o = (uint32_t)__builtin_amdgcn_readlane((int)id, k);
+            rank += (int)(o < id) | ((int)(o == id) & (int)(k < lane));
         }
     }
-    s_rank[wave][lane] = rank;
+#pragma unroll
+    for (int o = TOKENS; o < 64; o *= 2) rank += (uint32_t)__shfl_xor((int)rank, o);
+    if (lane < TOKENS) s_rank[wave][lane] = rank;
     __syncthreads();
-    if (wave || t >= T) return;
+    if (wave || lane >= TOKENS || t >= T) return;
+#pragma unroll
     for (int w = 1; w < WAVES; ++w) rank += s_rank[w][lane];
-    out[begin + rank] = (uint64_t)id << 32 | (uint32_t)t;
+    out[begin + rank] = (uint64_t)(id == LAST ? NO_ID : id) << 32 | (uint32_t)t;
 }
 
 // Sorted runs of `run` keys, MERGE_WAYS of them to one: a key's place is the number of keys in the runs that are smaller (no two are equal).  The searches of
@@ -374,7 +391,7 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(const embed_ba
 #pragma unroll
             for (int u = 0; u < AT_ONCE; ++u) {
                 const int k = min(q + u, known - 1);
-                v[u].load(row_of<BF16>(a.dy, (int64_t)(uint32_t)__builtin_amdgcn_readlane(token, k) * a.ld), p.at, a.d);
+                v[u].template load<true>(row_of<BF16>(a.dy, (int64_t)(uint32_t)__builtin_amdgcn_readlane(token, k) * a.ld), p.at, a.d);
                 if (ADD) {                     // (of other rows than a token's last one, something near by)
                     const bool wanted = ends >> k & 1;
                     const void* const row = row_of<OUT_BF16>(a.dtable, (int64_t)(uint32_t)__builtin_amdgcn_readlane(id, k) * a.ld_grad);
@@ -450,8 +467,10 @@ hipError_t launch_embed_sums(moe_ctx* c, embed_back_args a) {
     cut_row(pieces, a.parts, a.threads);
     a.width = (a.d + 7) / 8 * 8;
     if (!ADD) {
-        // rows to a block: enough to make light of looking through the batch, and blocks for all CUs
-        int64_t rows = (a.V + 2047) / 2048;
+        // rows to a block: few, but twice the bytes of the ids that it looks through (4096 x 4096 f32 of 131072: 64 rows 437 us, 16 386; 32768 x 7168 bf16 496 and 502)
+        int64_t rows = (a.V + 8191) / 8192;
+        const int64_t bytes = (int64_t)a.d * (OUT_BF16 ? 2 : 4), least = (8 * a.T + bytes - 1) / bytes;
+        if (rows < least) rows = least;
         if (rows > ZERO_BITS) rows = ZERO_BITS;
         a.zero_rows = (int)rows;
         a.zero_blocks = (int)((a.V + rows - 1) / rows);
@@ -467,10 +486,12 @@ hipError_t launch_embed_sums(moe_ctx* c, embed_back_args a) {
         return hipGetLastError();
     }
     uint64_t *keys = static_cast<uint64_t*>(c->grad_ws), *other = keys + a.T;
-    const int chunk = a.T <= RANK_ALONE ? RANK_ALONE : RANK_CHUNK, blocks = (int)((a.T + 63) / 64);
-    rank_tokens_kernel<OUT_BF16><<<blocks + a.zero_blocks, RANK_THREADS, 0, c->stream>>>(a, a.ids, blocks, chunk, keys);
-    for (int run = chunk; run < a.T; run *= MERGE_WAYS) {
-        merge_tokens_kernel<<<(unsigned)((a.T + EMBED_THREADS - 1) / EMBED_THREADS), EMBED_THREADS, 0, c->stream>>>(keys, (int)a.T, run, other);
+    const bool alone = a.T <= RANK_ALONE;
+    const int chunk = alone ? RANK_ALONE : RANK_CHUNK, tokens = alone ? 16 : 64, blocks = (int)((a.T + tokens - 1) / tokens);
+    if (alone) rank_tokens_kernel<OUT_BF16, 16><<<blocks + a.zero_blocks, RANK_THREADS, 0, c->stream>>>(a, a.ids, blocks, chunk, keys);
+    else rank_tokens_kernel<OUT_BF16, 64><<<blocks + a.zero_blocks, RANK_THREADS, 0, c->stream>>>(a, a.ids, blocks, chunk, keys);
+    for (int64_t run = chunk; run < a.T; run *= MERGE_WAYS) {
+        merge_tokens_kernel<<<(unsigned)((a.T + EMBED_THREADS - 1) / EMBED_THREADS), EMBED_THREADS, 0, c->stream>>>(keys, (int)a.T, (int)run, other);
         uint64_t* const sorted = other;
         other = keys;
         keys = sorted;
@@ -479,7 +500,7 @@ hipError_t launch_embed_sums(moe_ctx* c, embed_back_args a) {
     a.partial = reinterpret_cast<float*>(static_cast<uint64_t*>(c->grad_ws) + (2 * a.T + 1) / 2 * 2);
     const int64_t room = (GRAD_WS_BYTES - 16 * (a.T + 1)) / (2 * sizeof(float) * a.width);
     a.run = 8;
-    while ((a.T + a.run - 1) / a.run > room || a.T / (2 * a.run) * a.parts >= EMBED_BLOCKS || (a.T + a.run - 1) / a.run * a.parts > GRAD_TICKETS) a.run *= 2;
+    while ((a.T + a.run - 1) / a.run > room || a.T / (2 * a.run) * a.parts * width_of(BF16, OUT_BF16) >= EMBED_BLOCKS * 8 || (a.T + a.run - 1) / a.run * a.parts > GRAD_TICKETS) a.run *= 2;
     a.tickets = c->grad_tickets;
     const unsigned grid = (unsigned)((a.T + a.run - 1) / a.run * a.parts);
     if (a.d % width_of(BF16, OUT_BF16)) embed_sum_kernel<BF16, OUT_BF16, ADD, true><<<grid, a.threads, 0, c->stream>>>(a);
