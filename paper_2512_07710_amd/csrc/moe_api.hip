@@ -428,13 +428,13 @@ int moe_grad_norm(moe_ctx* c, const void* const* grads, const int64_t* counts, c
 
 int moe_clip_grads(moe_ctx* c, const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n, const double* sum_sq, float max_norm,
                    void* const* outs) {
-    if (!c || !list_ok(grads, counts, dtypes, n) || !sum_sq || !aligned(sum_sq, 8) || !(max_norm >= 0.f) || !std::isfinite(max_norm)) return MOE_EINVAL;
+    if (!c || !c->grad_ws || !list_ok(grads, counts, dtypes, n) || !sum_sq || !aligned(sum_sq, 8) || !(max_norm >= 0.f) || !std::isfinite(max_norm)) return MOE_EINVAL;
     if (outs && n > 0 && !list_ok(outs, counts, dtypes, n)) return MOE_EINVAL;
     for (int32_t i = 0; outs && i < n; ++i) {                  // (a gradient that is shifted onto itself)
         const uintptr_t a = (uintptr_t)grads[i], b = (uintptr_t)outs[i], bytes = (uintptr_t)counts[i] * type_bytes(dtypes[i]);
         if (a != b && (a > b ? a - b : b - a) < bytes) return MOE_EINVAL;
     }
-    return hip_rc(launch_clip_grads(c->stream, grads, counts, dtypes, n, sum_sq, max_norm, outs));
+    return hip_rc(launch_clip_grads(c, grads, counts, dtypes, n, sum_sq, max_norm, outs));
 }
 
 int moe_profile_enable(moe_ctx* c, int32_t on) {

@@ -153,7 +153,7 @@ hipError_t launch_token_logp_backward(hipStream_t s, const void* logits, int64_t
                                       float temperature, const float* dlogp, const float* dentropy, const float* stats, const float* entropy,
                                       void* dlogits, int64_t ld_grad, int32_t grad_dtype);
 hipError_t launch_grad_norm(moe_ctx* c, const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n, double* sum_sq, float* norm);
-hipError_t launch_clip_grads(hipStream_t s, const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n, const double* sum_sq,
+hipError_t launch_clip_grads(moe_ctx* c, const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n, const double* sum_sq,
                              float max_norm, void* const* outs);
 size_t route_workspace_bytes(int E, int d);
 size_t route_partial_bytes(int T, int E);
