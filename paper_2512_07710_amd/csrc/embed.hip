@@ -233,9 +233,16 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_few_kernel(const embed_ba
     const piece<W, TAIL> p(part * a.threads + threadIdx.x, a.d);
     const int id = a.ids[t];
     if ((uint32_t)id >= (uint32_t)a.V) return;
-    for (int k = threadIdx.x; k < FEW_TOKENS; k += blockDim.x) {           // (a wave has 64 consecutive ones)
-        const uint64_t same = __ballot(k < T && a.ids[k < T ? k : 0] == id);
-        if ((threadIdx.x & 63) == 0) s_same[k / 64] = same;
+    for (int k0 = threadIdx.x; k0 < FEW_TOKENS; k0 += 4 * blockDim.x) {    // (a wave has 64 consecutive ones)
+        int other[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) other[u] = a.ids[min(k0 + u * (int)blockDim.x, T - 1)];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int k = k0 + u * blockDim.x;
+            const uint64_t same = __ballot(k < T && other[u] == id);
+            if ((threadIdx.x & 63) == 0 && k < FEW_TOKENS) s_same[k / 64] = same;
+        }
     }
     __syncthreads();
     // a lane has 64 tokens: how many occurrences there are up to them
