@@ -306,7 +306,8 @@ int moe_linear_fp8_wgrad(moe_ctx* ctx, const uint16_t* dy, int64_t rows, int32_t
 
 /* ---- The two ends of a policy step ------------------------------------------------------------------------------------
  * Token ids to rows in front of the layer and the table's gradient behind it; what a rollout logs about its tokens, as a function with a gradient of
- * its own; the norm of all gradients and the clipping to it.  dtype, ld, [reserved] and determinism as on the training side. */
+ * its own; the norm of all gradients and the clipping to it.  dtype, ld, [reserved] and determinism as on the training side.  Arrays of a call do not overlap,
+ * except where that is said. */
 
 /* Rows of an embedding: y[t] = scale * table[ids[t]], multiplied in fp32, rounded once to y's type.  Ids outside [0,V), padding among them, give a row of
  * zeros.  ids [T] i32; table [V,d] dtype, ld; y [T,d] out_dtype, ld_y.  T <= 2^30, 1 <= d <= 65536, lds below 2^31, scale finite. */

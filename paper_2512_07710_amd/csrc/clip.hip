@@ -117,6 +117,7 @@ __device__ inline bool last_piece(int32_t* tickets, uint32_t piece, uint32_t pie
     return last_to_arrive(DeviceCount{tickets + (1 + g) * GRAD_TICKET_INTS}, (int)((pieces - g + groups - 1) / groups)) && last_to_arrive(DeviceCount{tickets}, (int)groups);
 }
 // Squares in fp64: no fp32 number's is out of its range, and the sum of 2^40 of them has 13 digits.  The last block adds up the pieces' sums in their order.
+// Bound by the bytes: 700 gradients of 2.8 GB 460 us, 6.0 TB/s read; 60 of 0.8 MB 5.4, the load, the piece's sum and the two tickets one behind the other.
 template <bool ARGS>
 __global__ __launch_bounds__(LIST_THREADS) void squares_kernel(const list_args a, const list_table t, double* sums, int32_t* tickets, double* sum_sq, float* norm) {
     __shared__ double s[LIST_THREADS / 64];
@@ -167,7 +168,9 @@ __device__ inline float clip_factor(double sum_sq, float max_norm) {
     const double f = (double)max_norm / sqrt(sum_sq);
     return sum_sq == 0.0 || f >= 1.0 ? 1.f : (float)f;         // (NaN stays)
 }
-// The pieces from the last to the first: what the norm's pass has read last is in the caches still
+// The pieces from the last to the first: what the norm's pass has read last is in the caches still.  Bound by the bytes: the 700 gradients into others 1059 us,
+// 5.2 TB/s read and written; 60 small ones 2.4.  In two launches with the norm: the factor needs every piece's sum, and a wait inside a kernel for all blocks,
+// pieces kept in registers, would hold no more than 0.1 GB of them.
 template <bool ARGS>
 __global__ __launch_bounds__(LIST_THREADS) void clip_kernel(const list_args a, const list_table t, const double* __restrict__ sum_sq, float max_norm) {
     const float factor = clip_factor(*sum_sq, max_norm);

@@ -8,7 +8,9 @@ namespace {
 
 constexpr int EMBED_THREADS = 256;
 constexpr int64_t EMBED_MAX_GRID = 1 << 22;
-constexpr int FEW_TOKENS = 1024, FEW_RUN = 16;         // tokens that need no sorting, rows of one token that one block adds up
+constexpr int FEW_TOKENS = 1024, FEW_NARROW = 2048;    // tokens that need no sorting, and of at most FEW_ELEMENTS together
+constexpr int64_t FEW_ELEMENTS = (int64_t)5 << 20;
+constexpr int FEW_RUN = 16;                            // rows of one token that one block adds up
 constexpr int RANK_THREADS = 1024, RANK_CHUNK = 4096, RANK_ALONE = 8192, MERGE_WAYS = 32, MERGE_AT_ONCE = 8;
 constexpr int SUM_AT_ONCE = 8;                         // sorted rows that a thread has on their way
 constexpr int EMBED_BLOCKS = 512;                      // that add up sorted tokens, about, of 2048 columns
@@ -101,7 +103,8 @@ struct embed_args {
     float scale;
 };
 // y[t] = scale table[ids[t]]: a copy.  A block has a part of the columns of AT_ONCE tokens, all on their way at a time; rows of the table are kept in the caches,
-// tokens come again, y is written past them
+// tokens come again, y is written past them.  Bound by memory, mostly y: 32768 x 7168 bf16 of 12 thousand different tokens 132 us, 4.8 TB/s
+// with each row read once (a token after another 235); 1 x 4096 2.1 us, two loads one behind the other and a store.
 template <bool BF16, bool OUT_BF16, bool TAIL>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_kernel(const embed_args a) {
     constexpr int W = width_of(BF16, OUT_BF16), AT_ONCE = 4;
@@ -144,7 +147,8 @@ struct embed_back_args {
 };
 __device__ inline uint32_t id_of(uint64_t key) { return (uint32_t)(key >> 32); }
 
-// Rows of tokens that do not occur: each block looks through the batch for those of its rows that do
+// Rows of tokens that do not occur: each block looks through the batch for those of its rows that do, and clears the others past the caches (into them 8 % slower).
+// Bound by the writes: 1.72 GB beside 32768 ids' ranks 320 us, 5.4 TB/s.
 template <bool OUT_BF16, bool TAIL>
 __device__ inline void clear_absent(const embed_back_args& a, int64_t v0, int rows, const uint32_t* seen) {
     constexpr int W = OUT_BF16 ? 8 : 4;
@@ -217,12 +221,15 @@ __device__ inline void join_partials(int64_t n, At at, float (&total)[W]) {
 }
 
 // Few tokens in one launch, without sorting: a block looks through the ids for the others of its token, and has work if FEW_RUN divides the number of those in
-// front of it; the runs of a frequent token are joined by the last of their blocks.
-template <bool BF16, bool OUT_BF16, bool ADD, bool TAIL>
+// front of it; the runs of a frequent token are joined by the last of their blocks.  Bound by a chain of its token's id, all ids, the counts, the rows and the
+// result, five trips to memory: 777 x 2177 f32 added to 10.5 us for 14 MB, sorted 15.2.  A block looks through T ids, so only for few and narrow rows: 1000 x 7168
+// 19.0 us, sorted 20.5; 1500 x 1024 bf16 10.7 and 13.8, 1100 x 4096 14.9 and 16.0, 1100 x 7168 20.8 and 21.0, 2000 x 4096 bf16 19.6 and 17.2.  A form for 2048 tokens
+// of its own: with that one the 1000 x 7168 take 21.2.
+template <bool BF16, bool OUT_BF16, bool ADD, bool TAIL, int TOKENS>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_few_kernel(const embed_back_args a) {
-    constexpr int W = width_of(BF16, OUT_BF16), MASKS = FEW_TOKENS / 64, AT_ONCE = 8;
+    constexpr int W = width_of(BF16, OUT_BF16), MASKS = TOKENS / 64, AT_ONCE = 8;
     __shared__ uint64_t s_same[MASKS];
-    __shared__ uint16_t s_list[FEW_TOKENS];
+    __shared__ uint16_t s_list[TOKENS];
     __shared__ uint32_t s_seen[ZERO_BITS / 32];
     __shared__ int32_t s_last;
     if (blockIdx.x >= a.sum_blocks) {
@@ -233,7 +240,7 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_few_kernel(const embed_ba
     const piece<W, TAIL> p(part * a.threads + threadIdx.x, a.d);
     const int id = a.ids[t];
     if ((uint32_t)id >= (uint32_t)a.V) return;
-    for (int k0 = threadIdx.x; k0 < FEW_TOKENS; k0 += 4 * blockDim.x) {    // (a wave has 64 consecutive ones)
+    for (int k0 = threadIdx.x; k0 < TOKENS; k0 += 4 * blockDim.x) {    // (a wave has 64 consecutive ones)
         int other[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) other[u] = a.ids[min(k0 + u * (int)blockDim.x, T - 1)];
@@ -241,7 +248,7 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_few_kernel(const embed_ba
         for (int u = 0; u < 4; ++u) {
             const int k = k0 + u * blockDim.x;
             const uint64_t same = __ballot(k < T && other[u] == id);
-            if ((threadIdx.x & 63) == 0 && k < FEW_TOKENS) s_same[k / 64] = same;
+            if ((threadIdx.x & 63) == 0 && k < TOKENS) s_same[k / 64] = same;
         }
     }
     __syncthreads();
@@ -253,7 +260,7 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_few_kernel(const embed_ba
     if (ahead % FEW_RUN) return;
     const int group = __builtin_ctzll(__ballot(mine != 0)), first = group * 64 + __builtin_ctzll(s_same[group]);
     // the occurrences in their order
-    for (int k = threadIdx.x; k < FEW_TOKENS; k += blockDim.x) {
+    for (int k = threadIdx.x; k < TOKENS; k += blockDim.x) {
         const uint64_t same = s_same[k / 64];
         if (same >> lane & 1)
             s_list[__builtin_amdgcn_readlane(upto, k / 64) - __popcll(same >> lane)] = (uint16_t)k;
@@ -288,7 +295,7 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_few_kernel(const embed_ba
 
 // Keys (id, token) in ascending order: tokens of one id stand together in the order of the batch.  A token's place in its chunk is the number of tokens there that
 // come before it: TOKENS of them to a block, the chunk's ids dealt to the 16 waves and to 64 / TOKENS groups of lanes.  Two instructions for 64 comparisons on all
-// CUs take less than a sorting network on few: 4096 tokens FILL_RANK_US us, the network 17.  The other blocks of the launch clear rows.
+// CUs take less than a sorting network on few: 4096 tokens 5.3 us, the network 17.  The other blocks of the launch clear rows.
 template <bool OUT_BF16, int TOKENS>
 __global__ __launch_bounds__(RANK_THREADS, 8) void rank_tokens_kernel(const embed_back_args a, const int32_t* __restrict__ ids, int blocks, int chunk,
                                                                       uint64_t* __restrict__ out) {
@@ -347,7 +354,7 @@ __global__ __launch_bounds__(RANK_THREADS, 8) void rank_tokens_kernel(const embe
 }
 
 // Sorted runs of `run` keys, MERGE_WAYS of them to one: a key's place is the number of keys in the runs that are smaller (no two are equal).  The searches of
-// eight runs go side by side, each step waits for the memory once.
+// eight runs go side by side, each step waits for the memory once: 12 steps of 0.5 us, 32768 tokens 7.9 us.
 __global__ __launch_bounds__(EMBED_THREADS) void merge_tokens_kernel(const uint64_t* __restrict__ keys, int T, int run, uint64_t* __restrict__ out) {
     const int i = blockIdx.x * EMBED_THREADS + threadIdx.x;
     if (i >= T) return;
@@ -374,6 +381,8 @@ __global__ __launch_bounds__(EMBED_THREADS) void merge_tokens_kernel(const uint6
 
 // A run of sorted tokens and a part of the columns to a block, whatever the tokens' frequencies.  A token whose rows all lie in the run is finished here; of one
 // that goes on from the run before, or into the next, there are sums in several runs, places 2 run and 2 run + 1, which the last of their blocks joins.
+// Bound by rows of dy that lie anywhere, SUM_AT_ONCE of a thread on their way: 32768 x 7168 bf16 of 12 thousand different tokens 143 us, 4.5 TB/s; by its chain (keys, rows,
+// partial sums, ticket, join) where a block has eight rows: 4096 x 5120 bf16 added to f32 30 us.
 template <bool BF16, bool OUT_BF16, bool ADD, bool TAIL>
 __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(const embed_back_args a) {
     constexpr int W = width_of(BF16, OUT_BF16), AT_ONCE = SUM_AT_ONCE;
@@ -474,7 +483,7 @@ hipError_t launch_embed_sums(moe_ctx* c, embed_back_args a) {
     cut_row(pieces, a.parts, a.threads);
     a.width = (a.d + 7) / 8 * 8;
     if (!ADD) {
-        // rows to a block: few, but twice the bytes of the ids that it looks through (4096 x 4096 f32 of 131072: 64 rows 437 us, 16 386; 32768 x 7168 bf16 496 and 502)
+        // rows to a block: few, so that no block ends late, but twice the bytes of the ids that it looks through (4096 x 4096 f32 of 131072: 64 rows 437 us, 16 386; 32768 x 7168 bf16 496 and 502)
         int64_t rows = (a.V + 8191) / 8192;
         const int64_t bytes = (int64_t)a.d * (OUT_BF16 ? 2 : 4), least = (8 * a.T + bytes - 1) / bytes;
         if (rows < least) rows = least;
@@ -482,14 +491,16 @@ hipError_t launch_embed_sums(moe_ctx* c, embed_back_args a) {
         a.zero_rows = (int)rows;
         a.zero_blocks = (int)((a.V + rows - 1) / rows);
     }
-    if (a.T <= FEW_TOKENS && a.T * a.parts <= GRAD_TICKETS && a.T * a.width * sizeof(float) <= GRAD_WS_BYTES && a.zero_blocks <= EMBED_MAX_GRID / 2) {
+    const bool few = a.T <= FEW_TOKENS;
+    if ((few || (a.T <= FEW_NARROW && a.T * a.d <= FEW_ELEMENTS)) && a.T * a.parts <= GRAD_TICKETS && a.T * a.width * sizeof(float) <= GRAD_WS_BYTES && a.zero_blocks <= EMBED_MAX_GRID / 2) {
         a.sum_blocks = a.T * a.parts;
         a.partial = static_cast<float*>(c->grad_ws);
         a.tickets = c->grad_tickets;
         const unsigned grid = (unsigned)(a.sum_blocks + a.zero_blocks);
         if (!grid) return hipSuccess;
-        if (a.d % width_of(BF16, OUT_BF16)) embed_few_kernel<BF16, OUT_BF16, ADD, true><<<grid, a.threads, 0, c->stream>>>(a);
-        else embed_few_kernel<BF16, OUT_BF16, ADD, false><<<grid, a.threads, 0, c->stream>>>(a);
+        auto launch = [&](auto kernel) { kernel<<<grid, a.threads, 0, c->stream>>>(a); };
+        if (a.d % width_of(BF16, OUT_BF16)) launch(few ? embed_few_kernel<BF16, OUT_BF16, ADD, true, FEW_TOKENS> : embed_few_kernel<BF16, OUT_BF16, ADD, true, FEW_NARROW>);
+        else launch(few ? embed_few_kernel<BF16, OUT_BF16, ADD, false, FEW_TOKENS> : embed_few_kernel<BF16, OUT_BF16, ADD, false, FEW_NARROW>);
         return hipGetLastError();
     }
     uint64_t *keys = static_cast<uint64_t*>(c->grad_ws), *other = keys + a.T;
@@ -506,6 +517,7 @@ hipError_t launch_embed_sums(moe_ctx* c, embed_back_args a) {
     a.keys = keys;
     a.partial = reinterpret_cast<float*>(static_cast<uint64_t*>(c->grad_ws) + (2 * a.T + 1) / 2 * 2);
     const int64_t room = (GRAD_WS_BYTES - 16 * (a.T + 1)) / (2 * sizeof(float) * a.width);
+    // a run of 8 tokens, longer ones where there are enough blocks all the same, and where the workspace or the tickets would not hold the runs' sums
     a.run = 8;
     while ((a.T + a.run - 1) / a.run > room || a.T / (2 * a.run) * a.parts * width_of(BF16, OUT_BF16) >= EMBED_BLOCKS * 8 || (a.T + a.run - 1) / a.run * a.parts > GRAD_TICKETS) a.run *= 2;
     a.tickets = c->grad_tickets;

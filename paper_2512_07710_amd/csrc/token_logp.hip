@@ -203,6 +203,8 @@ __device__ inline void write_row(const logp_args& a, int64_t r, const softmax_st
 
 // One pass over a row, or a part of it, for the sums and the alternatives.  The n-th largest of the largest logits that 64 groups of threads have among
 // their first vectors bounds the alternatives from below, closely; what reaches the bound, a few times n logits, is held in LDS and ranked in the end.
+// Bound by the logits' bytes: 4096 x 131072 bf16, n = 8 187 us, 5.7 TB/s (a pass over the row for each alternative 4496);
+// an exponential for each logit is 16 % of the cycles.  Rows that end late bound the fewer ones: 333 x 50001 f32 17.5.
 template <bool BF16, int THREADS, bool PARTS>
 __global__ __launch_bounds__(THREADS, 8) void logp_kernel(const logp_args a) {
     typedef row_type<BF16> T;
@@ -361,7 +363,8 @@ struct logp_grad_args {
 };
 
 // dz[v] = (sum_j dlogp_j (1[v = id_j] - p_v) - dH p_v (log p_v + H)) / temperature = 2^y (a y + b), and more at the given tokens.  A block has a row or, of
-// few rows, a part of one: the row's sums are there already.
+// few rows, a part of one: the row's sums are there already.  Bound by the writes: 1024 x 131072 bf16 to bf16 102 us, 4.9 TB/s read and written; 100 x 50001 f32
+// in parts 8.9 (whole rows 22.6).
 template <bool BF16, bool GRAD_BF16>
 __global__ __launch_bounds__(LOGP_THREADS) void logp_grad_kernel(const logp_grad_args a) {
     typedef row_type<BF16> T;

@@ -124,6 +124,17 @@ def test_gradient(gpu_lib, T, V, d, load, type, out):
             assert torch.equal(g[absent], before.cuda()[absent] if accumulate else torch.zeros_like(g[absent]))
 
 
+@pytest.mark.parametrize("T,V,d,load", [(2048, 300, 2560, "zipf"), (2048, 300, 2561, "zipf"), (1025, 300, 5200, "uniform"), (2049, 300, 100, "one")])
+def test_gradient_where_the_rows_become_too_wide_for_one_launch(gpu_lib, T, V, d, load):
+    rng = np.random.default_rng(d)
+    ids, dy, before = _text(T, V, load, rng), randn((T, d), "bf16", 3), randn((V, d), "f32", 4, 3.0)
+    with Context(gpu_lib) as ctx:
+        for accumulate in (False, True):
+            g = before.cuda().clone()
+            gpu_lib.moe_embed_backward(ctx, dy.cuda(), _dev(ids), 0.75, g, accumulate)
+            _check_gradient(ids, dy, 0.75, f64(before), accumulate, "f32", g)
+
+
 @pytest.mark.parametrize("type,out", PAIRS)
 def test_gradient_of_strided_rows(gpu_lib, type, out):
     rng = np.random.default_rng(5)
