@@ -77,8 +77,8 @@ struct row_type {
 template <bool BF16, int N>
 __device__ inline void store_grad(void* row, int64_t i, const float (&g)[N]) {
     char* const p = static_cast<char*>(row) + i * N * (BF16 ? 2 : 4);
-    if (BF16 && N == 8) *reinterpret_cast<u32x4_any*>(p) = u32x4{bf16_pair(g[0], g[1]), bf16_pair(g[2], g[3]), bf16_pair(g[4], g[5]), bf16_pair(g[6], g[7])};
-    else if (BF16) *reinterpret_cast<u32x2_any*>(p) = u32x2{bf16_pair(g[0], g[1]), bf16_pair(g[2], g[3])};
+    if constexpr (BF16 && N == 8) *reinterpret_cast<u32x4_any*>(p) = u32x4{bf16_pair(g[0], g[1]), bf16_pair(g[2], g[3]), bf16_pair(g[4], g[5]), bf16_pair(g[6], g[7])};
+    else if constexpr (BF16) *reinterpret_cast<u32x2_any*>(p) = u32x2{bf16_pair(g[0], g[1]), bf16_pair(g[2], g[3])};
     else
 #pragma unroll
         for (int h = 0; h < N; h += 4)

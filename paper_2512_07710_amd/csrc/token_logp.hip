@@ -10,8 +10,13 @@ constexpr int64_t LOGP_MAX_GRID = 1 << 22;
 constexpr int FEW_THREADS = 512, PART_THREADS = 1024, FEW_ROWS_IN_PARTS = 32, MAX_PARTS = 64; // rows in parts: a block's threads, parts of a row at most
 constexpr int MAX_SPLIT_ROWS = 128;            // (two parts or more in 256 blocks)
 constexpr int AT_ONCE = 4;                     // vectors that a thread works on together
-constexpr int TOP_GROUPS = 64;                 // groups of a block's threads, whose largest logits make the bound for alternatives: at least LOGP_MAX_TOP
-constexpr int top_held(int threads) { return threads > 64 ? 1088 : 320; }  // logits that a block holds: LOGP_MAX_TOP and one for each thread at least
+constexpr int RANKED = 64;                     // held logits that are ranked together
+// groups of a block's threads, whose largest logits make the bound for n alternatives.  Ranking 128 takes 1.2 us more of a short call, but a third as many
+// logits reach the bound of 64 of them (100 x 131072 bf16, n = 64 21.5 us, with 64 groups 48; 4096 rows n = 64 231 and 301, n = 20 206 and 202)
+constexpr int FEW_TOP = 32, GROUPS_OF_FEW = 64, GROUPS_OF_MANY = 128;
+__device__ inline bool many_groups(int threads, int n) { return threads > 256 && n > FEW_TOP; }
+// logits that a block holds: several times what reaches the bound of a row of 131072 at random, and all parts' lists; 38 KB of LDS for each 512 threads of a CU's 2048
+constexpr int top_held(int threads) { return threads > 256 ? 4160 : threads > 64 ? 1088 : 320; }
 const float ABOVE_LOWEST = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, LOWEST) - 1);
 
 struct logp_args {
@@ -44,7 +49,6 @@ __device__ inline uint32_t ordered(float v) {
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ inline uint64_t key_of(float v, int i) { return (uint64_t)ordered(v) << 32 | (uint32_t)~i; }
-__device__ inline uint64_t key_unless_nan(float v, int i) { return v == v ? key_of(v, i) : 0; }
 __device__ inline float value_of(uint64_t key) {
     const uint32_t o = (uint32_t)(key >> 32);
     return __uint_as_float(o ^ (o >> 31 ? 0x80000000u : 0xFFFFFFFFu));
@@ -54,10 +58,10 @@ __device__ inline int index_of(uint64_t key) { return ~(int)(uint32_t)key; }
 template <int THREADS>
 struct top_scratch {
     static constexpr int HELD = top_held(THREADS);
-    float groups[TOP_GROUPS];
+    float groups[GROUPS_OF_MANY];
     float bound;
     int count;
-    uint64_t held[HELD], best[LOGP_MAX_TOP];
+    uint64_t least, tops[THREADS], held[HELD], best[LOGP_MAX_TOP], kept[LOGP_MAX_TOP];
 };
 // over the lanes of a group of SIZE consecutive ones, in each of them
 template <int SIZE, class F>
@@ -69,23 +73,16 @@ __device__ inline int over_group(int v, F f) {
     if (SIZE > 8) v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x140, 0xf, 0xf, true));      // row_mirror
     return v;
 }
-// Each group's largest into s.groups, from its threads'
-template <int THREADS>
-__device__ inline void group_largest(float v, top_scratch<THREADS>& s) {
-    constexpr int SIZE = THREADS / TOP_GROUPS;
-    const int g = over_group<SIZE>(__float_as_int(v), [](int x, int y) { return __float_as_int(fmaxf(__int_as_float(x), __int_as_float(y))); });
-    if (threadIdx.x % SIZE == 0) s.groups[threadIdx.x / SIZE] = __int_as_float(g);
-}
-// The n-th largest of s.groups: n different logits are not below it.  Called by the whole block, which has written groups.
-template <int THREADS>
-__device__ inline float nth_of_groups(int n, top_scratch<THREADS>& s) {
-    constexpr int SIZE = THREADS / TOP_GROUPS;
+// The n-th largest of the first GROUPS of s.groups: n different logits are not below it.  Called by the whole block, which has written groups.
+template <int GROUPS, int THREADS>
+__device__ inline float nth_of(int n, top_scratch<THREADS>& s) {
+    constexpr int SIZE = THREADS / GROUPS;
     __syncthreads();
     const int i = threadIdx.x / SIZE, j0 = threadIdx.x % SIZE;
     const float mine = s.groups[i];
     int rank = 0;
 #pragma unroll
-    for (int j = 0; j < TOP_GROUPS; j += SIZE) {               // (no branches: the reads go out together)
+    for (int j = 0; j < GROUPS; j += SIZE) {                   // (no branches: the reads go out together)
         const float v = s.groups[j + j0];
         rank += (int)(v > mine) | ((int)(v == mine) & (int)(j + j0 < i));
     }
@@ -93,6 +90,20 @@ __device__ inline float nth_of_groups(int n, top_scratch<THREADS>& s) {
     if (rank == n - 1 && j0 == 0) s.bound = mine;
     __syncthreads();
     return s.bound;
+}
+// The same of the largest that groups of threads have
+template <int GROUPS, int THREADS>
+__device__ inline float nth_of_largest(float v, int n, top_scratch<THREADS>& s) {
+    constexpr int SIZE = THREADS / GROUPS;
+    const int g = over_group<SIZE>(__float_as_int(v), [](int x, int y) { return __float_as_int(fmaxf(__int_as_float(x), __int_as_float(y))); });
+    if (threadIdx.x % SIZE == 0) s.groups[threadIdx.x / SIZE] = __int_as_float(g);
+    return nth_of<GROUPS>(n, s);
+}
+template <int THREADS>
+__device__ inline float bound_of(float v, int n, top_scratch<THREADS>& s) {
+    if constexpr (THREADS > 256)
+        if (__builtin_expect(many_groups(THREADS, n), 0)) return nth_of_largest<GROUPS_OF_MANY>(v, n, s);
+    return nth_of_largest<GROUPS_OF_FEW>(v, n, s);
 }
 // what keys of logits from a bound on are not below; masked ones never are
 __device__ inline uint64_t bound_key(float bound) { return (uint64_t)ordered(fmaxf(bound, ABOVE_LOWEST)) << 32; }
@@ -104,75 +115,135 @@ __device__ inline void hold(uint64_t key, top_scratch<THREADS>& s) {
 }
 // The n first of the held ones in s.best, in order: SIZE threads count who is before one.  Called by the whole block, with a barrier before and behind it
 template <int THREADS>
-__device__ inline void rank_held(int count, int n, top_scratch<THREADS>& s) {
-    constexpr int SIZE = THREADS / TOP_GROUPS;
+__device__ __forceinline__ void rank_held(int count, int n, top_scratch<THREADS>& s) {
+    constexpr int SIZE = THREADS / RANKED;
     const int i = threadIdx.x / SIZE, j0 = threadIdx.x % SIZE;
-    if (threadIdx.x < TOP_GROUPS && (count & -TOP_GROUPS) + (int)threadIdx.x >= count && count % TOP_GROUPS)
-        s.held[(count & -TOP_GROUPS) + threadIdx.x] = 0;
+    if (threadIdx.x < RANKED && (count & -RANKED) + (int)threadIdx.x >= count && count % RANKED)
+        s.held[(count & -RANKED) + threadIdx.x] = 0;
     __syncthreads();
-    for (int i0 = 0; i0 < count; i0 += TOP_GROUPS) {
+    for (int i0 = 0; i0 < count; i0 += RANKED) {
         const uint64_t mine = s.held[i0 + i];
         int rank = 0;
-        for (int k0 = 0; k0 < count; k0 += TOP_GROUPS)
-#pragma unroll
-            for (int k = 0; k < TOP_GROUPS; k += SIZE) rank += s.held[k0 + k + j0] > mine;
+        for (int k0 = 0; k0 < count; k0 += RANKED)
+#pragma unroll 8
+            for (int k = 0; k < RANKED; k += SIZE) rank += s.held[k0 + k + j0] > mine;
         rank = over_group<SIZE>(rank, [](int x, int y) { return x + y; });
         if (j0 == 0 && rank < n && i0 + i < count) s.best[rank] = mine;
     }
 }
-// Many held ones: a bound from the largest of 64 groups of them leaves little more than n.  Returns how many.
+// What of the held ones is not below `least`.  Returns how many.
 template <int THREADS>
-__device__ inline int thin_held(int count, int n, top_scratch<THREADS>& s) {
-    uint64_t top = 0;
-    for (int k = threadIdx.x; k < count; k += THREADS) top = s.held[k] > top ? s.held[k] : top;
-    group_largest<THREADS>(top ? value_of(top) : -INFINITY, s);
-    const uint64_t bound = bound_key(nth_of_groups<THREADS>(n, s));
+__device__ __forceinline__ int keep_held(int count, uint64_t least, top_scratch<THREADS>& s) {
     if (threadIdx.x == 0) s.count = 0;
     for (int k0 = 0; k0 < count; k0 += THREADS) {              // (into places that have been read)
         const uint64_t key = k0 + (int)threadIdx.x < count ? s.held[k0 + threadIdx.x] : 0;
         __syncthreads();
-        if (key >= bound) hold(key, s);
+        if (key >= least) hold(key, s);
     }
     __syncthreads();
     return s.count;
 }
-// Where too many logits reach the bound, all of them once more, THREADS at a time, with the last of the n first before them as the bound: at(i), i < count.
-// Returns how many are in s.best.
-template <int THREADS, class At>
-__device__ inline int select_all(int64_t count, int n, At at, top_scratch<THREADS>& s) {
-    __syncthreads();
-    if (threadIdx.x == 0) s.count = 0;
-    uint64_t bound = bound_key(LOWEST);
-    int held = 0;
-    for (int64_t i = threadIdx.x; i - threadIdx.x < count; i += THREADS) {
-        __syncthreads();
-        const uint64_t key = i < count ? at(i) : 0;
-        if (key > bound) hold(key, s);
-        __syncthreads();
-        const int now = s.count;
-        if (now == held) continue;             // (the same for the whole block)
-        held = now < n ? now : n;
-        __syncthreads();
-        rank_held<THREADS>(now, n, s);
-        __syncthreads();
-        if (threadIdx.x < held) s.held[threadIdx.x] = s.best[threadIdx.x];
-        if (threadIdx.x == 0) s.count = held;
-        if (held == n) bound = s.best[n - 1];
+// The n first of `count` held ones in s.best.  Returns their number.  Ranking takes count^2 / THREADS steps of a thread, so many are thinned first: by the bound
+// of the groups' largest, which leaves little more than n as a rule, and by the n-th of the threads' largest, which leaves n threads' at most.
+template <int THREADS>
+__device__ __forceinline__ int first_held(int count, int n, top_scratch<THREADS>& s) {
+    if (__builtin_expect(count > 2 * RANKED, 0)) {             // (a program that goes straight on is fetched sooner)
+        uint64_t top = 0;
+        for (int k = threadIdx.x; k < count; k += THREADS) top = s.held[k] > top ? s.held[k] : top;
+        s.tops[threadIdx.x] = top;
+        count = keep_held<THREADS>(count, bound_key(bound_of<THREADS>(top ? value_of(top) : -INFINITY, n, s)), s);
+        if (count > THREADS + RANKED) {        // (so that each thread has had one, and no two the same)
+            int rank = 0;
+#pragma unroll 8
+            for (int j = 0; j < THREADS; ++j) rank += s.tops[j] > top;
+            if (rank == n - 1) s.least = top;
+            __syncthreads();
+            count = keep_held<THREADS>(count, s.least, s);
+        }
     }
-    __syncthreads();
-    return held;
-}
-// The n first of what was held, or where that were too many, of all; in s.best.  Returns their number.
-template <int THREADS, class At>
-__device__ inline int select_top(int64_t all, int n, At at, top_scratch<THREADS>& s) {
-    __syncthreads();
-    int count = s.count;
-    if (count > s.HELD) return select_all<THREADS>(all, n, at, s);
-    if (count > 2 * TOP_GROUPS) count = thin_held<THREADS>(count, n, s);
     __syncthreads();
     rank_held<THREADS>(count, n, s);
     __syncthreads();
     return count < n ? count : n;
+}
+// A thread's vectors i, i + THREADS, .. of a row
+template <bool BF16, int THREADS>
+__device__ inline void load_vectors(u32x4 (&v)[AT_ONCE], const void* row, int i, int end) {
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) v[u] = i + u * THREADS < end ? row_type<BF16>::load(row, i + u * THREADS) : row_type<BF16>::none();
+}
+// the largest of each of them, and of all
+template <bool BF16>
+__device__ inline float largest_of(const u32x4 (&v)[AT_ONCE], float (&tops)[AT_ONCE]) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+        const u32x4 one[1] = {v[u]};
+        tops[u] = running_sums<BF16>::largest(one);
+        top = fmaxf(top, tops[u]);
+    }
+    return top;
+}
+// The logits of these vectors that reach the bound, and whose keys are not below `least`
+template <bool BF16, int THREADS>
+__device__ __forceinline__ void hold_above(const u32x4 (&v)[AT_ONCE], const float (&tops)[AT_ONCE], int i, float bound, uint64_t least, top_scratch<THREADS>& s) {
+    typedef row_type<BF16> T;
+    constexpr int N = T::N;
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+        if (!(tops[u] >= bound)) continue;
+        uint32_t above = 0;                    // a bit for each element.  Few lanes have one, seldom more
+#pragma unroll
+        for (int e = 0; e < N; ++e) above |= (uint32_t)(T::at(v[u], e) >= bound) << e;
+        while (above) {
+            const int at = __builtin_ctz(above);
+            float x = T::at(v[u], 0);
+#pragma unroll
+            for (int e = 1; e < N; ++e) x = e == at ? T::at(v[u], e) : x;
+            const uint64_t key = key_of(x, (i + u * THREADS) * N + at);
+            if (key >= least) hold(key, s);
+            above &= above - 1;
+        }
+    }
+}
+// Where too many logits reach the bound (they ascend, or many are equal), the vectors from `begin` to `end` and `extra` once more, AT_ONCE of each thread at a time:
+// with the n first of those before, and again with a higher bound, the last of the n first among those that found a place, as long as there are too many (each
+// time HELD - 2 n fewer or more).  4096 x 131072 bf16, n = 8: ascending rows 740 us, equal logits 750, the first half masked 350.  Returns how many are in s.best.
+template <bool BF16, int THREADS>
+__device__ __forceinline__ int select_again(const void* row, int begin, int end, float extra, int extra_at, int n, top_scratch<THREADS>& s) {
+    uint64_t least = bound_key(LOWEST);
+    int kept = 0;
+    for (int i = begin + threadIdx.x; i - (int)threadIdx.x < end;) {
+        u32x4 v[AT_ONCE];
+        float tops[AT_ONCE];
+        const float more = i - (int)threadIdx.x + AT_ONCE * THREADS < end ? -INFINITY : extra;
+        load_vectors<BF16, THREADS>(v, row, i, end);
+        const float top = largest_of<BF16>(v, tops);
+        int count = 0;
+        if (__syncthreads_or(fmaxf(top, more) >= value_of(least))) {
+            const uint64_t of_these = bound_key(bound_of<THREADS>(top, n, s));
+            least = of_these > least ? of_these : least;
+            if ((int)threadIdx.x < kept) s.held[threadIdx.x] = s.kept[threadIdx.x];
+            if (threadIdx.x == 0) s.count = kept;
+            __syncthreads();
+            int at = i;                        // (read again: held in registers meanwhile they would be taken from the pass before)
+            asm volatile("" : "+v"(at));
+            load_vectors<BF16, THREADS>(v, row, at, end);
+            largest_of<BF16>(v, tops);
+            hold_above<BF16, THREADS>(v, tops, at, value_of(least), least, s);
+            if (more >= value_of(least) && key_of(more, extra_at) >= least) hold(key_of(more, extra_at), s);
+            __syncthreads();
+            count = s.count;
+            const int found = first_held<THREADS>(count < s.HELD ? count : s.HELD, n, s);
+            if (found == n) least = s.best[n - 1];
+            if (count <= s.HELD) {
+                kept = found;
+                if ((int)threadIdx.x < kept) s.kept[threadIdx.x] = s.best[threadIdx.x];
+            }
+        }
+        if (count <= s.HELD) i += AT_ONCE * THREADS;
+    }
+    return kept;
 }
 
 // A row's results, from its sums and from `found` alternatives in s.best
@@ -201,7 +272,7 @@ __device__ inline void write_row(const logp_args& a, int64_t r, const softmax_st
     }
 }
 
-// One pass over a row, or a part of it, for the sums and the alternatives.  The n-th largest of the largest logits that 64 groups of threads have among
+// One pass over a row, or a part of it, for the sums and the alternatives.  The n-th largest of the largest logits that groups of threads have among
 // their first vectors bounds the alternatives from below, closely; what reaches the bound, a few times n logits, is held in LDS and ranked in the end.
 // Bound by the logits' bytes: 4096 x 131072 bf16, n = 8 187 us, 5.7 TB/s (a pass over the row for each alternative 4496);
 // an exponential for each logit is 16 % of the cycles.  Rows that end late bound the fewer ones: 333 x 50001 f32 17.5.
@@ -219,72 +290,44 @@ __global__ __launch_bounds__(THREADS, 8) void logp_kernel(const logp_args a) {
     const int last = !PARTS || part == a.parts - 1 ? a.V : end * N;        // (the last part has the elements behind the vectors)
     running_sums<BF16> sums(a.inv_temp * LOG2E);
     float bound = NAN;                         // what an alternative reaches (without alternatives nothing does)
-    // the logits of these vectors that reach the bound; tops: the largest of each
-    auto hold_above = [&](const u32x4(&v)[AT_ONCE], const float(&tops)[AT_ONCE], int i) {
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
-            if (!(tops[u] >= bound)) continue;
-            uint32_t above = 0;                // a bit for each element.  Few lanes have one, seldom more
-#pragma unroll
-            for (int e = 0; e < N; ++e) above |= (uint32_t)(T::at(v[u], e) >= bound) << e;
-            while (above) {
-                const int at = __builtin_ctz(above);
-                float x = T::at(v[u], 0);
-#pragma unroll
-                for (int e = 1; e < N; ++e) x = e == at ? T::at(v[u], e) : x;
-                hold(key_of(x, (i + u * THREADS) * N + at), s_top);
-                above &= above - 1;
-            }
-        }
-    };
-    auto largest = [&](const u32x4(&v)[AT_ONCE], float(&tops)[AT_ONCE]) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
-            const u32x4 one[1] = {v[u]};
-            tops[u] = sums.largest(one);
-            top = fmaxf(top, tops[u]);
-        }
-        return top;
-    };
-    auto load = [&](u32x4(&v)[AT_ONCE], int i) {
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) v[u] = i + u * THREADS < end ? T::load(z, i + u * THREADS) : T::none();
-    };
     int i = begin + tid;
     const float extra = end * N + tid < last ? load1<BF16>(z, end * N + tid) : -INFINITY;
     {
         u32x4 v[AT_ONCE];
         float tops[AT_ONCE];
-        load(v, i);
-        const float top = largest(v, tops);
+        load_vectors<BF16, THREADS>(v, z, i, end);
+        const float top = largest_of<BF16>(v, tops);
         if (n) {
-            group_largest<THREADS>(top, s_top);
             if (tid == 0) s_top.count = 0;
-            bound = fmaxf(nth_of_groups<THREADS>(n, s_top), LOWEST);
+            bound = fmaxf(bound_of<THREADS>(top, n, s_top), LOWEST);
         }
         sums.take(top);
         sums.sum(v);
         // n of the first vectors' logits are not below the bound, so one behind them that equals it has n before it
         const float behind = next_above(bound);
         bound = bound > LOWEST ? bound : behind;
-        if (top >= bound) hold_above(v, tops, i);
+        if (top >= bound) hold_above<BF16, THREADS>(v, tops, i, bound, 0, s_top);
         bound = behind;
     }
     for (i += AT_ONCE * THREADS; i - tid < end; i += AT_ONCE * THREADS) {
         u32x4 v[AT_ONCE];
         float tops[AT_ONCE];
-        load(v, i);
-        const float top = largest(v, tops);
+        load_vectors<BF16, THREADS>(v, z, i, end);
+        const float top = largest_of<BF16>(v, tops);
         sums.take(top);
         sums.sum(v);
-        if (top >= bound) hold_above(v, tops, i);
+        if (top >= bound) hold_above<BF16, THREADS>(v, tops, i, bound, 0, s_top);
     }
     if (extra >= bound) hold(key_of(extra, end * N + tid), s_top);
     sums.add_one(extra);
     softmax_stats st = block_join(sums.st, sums.c, s_scratch);
-    int found = n ? select_top<THREADS>(last - begin * N, n, [&](int64_t k) { return key_unless_nan(load1<BF16>(z, begin * N + k), (int)(begin * N + k)); }, s_top) : 0;
-    if (PARTS) {
+    int found = 0;
+    if (n) {
+        __syncthreads();
+        const int count = s_top.count;
+        found = __builtin_expect(count <= s_top.HELD, 1) ? first_held<THREADS>(count, n, s_top) : select_again<BF16, THREADS>(z, begin, end, extra, end * N + tid, n, s_top);
+    }
+    if constexpr (PARTS) {
         float* const mine = a.part_sums + (r * a.parts + part) * 3;
         uint64_t* const tops = a.part_tops + r * a.parts * n;
         if (tid == 0) {
@@ -300,6 +343,7 @@ __global__ __launch_bounds__(THREADS, 8) void logp_kernel(const logp_args a) {
         const float* const all = a.part_sums + r * a.parts * 3;
         auto at = [&](int64_t k) { return __hip_atomic_load(tops + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
         constexpr int EACH = MAX_PARTS * LOGP_MAX_TOP / THREADS;
+        static_assert(!PARTS || top_scratch<THREADS>::HELD >= MAX_PARTS * LOGP_MAX_TOP, "room for all parts' lists");
         uint64_t theirs[EACH];                 // (all on their way at a time)
 #pragma unroll
         for (int e = 0; e < EACH; ++e) theirs[e] = tid + e * THREADS < a.parts * n ? at(tid + e * THREADS) : 0;
@@ -315,8 +359,9 @@ __global__ __launch_bounds__(THREADS, 8) void logp_kernel(const logp_args a) {
         }
         if (n) {
             // the parts' lists as one: the bound from the first of each
-            const int firsts = TOP_GROUPS / a.parts;           // of each part
-            if (tid < TOP_GROUPS) s_top.groups[tid] = -INFINITY;
+            const bool many = many_groups(THREADS, n);
+            const int firsts = (many ? GROUPS_OF_MANY : GROUPS_OF_FEW) / a.parts;              // of each part
+            if (tid < GROUPS_OF_MANY) s_top.groups[tid] = -INFINITY;
             if (tid == 0) s_top.count = 0;
             __syncthreads();
 #pragma unroll
@@ -324,11 +369,12 @@ __global__ __launch_bounds__(THREADS, 8) void logp_kernel(const logp_args a) {
                 const int k = tid + e * THREADS;
                 if (k < a.parts * n && k % n < firsts) s_top.groups[k / n * firsts + k % n] = theirs[e] ? value_of(theirs[e]) : -INFINITY;
             }
-            const uint64_t first = bound_key(nth_of_groups<THREADS>(n, s_top));
+            const uint64_t first = bound_key(many ? nth_of<GROUPS_OF_MANY>(n, s_top) : nth_of<GROUPS_OF_FEW>(n, s_top));
 #pragma unroll
             for (int e = 0; e < EACH; ++e)
                 if (theirs[e] >= first) hold(theirs[e], s_top);
-            found = select_top<THREADS>(a.parts * n, n, at, s_top);
+            __syncthreads();
+            found = first_held<THREADS>(s_top.count, n, s_top);
         }
         __syncthreads();
         if (tid == 0) {

@@ -109,6 +109,31 @@ def test_alternatives_in_every_order(gpu_lib, rows, V, n, how, type):
         _check_forward(z, ids, n, 1.0, _forward(gpu_lib, ctx, z, ids, n))
 
 
+def _crowded(V, how, type):
+    """Rows in which many logits reach what the first ones promise."""
+    step, noise = torch.arange(V).double(), randn((V,), "f32", 21).double()
+    z = {"rising": step / V * 20, "equal": step * 0 - 2, "rising noise": noise + step / V * 30, "steps": torch.floor(step / 5000), "noise": noise,
+         "open behind": torch.where(step < V * 3 // 4, float("-inf"), noise), "one open, then equal": torch.where(step < 20000, float("-inf"), 1.0)}[how]
+    if how == "one open, then equal":
+        z[5] = 0.5
+    z[V - 2] = float("-inf")
+    return z.to(TYPES[type])
+
+
+@pytest.mark.parametrize("type", ["bf16", "f32"])
+@pytest.mark.parametrize("how", ["rising", "equal", "rising noise", "steps", "noise", "open behind", "one open, then equal"])
+@pytest.mark.parametrize("rows,V", [(3, 270001), (130, 100003), (650, 50005)])
+def test_many_alternatives_for_a_place(gpu_lib, rows, V, how, type):
+    z = _crowded(V, how, type).reshape(1, V)
+    ids = np.array([[7, V - 1]], dtype=np.int32)
+    with Context(gpu_lib) as ctx:
+        for n in (1, 33, 64):
+            got = _forward(gpu_lib, ctx, z.repeat(rows, 1), np.tile(ids, (rows, 1)), n)
+            _check_forward(z, ids, n, 1.0, [x[:1] for x in got])
+            for x in got:
+                assert torch.equal(x, x[:1].expand_as(x))
+
+
 @pytest.mark.parametrize("type", ["bf16", "f32"])
 @pytest.mark.parametrize("V", [40, 3001, 70000])
 def test_masks(gpu_lib, V, type):
