@@ -175,7 +175,7 @@ __device__ inline void clear_rows(const embed_back_args& a, int block, uint32_t*
 #pragma unroll
         for (int u = 0; u < AT_ONCE; ++u) {
             const uint32_t at = (uint32_t)id[u] - (uint32_t)v0;                // (ids in front of v0 wrap to large numbers)
-            if (at < (uint32_t)rows && id[u] >= 0) atomicOr(&seen[at / 32], 1u << at % 32);
+            if (at < (uint32_t)rows && id[u] >= 0 && !(seen[at / 32] >> at % 32 & 1)) atomicOr(&seen[at / 32], 1u << at % 32);     // (once for a frequent token)
         }
     }
     __syncthreads();

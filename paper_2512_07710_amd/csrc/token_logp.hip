@@ -411,8 +411,8 @@ struct logp_grad_args {
 // dz[v] = (sum_j dlogp_j (1[v = id_j] - p_v) - dH p_v (log p_v + H)) / temperature = 2^y (a y + b), and more at the given tokens.  A block has a row or, of
 // few rows, a part of one: the row's sums are there already.  Bound by the writes: 1024 x 131072 bf16 to bf16 102 us, 4.9 TB/s read and written; 100 x 50001 f32
 // in parts 8.9 (whole rows 22.6).
-template <bool BF16, bool GRAD_BF16>
-__global__ __launch_bounds__(LOGP_THREADS) void logp_grad_kernel(const logp_grad_args a) {
+template <bool BF16, bool GRAD_BF16, int THREADS>
+__global__ __launch_bounds__(THREADS) void logp_grad_kernel(const logp_grad_args a) {
     typedef row_type<BF16> T;
     constexpr int N = T::N;
     __shared__ float s_d[LOGP_MAX_GIVEN], s_v[LOGP_MAX_GIVEN];
@@ -441,7 +441,7 @@ __global__ __launch_bounds__(LOGP_THREADS) void logp_grad_kernel(const logp_grad
     live &= !(m == -INFINITY && s == 0.f);
     if (!live) {                               // (the same for the whole block)
         const float none[N] = {};
-        for (int i = begin + tid; i < end; i += LOGP_THREADS) store_grad<GRAD_BF16, N>(out, i, none);
+        for (int i = begin + tid; i < end; i += THREADS) store_grad<GRAD_BF16, N>(out, i, none);
         if (behind < last) store1<GRAD_BF16>(out, behind, 0.f);
         return;
     }
@@ -459,17 +459,17 @@ __global__ __launch_bounds__(LOGP_THREADS) void logp_grad_kernel(const logp_grad
         store_grad<GRAD_BF16, N>(out, i, g);
     };
     int i = begin + tid;
-    for (; i + (AT_ONCE - 1) * LOGP_THREADS < end; i += AT_ONCE * LOGP_THREADS) {
+    for (; i + (AT_ONCE - 1) * THREADS < end; i += AT_ONCE * THREADS) {
         u32x4 v[AT_ONCE];
 #pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) v[u] = T::load(z, i + u * LOGP_THREADS);
+        for (int u = 0; u < AT_ONCE; ++u) v[u] = T::load(z, i + u * THREADS);
 #pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) put(v[u], i + u * LOGP_THREADS);
+        for (int u = 0; u < AT_ONCE; ++u) put(v[u], i + u * THREADS);
     }
-    for (; i < end; i += LOGP_THREADS) put(T::load(z, i), i);
+    for (; i < end; i += THREADS) put(T::load(z, i), i);
     if (behind < last) store1<GRAD_BF16>(out, behind, of(extra));
     // the given tokens, by the threads that have written their places: one with several gradients receives their sum as often
-    const int owner = id < end * N ? (id / N - begin) % LOGP_THREADS : id - end * N;
+    const int owner = id < end * N ? (id / N - begin) % THREADS : id - end * N;
     const bool here = id >= begin * N && id < last && owner >> 6 == tid >> 6 && !(v_id <= LOWEST);
     for (uint64_t left = __ballot(here); left; left &= left - 1) {
         const int j = __builtin_ctzll(left), to = __builtin_amdgcn_readlane(id, j);
@@ -493,6 +493,16 @@ hipError_t launch_whole(hipStream_t s, const logp_args& a, int vecs) {
     if (vecs <= 256 * AT_ONCE) return launch_rows<256>(s, logp_kernel<BF16, 256, false>, a, a.rows);
     if (vecs > 1024 * AT_ONCE && a.rows <= 640) return launch_rows<1024>(s, logp_kernel<BF16, 1024, false>, a, a.rows);
     return launch_rows<512>(s, logp_kernel<BF16, 512, false>, a, a.rows);
+}
+
+// Many short rows in blocks of one wave (65536 x 100 bf16 31.6 us, in larger ones 87; 8192 x 2000 14.4 and 16.4; but 500 x 2000 to f32 5.1 and 4.0)
+template <bool BF16>
+hipError_t launch_gradient(hipStream_t s, const logp_grad_args& a, bool grad_bf16, int vecs) {
+    const int64_t n = a.rows * a.parts;
+    if (vecs <= 64 * AT_ONCE && a.rows >= 2048)
+        return grad_bf16 ? launch_rows<64>(s, logp_grad_kernel<BF16, true, 64>, a, n) : launch_rows<64>(s, logp_grad_kernel<BF16, false, 64>, a, n);
+    return grad_bf16 ? launch_rows<LOGP_THREADS>(s, logp_grad_kernel<BF16, true, LOGP_THREADS>, a, n)
+                     : launch_rows<LOGP_THREADS>(s, logp_grad_kernel<BF16, false, LOGP_THREADS>, a, n);
 }
 
 }  // namespace
@@ -528,12 +538,7 @@ hipError_t launch_token_logp_backward(hipStream_t s, const void* logits, int64_t
         if (parts > 1) a.parts = (int)parts;
         a.part_vecs = (vecs + a.parts - 1) / a.parts;
     }
-    const int64_t n = rows * a.parts;
-    if (dtype == MOE_BF16)
-        return grad_dtype == MOE_BF16 ? launch_rows<LOGP_THREADS>(s, logp_grad_kernel<true, true>, a, n)
-                                      : launch_rows<LOGP_THREADS>(s, logp_grad_kernel<true, false>, a, n);
-    return grad_dtype == MOE_BF16 ? launch_rows<LOGP_THREADS>(s, logp_grad_kernel<false, true>, a, n)
-                                  : launch_rows<LOGP_THREADS>(s, logp_grad_kernel<false, false>, a, n);
+    return dtype == MOE_BF16 ? launch_gradient<true>(s, a, grad_dtype == MOE_BF16, vecs) : launch_gradient<false>(s, a, grad_dtype == MOE_BF16, vecs);
 }
 
 }  // namespace moe355

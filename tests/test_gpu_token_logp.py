@@ -256,6 +256,19 @@ def test_backward(gpu_lib, shape, type, out):
                 assert torch.equal(g, _backward(gpu_lib, ctx, z, ids, dlogp, h, fwd, out, 0.8, in_place=True))
 
 
+@pytest.mark.parametrize("type,out", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("V,m", [(1, 1), (70, 3), (1023, 2), (2048, 1)])
+def test_backward_of_many_short_rows(gpu_lib, V, m, type, out):
+    rows = 2050
+    z, ids = _inputs(rows, V, m, type, 22)
+    ids[::7] = -1
+    dlogp, dH = randn((rows, m), "f32", 23), randn((rows,), "f32", 24)
+    with Context(gpu_lib) as ctx:
+        got = _forward(gpu_lib, ctx, z, ids, 0, 1.3)
+        grad = _backward(gpu_lib, ctx, z, ids, dlogp, dH, got, out, 1.3)
+        _check_backward(z, ids, dlogp, dH, 1.3, out, grad)
+
+
 def test_rows_without_effect_are_zeros_whatever_they_hold(gpu_lib):
     z, ids = _inputs(4, 500, 2, "f32", 12)
     z[1] = float("nan")
