@@ -20,7 +20,7 @@ struct list_entry {
 // Gradients cut into pieces of `chunk` elements, one for each block; first: a gradient's first piece
 struct list_args {
     list_entry entry[LIST_ARGS];
-    uint32_t first[LIST_ARGS];                         // (~0 behind the last gradient)
+    uint32_t first[LIST_ARGS];
 };
 struct list_table {
     const list_entry* entry;

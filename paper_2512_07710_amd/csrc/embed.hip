@@ -13,6 +13,7 @@ constexpr int64_t FEW_ELEMENTS = (int64_t)5 << 20;
 constexpr int FEW_RUN = 16;                            // rows of one token that one block adds up
 constexpr int RANK_THREADS = 1024, RANK_CHUNK = 4096, RANK_ALONE = 8192, MERGE_WAYS = 32, MERGE_AT_ONCE = 8;
 constexpr int SUM_AT_ONCE = 8;                         // sorted rows that a thread has on their way
+constexpr int JOIN_AT_ONCE = 8, JOIN_TWICE = 32;        // sums of a token's runs that a thread has on their way, and from how many on they are joined in groups first
 constexpr int EMBED_BLOCKS = 512;                      // that add up sorted tokens, about, of 2048 columns
 constexpr int ZERO_BITS = 4096;                        // rows that a block clears at most
 constexpr uint32_t NO_ID = 0xFFFFFFFFu;                // of tokens outside the table: behind the others
@@ -202,7 +203,7 @@ __device__ inline void store_partial(float* at, const float (&sum)[W]) {
 // The sum of n of them, at(q)
 template <int W, class At>
 __device__ inline void join_partials(int64_t n, At at, float (&total)[W]) {
-    constexpr int AT_ONCE = 8;
+    constexpr int AT_ONCE = JOIN_AT_ONCE;
 #pragma unroll
     for (int j = 0; j < W; ++j) total[j] = 0.f;
     for (int64_t q = 0; q < n; q += AT_ONCE) {
@@ -380,7 +381,8 @@ __global__ __launch_bounds__(EMBED_THREADS) void merge_tokens_kernel(const uint6
 }
 
 // A run of sorted tokens and a part of the columns to a block, whatever the tokens' frequencies.  A token whose rows all lie in the run is finished here; of one
-// that goes on from the run before, or into the next, there are sums in several runs, places 2 run and 2 run + 1, which the last of their blocks joins.
+// that goes on from the run before, or into the next, there are sums in several runs, places 2 run and 2 run + 1, which the last of their blocks joins; of many
+// runs the last of each group first (4096 x 5120 bf16 of one token added to f32 34 us, half of them 37; joined by one block 55 and 41).
 // Bound by rows of dy that lie anywhere, SUM_AT_ONCE of a thread on their way: 32768 x 7168 bf16 of 12 thousand different tokens 143 us, 4.5 TB/s; by its chain (keys, rows,
 // partial sums, ticket, join) where a block has eight rows: 4096 x 5120 bf16 added to f32 30 us.
 template <bool BF16, bool OUT_BF16, bool ADD, bool TAIL>
@@ -452,11 +454,24 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(const embed_ba
             to += __popcll(same);
             behind = !~same;
         }
-        if (!last_block(a.tickets + from * a.parts + part, (int)(to - from + 1), s_last)) return;
+        auto sum_of = [&](int64_t q) { return place(q == from ? 2 * q + 1 : 2 * q); };         // of run q
+        int64_t all = to - from + 1;
+        int group = 1;
+        float total[W];
+        if (all >= JOIN_TWICE) {
+            while ((int64_t)group * group < all) group += JOIN_AT_ONCE;
+            const int64_t groups = all / group, mine = (r - from) / group < groups ? (r - from) / group : groups - 1, first = from + mine * group;
+            const int64_t n = mine == groups - 1 ? to - first + 1 : group;
+            // (the ticket of a run in which no other token begins)
+            if (!last_block(a.tickets + (first + 1) * a.parts + part, (int)n, s_last)) return;
+            join_partials(n, [&](int64_t q) { return sum_of(first + q); }, total);
+            if (p.in_row) store_partial(sum_of(first), total);
+            all = groups;
+        }
+        if (!last_block(a.tickets + from * a.parts + part, (int)all, s_last)) return;
         columns<OUT_BF16, W, TAIL> was;
         if (ADD) was.load(row_of<OUT_BF16>(a.dtable, id * a.ld_grad), p.at, a.d);
-        float total[W];
-        join_partials(to - from + 1, [&](int64_t q) { return place(q == 0 ? 2 * from + 1 : 2 * (from + q)); }, total);
+        join_partials(all, [&](int64_t q) { return sum_of(from + q * group); }, total);
         finish<OUT_BF16, ADD>(a, id, p, was, total);
     };
     const bool through = from_before && goes_on && first_id == last_id;

@@ -124,6 +124,26 @@ def test_gradient(gpu_lib, T, V, d, load, type, out):
             assert torch.equal(g[absent], before.cuda()[absent] if accumulate else torch.zeros_like(g[absent]))
 
 
+@pytest.mark.parametrize("type,out", PAIRS)
+@pytest.mark.parametrize("d", [24, 1033])
+def test_gradient_of_frequent_tokens(gpu_lib, d, type, out):
+    """Tokens whose sorted places go through 31 to 160 runs, some of them from the start of one to the end of another."""
+    counts = [8, 31 * 8, 32 * 8, 3, 33 * 8 + 5, 30 * 8 + 1, 8 * 40 - 1, 65 * 8 + 2, 1, 159 * 8 + 7, 64 * 8]
+    rng = np.random.default_rng(31)
+    ids = rng.permutation(np.repeat(np.arange(len(counts)), counts)).astype(np.int32)
+    T, V = len(ids), len(counts) + 1
+    dy, before = randn((T, d), type, 32), randn((V, d), out, 33, 3.0)
+    with Context(gpu_lib) as ctx:
+        for accumulate in (False, True):
+            got = []
+            for _ in range(3):
+                g = before.cuda().clone()
+                gpu_lib.moe_embed_backward(ctx, dy.cuda(), _dev(ids), 0.75, g, accumulate)
+                got.append(g)
+            _check_gradient(ids, dy, 0.75, f64(before), accumulate, out, got[0])
+            assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+
+
 @pytest.mark.parametrize("T,V,d,load", [(2048, 300, 2560, "zipf"), (2048, 300, 2561, "zipf"), (1025, 300, 5200, "uniform"), (2049, 300, 100, "one")])
 def test_gradient_where_the_rows_become_too_wide_for_one_launch(gpu_lib, T, V, d, load):
     rng = np.random.default_rng(d)
