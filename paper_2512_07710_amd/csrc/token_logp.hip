@@ -1,5 +1,6 @@
 // Log-probabilities of given tokens, entropy and the most likely tokens of rows of logits; and the logits' gradient from those of the first two.
 #include "softmax_rows.hpp"
+#include "step_rules.hpp"
 #include "ticket.hpp"
 
 namespace moe355 {
@@ -284,14 +285,14 @@ __global__ __launch_bounds__(THREADS, 8) void logp_kernel(const logp_args a) {
     __shared__ top_scratch<THREADS> s_top;
     __shared__ int32_t s_last;
     const int64_t r = PARTS ? blockIdx.x / a.parts : a.first + blockIdx.x;
-    const int part = PARTS ? blockIdx.x % a.parts : 0, tid = threadIdx.x, n = a.n, vecs = a.V / N;
+    const int part = PARTS ? blockIdx.x % a.parts : 0, tid = threadIdx.x, n = a.n;
     const void* const z = row_of<BF16>(a.logits, r * a.ld);
-    const int begin = PARTS ? min(part * a.part_vecs, vecs) : 0, end = PARTS ? min(begin + a.part_vecs, vecs) : vecs;
-    const int last = !PARTS || part == a.parts - 1 ? a.V : end * N;        // (the last part has the elements behind the vectors)
+    const row_part piece = PARTS ? part_of_row(a.V, N, part, a.parts, a.part_vecs) : part_of_row(a.V, N, 0, 1, a.V);
+    const int begin = piece.begin, end = piece.end, behind_at = piece.behind(tid);
     running_sums<BF16> sums(a.inv_temp * LOG2E);
     float bound = NAN;                         // what an alternative reaches (without alternatives nothing does)
     int i = begin + tid;
-    const float extra = end * N + tid < last ? load1<BF16>(z, end * N + tid) : -INFINITY;
+    const float extra = behind_at >= 0 ? load1<BF16>(z, behind_at) : -INFINITY;
     {
         u32x4 v[AT_ONCE];
         float tops[AT_ONCE];
@@ -318,14 +319,14 @@ __global__ __launch_bounds__(THREADS, 8) void logp_kernel(const logp_args a) {
         sums.sum(v);
         if (top >= bound) hold_above<BF16, THREADS>(v, tops, i, bound, 0, s_top);
     }
-    if (extra >= bound) hold(key_of(extra, end * N + tid), s_top);
+    if (extra >= bound) hold(key_of(extra, behind_at), s_top);
     sums.add_one(extra);
     softmax_stats st = block_join(sums.st, sums.c, s_scratch);
     int found = 0;
     if (n) {
         __syncthreads();
         const int count = s_top.count;
-        found = __builtin_expect(count <= s_top.HELD, 1) ? first_held<THREADS>(count, n, s_top) : select_again<BF16, THREADS>(z, begin, end, extra, end * N + tid, n, s_top);
+        found = __builtin_expect(count <= s_top.HELD, 1) ? first_held<THREADS>(count, n, s_top) : select_again<BF16, THREADS>(z, begin, end, extra, behind_at, n, s_top);
     }
     if constexpr (PARTS) {
         float* const mine = a.part_sums + (r * a.parts + part) * 3;
@@ -418,8 +419,9 @@ __global__ __launch_bounds__(THREADS) void logp_grad_kernel(const logp_grad_args
     __shared__ float s_d[LOGP_MAX_GIVEN], s_v[LOGP_MAX_GIVEN];
     __shared__ int s_id[LOGP_MAX_GIVEN];
     const int64_t b = a.first + blockIdx.x, r = b / a.parts;
-    const int part = (int)(b % a.parts), tid = threadIdx.x, vecs = a.V / N;
-    const int begin = min(part * a.part_vecs, vecs), end = min(begin + a.part_vecs, vecs), last = part == a.parts - 1 ? a.V : end * N;
+    const int tid = threadIdx.x;
+    const row_part piece = part_of_row(a.V, N, (int)(b % a.parts), a.parts, a.part_vecs);
+    const int begin = piece.begin, end = piece.end;
     const void* const z = row_of<BF16>(a.logits, r * a.ld);
     void* const out = row_of<GRAD_BF16>(a.dlogits, r * a.ld_grad);
     const float m = a.stats[2 * r], s = a.stats[2 * r + 1], dH = a.dentropy ? a.dentropy[r] : 0.f;
@@ -431,8 +433,8 @@ __global__ __launch_bounds__(THREADS) void logp_grad_kernel(const logp_grad_args
         s_v[tid] = v;
         s_d[tid] = d;
     }
-    const int behind = end * N + tid;                          // an element behind the vectors
-    const float extra = behind < last ? load1<BF16>(z, behind) : 0.f;
+    const int behind = piece.behind(tid);                      // an element behind the vectors
+    const float extra = behind >= 0 ? load1<BF16>(z, behind) : 0.f;
     __syncthreads();
     const int lane = tid & 63;                                 // (each wave has the given tokens, one to a lane)
     const int id = lane < a.m ? s_id[lane] : -1;
@@ -442,7 +444,7 @@ __global__ __launch_bounds__(THREADS) void logp_grad_kernel(const logp_grad_args
     if (!live) {                               // (the same for the whole block)
         const float none[N] = {};
         for (int i = begin + tid; i < end; i += THREADS) store_grad<GRAD_BF16, N>(out, i, none);
-        if (behind < last) store1<GRAD_BF16>(out, behind, 0.f);
+        if (behind >= 0) store1<GRAD_BF16>(out, behind, 0.f);
         return;
     }
     const float c = a.inv_temp * LOG2E, scale = a.inv_temp / s;
@@ -467,10 +469,10 @@ __global__ __launch_bounds__(THREADS) void logp_grad_kernel(const logp_grad_args
         for (int u = 0; u < AT_ONCE; ++u) put(v[u], i + u * THREADS);
     }
     for (; i < end; i += THREADS) put(T::load(z, i), i);
-    if (behind < last) store1<GRAD_BF16>(out, behind, of(extra));
+    if (behind >= 0) store1<GRAD_BF16>(out, behind, of(extra));
     // the given tokens, by the threads that have written their places: one with several gradients receives their sum as often
-    const int owner = id < end * N ? (id / N - begin) % THREADS : id - end * N;
-    const bool here = id >= begin * N && id < last && owner >> 6 == tid >> 6 && !(v_id <= LOWEST);
+    const int owner = id < piece.place ? (id / N - begin) % THREADS : id - piece.place;
+    const bool here = id >= begin * N && id < piece.place + piece.rest && owner >> 6 == tid >> 6 && !(v_id <= LOWEST);
     for (uint64_t left = __ballot(here); left; left &= left - 1) {
         const int j = __builtin_ctzll(left), to = __builtin_amdgcn_readlane(id, j);
         const float more = wave_total(id == to ? d : 0.f), v = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v_id), j));
