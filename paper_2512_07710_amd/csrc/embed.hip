@@ -1,6 +1,7 @@
 // Rows of an embedding table for token ids, and the table's gradient by sorted tokens.
 #include "grad_common.hpp"
 #include "lanes.hpp"
+#include "step_rules.hpp"
 #include "ticket.hpp"
 
 namespace moe355 {
@@ -15,7 +16,6 @@ constexpr int RANK_THREADS = 1024, RANK_CHUNK = 4096, RANK_ALONE = 8192, MERGE_W
 constexpr int SUM_AT_ONCE = 8;                         // sorted rows that a thread has on their way
 constexpr int JOIN_AT_ONCE = 8, JOIN_TWICE = 32;        // sums of a token's runs that a thread has on their way, and from how many on they are joined in groups first
 constexpr int EMBED_BLOCKS = 512;                      // that add up sorted tokens, about, of 2048 columns
-constexpr int ZERO_BITS = 4096;                        // rows that a block clears at most
 constexpr uint32_t NO_ID = 0xFFFFFFFFu;                // of tokens outside the table: behind the others
 
 // A thread's W columns of a row of d.  TAIL: d need not be a multiple of W; the last thread then reads the last W columns, and `skip` of them are its neighbour's,
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_few_kernel(const embed_ba
     constexpr int W = width_of(BF16, OUT_BF16), MASKS = TOKENS / 64, AT_ONCE = 8;
     __shared__ uint64_t s_same[MASKS];
     __shared__ uint16_t s_list[TOKENS];
-    __shared__ uint32_t s_seen[ZERO_BITS / 32];
+    __shared__ uint32_t s_seen[CLEAR_MOST / 32];
     __shared__ int32_t s_last;
     if (blockIdx.x >= a.sum_blocks) {
         if (!ADD) clear_rows<OUT_BF16>(a, (int)(blockIdx.x - a.sum_blocks), s_seen);
@@ -302,7 +302,7 @@ __global__ __launch_bounds__(RANK_THREADS, 8) void rank_tokens_kernel(const embe
                                                                       uint64_t* __restrict__ out) {
     constexpr int WAVES = RANK_THREADS / 64, SLICES = 64 / TOKENS, PAD = 4, LOADS = RANK_ALONE / RANK_THREADS;
     constexpr uint32_t LAST = 0x7FFFFFFFu;     // in place of ids outside the table; one more is a number still
-    static_assert(RANK_ALONE >= RANK_CHUNK && RANK_ALONE % (RANK_THREADS * SLICES) == 0 && RANK_ALONE >= ZERO_BITS / 32, "whole groups of ids for each lane");
+    static_assert(RANK_ALONE >= RANK_CHUNK && RANK_ALONE % (RANK_THREADS * SLICES) == 0 && RANK_ALONE >= CLEAR_MOST / 32, "whole groups of ids for each lane");
     __shared__ u32x4 s_ids[(RANK_ALONE + WAVES * SLICES * PAD) / 4];
     __shared__ uint32_t s_rank[WAVES][TOKENS];
     if ((int)blockIdx.x >= blocks) {
@@ -498,16 +498,12 @@ hipError_t launch_embed_sums(moe_ctx* c, embed_back_args a) {
     cut_row(pieces, a.parts, a.threads);
     a.width = (a.d + 7) / 8 * 8;
     if (!ADD) {
-        // rows to a block: few, so that no block ends late, but twice the bytes of the ids that it looks through (4096 x 4096 f32 of 131072: 64 rows 437 us, 16 386; 32768 x 7168 bf16 496 and 502)
-        int64_t rows = (a.V + 8191) / 8192;
-        const int64_t bytes = (int64_t)a.d * (OUT_BF16 ? 2 : 4), least = (8 * a.T + bytes - 1) / bytes;
-        if (rows < least) rows = least;
-        if (rows > ZERO_BITS) rows = ZERO_BITS;
-        a.zero_rows = (int)rows;
-        a.zero_blocks = (int)((a.V + rows - 1) / rows);
+        const clear_plan clear = clearing(a.V, a.T, (int64_t)a.d * (OUT_BF16 ? 2 : 4));
+        a.zero_rows = clear.rows;
+        a.zero_blocks = clear.blocks;
     }
     const bool few = a.T <= FEW_TOKENS;
-    if ((few || (a.T <= FEW_NARROW && a.T * a.d <= FEW_ELEMENTS)) && a.T * a.parts <= GRAD_TICKETS && a.T * a.width * sizeof(float) <= GRAD_WS_BYTES && a.zero_blocks <= EMBED_MAX_GRID / 2) {
+    if ((few || (a.T <= FEW_NARROW && a.T * a.d <= FEW_ELEMENTS)) && a.T * a.parts <= GRAD_TICKETS && a.T * a.width * sizeof(float) <= GRAD_WS_BYTES) {
         a.sum_blocks = a.T * a.parts;
         a.partial = static_cast<float*>(c->grad_ws);
         a.tickets = c->grad_tickets;

@@ -1,7 +1,10 @@
-"""How the two ends of a policy step deal their work (csrc/step_rules.hpp), compiled for the host: no place outside a row, whatever its length."""
+"""How the two ends of a policy step deal their work (csrc/step_rules.hpp), compiled for the host: no place outside a row, whatever its length, and blocks for every
+row of a table, however many there are."""
 import subprocess
+import sys
 
 import pytest
+import torch
 
 from paper_2512_07710_amd.build import CSRC, HIPCC, ROOT
 
@@ -33,6 +36,12 @@ int main() {
                 covered += expect - p.place;
             }
             printf("%d\n", bad | 8 * (covered != V));
+        } else if (!strcmp(what, "clear")) {                   // V, tokens, bytes of a row: rows to a block, blocks
+            int V;
+            int64_t T, bytes;
+            if (scanf("%d %ld %ld", &V, &T, &bytes) != 3) return 1;
+            const clear_plan p = clearing(V, T, bytes);
+            printf("%d %d\n", p.rows, p.blocks);
         }
     }
 }
@@ -62,3 +71,27 @@ def test_every_logit_of_a_row_has_one_place(ask, N, threads):
     cases = [(V, N, parts, threads) for V in LENGTHS for parts in (1, 2, 3, 16, 64, 2048)]
     for case, bad in zip(cases, ask("row", cases)):
         assert bad == 0, (case, bad)
+
+
+def test_every_row_of_a_table_is_cleared_by_one_block(ask):
+    cases = [(V, T, bytes) for V in LENGTHS + [8191, 8192, 8193, 2 ** 25, 2 ** 25 + 1, 2 ** 31 - 8192, 2 ** 31 - 8191, 2 ** 31 - 8193] for T in (0, 1, 1024, 2 ** 21)
+             for bytes in (2, 4, 14336, 262144)]
+    for (V, T, bytes), (rows, blocks) in zip(cases, ask("clear", cases)):
+        assert 1 <= rows <= 4096 and (blocks - 1) * rows < V <= blocks * rows and blocks <= 2 ** 19, (V, T, bytes, rows, blocks)
+        assert rows == min(4096, max(-(-V // 8192), -(-8 * T // bytes))), (V, T, bytes, rows)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="for machines without a GPU: the call would run on made-up pointers")
+@pytest.mark.parametrize("V", [2 ** 31 - 8192, 2 ** 31 - 8191, 2 ** 31 - 1])
+@pytest.mark.parametrize("T", [0, 1])
+def test_the_gradient_of_the_largest_tables_comes_back(V, T):
+    """With a status: the plan of its launches is the host's own arithmetic, and no launch succeeds here."""
+    code = f"""
+import ctypes
+import paper_2512_07710_amd as moe
+ctx = ctypes.create_string_buffer(b"\x40" * 4096, 4096)
+P = 1 << 20
+print("status", moe.load_library().moe_embed_backward(ctypes.addressof(ctx), P, P, {T}, {V}, 1, 1, 0, 1.0, 0, P, 1, 0))
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=ROOT)
+    assert r.returncode == 0 and "status -2" in r.stdout, (r.returncode, r.stdout, r.stderr[-300:])
