@@ -14,8 +14,7 @@ constexpr int64_t FEW_ELEMENTS = (int64_t)5 << 20;
 constexpr int FEW_RUN = 16;                            // rows of one token that one block adds up
 constexpr int RANK_THREADS = 1024, RANK_CHUNK = 4096, RANK_ALONE = 8192, MERGE_WAYS = 32, MERGE_AT_ONCE = 8;
 constexpr int SUM_AT_ONCE = 8;                         // sorted rows that a thread has on their way
-constexpr int JOIN_AT_ONCE = 8, JOIN_TWICE = 32;        // sums of a token's runs that a thread has on their way, and from how many on they are joined in groups first
-constexpr int EMBED_BLOCKS = 512;                      // that add up sorted tokens, about, of 2048 columns
+constexpr int JOIN_TWICE = 32;                         // sums of a token's runs from which on they are joined in groups first
 constexpr uint32_t NO_ID = 0xFFFFFFFFu;                // of tokens outside the table: behind the others
 
 // A thread's W columns of a row of d.  TAIL: d need not be a multiple of W; the last thread then reads the last W columns, and `skip` of them are its neighbour's,
@@ -144,7 +143,7 @@ struct embed_back_args {
     int32_t* tickets;
     // sorted tokens in runs of `run`
     const uint64_t* keys;
-    int run;
+    int run, fold;
 };
 __device__ inline uint32_t id_of(uint64_t key) { return (uint32_t)(key >> 32); }
 
@@ -392,7 +391,7 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(const embed_ba
     const int64_t r = blockIdx.x / a.parts, begin = r * a.run, end = begin + a.run < a.T ? begin + a.run : a.T;
     const int part = (int)(blockIdx.x % a.parts), lane = threadIdx.x & 63;
     const piece<W, TAIL> p(part * a.threads + threadIdx.x, a.d);
-    float sum[W] = {}, head[W] = {};
+    float sum[W] = {}, older[W] = {}, head[W] = {};            // (of the present token: rows since the last fold, those before it)
     const uint32_t first_id = id_of(a.keys[begin]), last_id = id_of(a.keys[end - 1]);
     const bool from_before = begin > 0 && first_id != NO_ID && id_of(a.keys[begin - 1]) == first_id;
     const bool goes_on = end < a.T && last_id != NO_ID && id_of(a.keys[end]) == last_id;
@@ -422,6 +421,8 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(const embed_ba
                 for (int j = 0; j < W; ++j) sum[j] += q + u < known ? v[u].at(j) : 0.f;
                 if (ADD) was[u].here();
                 if (!(ends >> (q + u) & 1)) continue;          // (no bits from `known` on)
+#pragma unroll
+                for (int j = 0; j < W; ++j) sum[j] += older[j];
                 if (open) {
 #pragma unroll
                     for (int j = 0; j < W; ++j) head[j] = sum[j];
@@ -430,10 +431,19 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(const embed_ba
                 }
                 open = false;
 #pragma unroll
-                for (int j = 0; j < W; ++j) sum[j] = 0.f;
+                for (int j = 0; j < W; ++j) sum[j] = older[j] = 0.f;
+            }
+        }
+        if (((k0 - begin + 64) & (a.fold - 1)) == 0) {
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                older[j] += sum[j];
+                sum[j] = 0.f;
             }
         }
     }
+#pragma unroll
+    for (int j = 0; j < W; ++j) sum[j] += older[j];
     auto place = [&](int64_t n) { return a.partial + n * a.width + p.nominal; };
     if (from_before && !open && p.in_row) store_partial(place(2 * r), head);
     if (goes_on && p.in_row) store_partial(place(open ? 2 * r : 2 * r + 1), sum);
@@ -459,7 +469,7 @@ __global__ __launch_bounds__(EMBED_THREADS) void embed_sum_kernel(const embed_ba
         int group = 1;
         float total[W];
         if (all >= JOIN_TWICE) {
-            while ((int64_t)group * group < all) group += JOIN_AT_ONCE;
+            group = runs_of_group(all);
             const int64_t groups = all / group, mine = (r - from) / group < groups ? (r - from) / group : groups - 1, first = from + mine * group;
             const int64_t n = mine == groups - 1 ? to - first + 1 : group;
             // (the ticket of a run in which no other token begins)
@@ -528,9 +538,8 @@ hipError_t launch_embed_sums(moe_ctx* c, embed_back_args a) {
     a.keys = keys;
     a.partial = reinterpret_cast<float*>(static_cast<uint64_t*>(c->grad_ws) + (2 * a.T + 1) / 2 * 2);
     const int64_t room = (GRAD_WS_BYTES - 16 * (a.T + 1)) / (2 * sizeof(float) * a.width);
-    // a run of 8 tokens, longer ones where there are enough blocks all the same, and where the workspace or the tickets would not hold the runs' sums
-    a.run = 8;
-    while ((a.T + a.run - 1) / a.run > room || a.T / (2 * a.run) * a.parts * width_of(BF16, OUT_BF16) >= EMBED_BLOCKS * 8 || (a.T + a.run - 1) / a.run * a.parts > GRAD_TICKETS) a.run *= 2;
+    a.run = (int)run_of_tokens(a.T, a.parts, width_of(BF16, OUT_BF16), room, GRAD_TICKETS);
+    a.fold = rows_of_fold(a.run);
     a.tickets = c->grad_tickets;
     const unsigned grid = (unsigned)((a.T + a.run - 1) / a.run * a.parts);
     if (a.d % width_of(BF16, OUT_BF16)) embed_sum_kernel<BF16, OUT_BF16, ADD, true><<<grid, a.threads, 0, c->stream>>>(a);

@@ -30,4 +30,27 @@ inline clear_plan clearing(int V, int64_t T, int64_t row_bytes) {
     return clear_plan{(int)rows, (int)((V + rows - 1) / rows)};
 }
 
+// Sorted tokens in runs, one to a block (a part of the columns each), by embed.hip: eight tokens, more where there are enough blocks all the same, and where the
+// workspace or the tickets would not hold the runs' sums.  room: runs that the workspace holds
+constexpr int EMBED_BLOCKS = 512;              // that add up sorted tokens, about, of 2048 columns
+inline int64_t run_of_tokens(int64_t T, int parts, int columns, int64_t room, int64_t tickets) {
+    int64_t run = 8;
+    while ((T + run - 1) / run > room || T / (2 * run) * parts * columns >= EMBED_BLOCKS * 8 || (T + run - 1) / run * parts > tickets) run *= 2;
+    return run;
+}
+// Rows of a run that are added up before their sum joins the run's: 64, the rows that a block looks at together, or about the root of a long run.  One after another
+// 2048 equal rows lose up to 500 half units of the last place, with no sign that evens it out, and so would every run
+__host__ __device__ inline int rows_of_fold(int64_t run) {
+    int fold = 64;
+    while ((int64_t)fold * fold < run) fold *= 2;
+    return fold;
+}
+// Runs of a token's sums that are joined first, of `all`: about the root
+constexpr int JOIN_AT_ONCE = 8;                // sums that a thread has on their way
+__host__ __device__ inline int runs_of_group(int64_t all) {
+    int group = 1;
+    while ((int64_t)group * group < all) group += JOIN_AT_ONCE;
+    return group;
+}
+
 }  // namespace moe355

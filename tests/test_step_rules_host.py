@@ -8,7 +8,8 @@ import torch
 
 from paper_2512_07710_amd.build import CSRC, HIPCC, ROOT
 
-PROGRAM = r"""
+TICKETS, WORKSPACE = (1 + 64 + 512) * 32, 64 << 20             # of a context
+PROGRAM = f"constexpr int TICKETS = {TICKETS};\n" + r"""
 #include <hip/hip_runtime.h>
 #include "step_rules.hpp"
 #include <cstdio>
@@ -42,6 +43,12 @@ int main() {
             if (scanf("%d %ld %ld", &V, &T, &bytes) != 3) return 1;
             const clear_plan p = clearing(V, T, bytes);
             printf("%d %d\n", p.rows, p.blocks);
+        } else if (!strcmp(what, "runs")) {                    // T, parts and columns of a thread, room: a run, rows of it to a fold, runs of a group
+            int parts, columns;
+            int64_t T, room;
+            if (scanf("%ld %d %d %ld", &T, &parts, &columns, &room) != 4) return 1;
+            const int64_t run = run_of_tokens(T, parts, columns, room, TICKETS);
+            printf("%ld %d %d\n", run, rows_of_fold(run), runs_of_group((T + run - 1) / run));
         }
     }
 }
@@ -95,3 +102,25 @@ print("status", moe.load_library().moe_embed_backward(ctypes.addressof(ctx), P, 
 """
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=ROOT)
     assert r.returncode == 0 and "status -2" in r.stdout, (r.returncode, r.stdout, r.stderr[-300:])
+
+
+def _additions(ask, cases):
+    """For (T, d, both arrays bf16): additions one after another that a row's share of its token's sum goes through at most."""
+    asked = []
+    for T, d, narrow in cases:
+        columns = 8 if narrow else 4
+        room = (WORKSPACE - 16 * (T + 1)) // (8 * -(-d // 8) * 8)
+        asked.append((T, -(-d // (columns * 256)), columns, room))
+    for (T, d, _), (_, parts, _, room), (run, fold, group) in zip(cases, asked, ask("runs", asked)):
+        runs = -(-T // run)
+        assert runs <= room and runs * parts <= TICKETS and run & (run - 1) == 0 and fold & (fold - 1) == 0 and fold % 64 == 0
+        groups = max(1, runs // group)
+        yield min(run, fold) + (run // fold if run > fold else 0) + (runs if runs < 32 else runs - (groups - 1) * group + groups)
+
+
+def test_sums_of_a_frequent_token_are_short_chains(ask):
+    small = [(2 ** 21, 64, False), (2 ** 21, 64, True), (2 ** 20, 512, False), (2 ** 20 + 77, 131, False), (2 ** 20 + 77, 131, True), (32768, 7168, True), (4096, 5120, False)]
+    assert max(_additions(ask, small)) <= 200
+    every = [(T, d, narrow) for T in (1025, 2049, 4096, 30000, 131072, 10 ** 6, 2 ** 20 + 1, 2 ** 21) for d in (1, 8, 100, 1000, 5120, 7168, 20000, 65536) for narrow in (True, False)]
+    chains = dict(zip(every, _additions(ask, every)))
+    assert max(n for (T, d, _), n in chains.items() if d <= 7168) <= 320 and max(chains.values()) <= 900, sorted(chains.items(), key=lambda c: -c[1])[:5]
