@@ -351,7 +351,8 @@ int moe_token_logp_backward(moe_ctx* ctx, const void* logits, int64_t ld, int32_
 int moe_grad_norm(moe_ctx* ctx, const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n, double* sum_sq, float* norm);
 
 /* Clipping to a largest norm [reserved]: outs[i] = grads[i] * min(1, max_norm / sqrt(sum_sq[0])), the factor rounded to fp32, the product to the gradient's type.
- *   outs: HOST array of n device pointers, or NULL: in place; outs[i] == grads[i] is in place as well; no array may overlap another otherwise.
+ *   outs: HOST array of n device pointers, or NULL: in place; outs[i] == grads[i] is in place as well; no array may overlap another otherwise
+ *   (an output over any gradient is refused; MOE_ENOMEM if host memory for that check cannot be had).
  *   A factor of 1 changes nothing, and gradients in place are then neither read nor written.  sum_sq 0: factor 1; infinite: 0; NaN: NaN, as their elements
  *   then come out.  max_norm >= 0, finite. */
 int moe_clip_grads(moe_ctx* ctx, const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n, const double* sum_sq, float max_norm,

@@ -1,7 +1,9 @@
 // C-ABI entry points of libmoe355: argument validation, context and workspace.
 #include "moe_internal.hpp"
 
+#include <algorithm>
 #include <cmath>
+#include <memory>
 #include <new>
 
 using namespace moe355;
@@ -88,6 +90,48 @@ bool list_ok(const void* const* arrays, const int64_t* counts, const int32_t* dt
         if (counts[i] && (!arrays[i] || !aligned(arrays[i], type_bytes(dtypes[i])))) return false;
     }
     return true;
+}
+
+// MOE_EINVAL if an output lies over a gradient other than its own, or over its own at another place: blocks would overwrite what others have not read yet
+int outs_apart(const void* const* grads, void* const* outs, const int64_t* counts, const int32_t* dtypes, int32_t n) {
+    struct range {
+        uintptr_t begin, end;
+        bool written;
+    };
+    auto range_of = [&](const void* p, int32_t i, bool written) { return range{(uintptr_t)p, (uintptr_t)p + (uintptr_t)counts[i] * type_bytes(dtypes[i]), written}; };
+    auto elsewhere = [&](int32_t i) { return counts[i] && outs[i] != grads[i]; };
+    // as a rule the outputs have memory of their own, or are all in place
+    uintptr_t first[2] = {UINTPTR_MAX, UINTPTR_MAX}, behind[2] = {};
+    for (int32_t i = 0; i < n; ++i)
+        for (int o = 0; o < 2; ++o) {
+            if (!(o ? elsewhere(i) : counts[i] != 0)) continue;
+            const range r = range_of(o ? outs[i] : grads[i], i, false);
+            first[o] = std::min(first[o], r.begin);
+            behind[o] = std::max(behind[o], r.end);
+        }
+    if (behind[0] <= first[1] || behind[1] <= first[0]) return MOE_OK;
+    // all of them in the order of their addresses
+    const std::unique_ptr<range[]> all(new (std::nothrow) range[2 * (size_t)n]);
+    if (!all) return MOE_ENOMEM;
+    range* const g = all.get();
+    int32_t ng = 0, no = 0;
+    for (int32_t i = 0; i < n; ++i)
+        if (counts[i]) g[ng++] = range_of(grads[i], i, outs[i] == grads[i]);
+    range* const o = g + ng;
+    for (int32_t i = 0; i < n; ++i)
+        if (elsewhere(i)) o[no++] = range_of(outs[i], i, true);
+    auto ahead = [](const range& a, const range& b) { return a.begin < b.begin; };
+    if (!std::is_sorted(g, o, ahead)) std::sort(g, o, ahead);
+    if (!std::is_sorted(o, o + no, ahead)) std::sort(o, o + no, ahead);
+    uintptr_t read_to = 0, written_to = 0;
+    for (int32_t i = 0, j = 0; i < ng || j < no;) {
+        const bool read = j == no || (i < ng && g[i].begin <= o[j].begin);
+        const range& r = read ? g[i++] : o[j++];
+        if ((read && r.begin < written_to) || (r.written && r.begin < read_to)) return MOE_EINVAL;
+        if (read) read_to = std::max(read_to, r.end);
+        if (r.written) written_to = std::max(written_to, r.end);
+    }
+    return MOE_OK;
 }
 
 }  // namespace
@@ -429,10 +473,9 @@ int moe_grad_norm(moe_ctx* c, const void* const* grads, const int64_t* counts, c
 int moe_clip_grads(moe_ctx* c, const void* const* grads, const int64_t* counts, const int32_t* dtypes, int32_t n, const double* sum_sq, float max_norm,
                    void* const* outs) {
     if (!c || !c->grad_ws || !list_ok(grads, counts, dtypes, n) || !sum_sq || !aligned(sum_sq, 8) || !(max_norm >= 0.f) || !std::isfinite(max_norm)) return MOE_EINVAL;
-    if (outs && n > 0 && !list_ok(outs, counts, dtypes, n)) return MOE_EINVAL;
-    for (int32_t i = 0; outs && i < n; ++i) {                  // (a gradient that is shifted onto itself)
-        const uintptr_t a = (uintptr_t)grads[i], b = (uintptr_t)outs[i], bytes = (uintptr_t)counts[i] * type_bytes(dtypes[i]);
-        if (a != b && (a > b ? a - b : b - a) < bytes) return MOE_EINVAL;
+    if (outs && n > 0) {
+        if (!list_ok(outs, counts, dtypes, n)) return MOE_EINVAL;
+        if (const int rc = outs_apart(grads, outs, counts, dtypes, n)) return rc;
     }
     return hip_rc(launch_clip_grads(c, grads, counts, dtypes, n, sum_sq, max_norm, outs));
 }
