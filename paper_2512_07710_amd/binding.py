@@ -460,7 +460,7 @@ def moe_token_logp_backward(ctx, logits, ids, dlogp, dentropy, stats, entropy, d
 
 class GradList:
     """Gradients (bf16 or f32, contiguous, apart from each other) as the list that moe_grad_norm and moe_clip_grads take: their addresses, counts and types,
-    read once.  It keeps the tensors; one that is given other memory later (set_, resize_) needs a new list."""
+    read once, which takes about a microsecond a tensor.  It keeps the tensors; one that is given other memory later (set_, resize_) needs a new list."""
 
     def __init__(self, tensors):
         self.tensors = tensors = list(tensors)
@@ -493,7 +493,8 @@ def moe_grad_norm(ctx, grads, sum_sq, norm=None) -> None:
 
 
 def moe_clip_grads(ctx, grads, sum_sq, max_norm, outs=None) -> None:
-    """grads, outs: GradLists, or tensors to make them of, of the same types and sizes; outs None: in place."""
+    """grads, outs: GradLists, or tensors to make them of, of the same types and sizes; outs None: in place.  An output has its gradient's place or memory of
+    its own."""
     lib = _lib or load_library()
     g = _list(grads)
     o = None if outs is None else _list(outs)

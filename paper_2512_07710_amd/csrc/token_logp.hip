@@ -209,7 +209,8 @@ __device__ __forceinline__ void hold_above(const u32x4 (&v)[AT_ONCE], const floa
 }
 // Where too many logits reach the bound (they ascend, or many are equal), the vectors from `begin` to `end` and `extra` once more, AT_ONCE of each thread at a time:
 // with the n first of those before, and again with a higher bound, the last of the n first among those that found a place, as long as there are too many (each
-// time HELD - 2 n fewer or more).  4096 x 131072 bf16, n = 8: ascending rows 740 us, equal logits 750, the first half masked 350.  Returns how many are in s.best.
+// time HELD - 2 n fewer or more).  4096 x 131072 bf16, n = 8 | 64: ascending rows 702 | 1323 us, equal logits 716 | 789, the first half masked 343 | 395.  Returns how
+// many are in s.best.
 template <bool BF16, int THREADS>
 __device__ __forceinline__ int select_again(const void* row, int begin, int end, float extra, int extra_at, int n, top_scratch<THREADS>& s) {
     uint64_t least = bound_key(LOWEST);
@@ -276,7 +277,7 @@ __device__ inline void write_row(const logp_args& a, int64_t r, const softmax_st
 // One pass over a row, or a part of it, for the sums and the alternatives.  The n-th largest of the largest logits that groups of threads have among
 // their first vectors bounds the alternatives from below, closely; what reaches the bound, a few times n logits, is held in LDS and ranked in the end.
 // Bound by the logits' bytes: 4096 x 131072 bf16, n = 8 187 us, 5.7 TB/s (a pass over the row for each alternative 4496);
-// an exponential for each logit is 16 % of the cycles.  Rows that end late bound the fewer ones: 333 x 50001 f32 17.5.
+// the vector ALU, an exponential for each logit among its work, is busy for 16 % of the waves' cycles.  Rows that end late bound the fewer ones: 333 x 50001 f32 17.5.
 template <bool BF16, int THREADS, bool PARTS>
 __global__ __launch_bounds__(THREADS, 8) void logp_kernel(const logp_args a) {
     typedef row_type<BF16> T;
@@ -411,7 +412,7 @@ struct logp_grad_args {
 
 // dz[v] = (sum_j dlogp_j (1[v = id_j] - p_v) - dH p_v (log p_v + H)) / temperature = 2^y (a y + b), and more at the given tokens.  A block has a row or, of
 // few rows, a part of one: the row's sums are there already.  Bound by the writes: 1024 x 131072 bf16 to bf16 102 us, 4.9 TB/s read and written; 100 x 50001 f32
-// in parts 8.9 (whole rows 22.6).
+// in parts 8.5 (whole rows 12.1).
 template <bool BF16, bool GRAD_BF16, int THREADS>
 __global__ __launch_bounds__(THREADS) void logp_grad_kernel(const logp_grad_args a) {
     typedef row_type<BF16> T;
